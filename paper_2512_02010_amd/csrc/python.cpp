@@ -1,4 +1,4 @@
-// Python's way to the C ABI (include/nvfp4_46.h): output allocation, argument marshalling and the call in
+// Python's way to the C ABI (include/nvfp4_46.h, include/finetune/nvfp4_finetune.h): output allocation, argument marshalling and the call in
 // one C function per entry point.  binding.py hands in the entry points of the library that it loaded and the
 // exception for statuses other than NVFP4_OK.
 //
@@ -11,12 +11,14 @@
 #include <cstring>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include "finetune/nvfp4_finetune.h"
 #include "gemm_shapes.hpp"
 #include "layer.hpp"
 #include "nvfp4_46.h"
@@ -41,6 +43,16 @@ struct LayerEntryPoints {
   decltype(&nvfp4_46_wgrad_operands) wgrad_operands;
 };
 LayerEntryPoints layer;
+// ... and of finetune.py's ENTRY_POINTS.
+struct FinetuneEntryPoints {
+  decltype(&nvfp4_adapters_workspace_bytes) adapters_workspace_bytes;
+  decltype(&nvfp4_adapters_forward) adapters_forward;
+  decltype(&nvfp4_adapters_backward) adapters_backward;
+  decltype(&nvfp4_distill_forward) distill_forward;
+  decltype(&nvfp4_distill_backward) distill_backward;
+  decltype(&nvfp4_distill_step) distill_step;
+};
+FinetuneEntryPoints finetune;
 PyObject *error_class;     // Nvfp4Error(status, name of the entry point)
 PyObject *empty;           // (shape, dtype, device) -> tensor
 
@@ -504,6 +516,212 @@ PyObject *product_of_columns(PyObject *const *a, Py_ssize_t n) {
   return out.release();
 }
 
+// ---- finetune.py: adapters and distillation.  Tensors of any class, rows with a stride; what the library needs besides is
+// allocated here, for the stream that the call's work goes to (memory that the allocator holds for another stream could be handed
+// on while this one still uses it).
+
+const at::Tensor &tensor(PyObject *o, const char *what) {
+  if (!THPVariable_Check(o)) PyErr_Format(PyExc_AssertionError, "%s must be a tensor", what);
+  else if (THPVariable_Unpack(o).is_cuda()) return THPVariable_Unpack(o);
+  else PyErr_Format(PyExc_AssertionError, "%s must be a device tensor", what);
+  throw Failed{};
+}
+[[noreturn]] void misfit(const char *what, const char *wanted) {
+  PyErr_Format(PyExc_AssertionError, "%s must be %s", what, wanted);
+  throw Failed{};
+}
+// A dense tensor of one type, of this shape, on the device of `like`.
+void *dense(PyObject *o, const char *what, const at::Tensor &like, at::IntArrayRef shape, at::ScalarType type) {
+  const at::Tensor &t = tensor(o, what);
+  if (t.device() != like.device()) misfit(what, "on the device of the others");
+  if (t.scalar_type() != type) misfit(what, c10::toString(type));
+  if (t.sizes() != shape) misfit(what, "of a shape that fits the others");
+  if (!t.is_contiguous()) misfit(what, "contiguous");
+  return t.data_ptr();
+}
+// Rows [rows][cols] with adjacent columns; *ld their stride (that of no or one row is the row's length).
+void *rows_of(PyObject *o, const char *what, const at::Tensor &like, int64_t rows, int64_t cols, at::ScalarType type, int64_t *ld) {
+  const at::Tensor &t = tensor(o, what);
+  if (t.device() != like.device()) misfit(what, "on the device of the others");
+  if (t.scalar_type() != type) misfit(what, c10::toString(type));
+  if (t.dim() != 2 || t.size(0) != rows || t.size(1) != cols) misfit(what, "of a shape that fits the others");
+  if (cols > 1 && t.stride(1) != 1) misfit(what, "of adjacent columns");
+  *ld = rows > 1 ? t.stride(0) : cols;
+  return t.data_ptr();
+}
+// The caller's workspace, or one of `need` bytes that lives as long as this.
+struct Scratch {
+  void *p;
+  size_t bytes;
+  PyObject *held;
+  Scratch(PyObject *given, int64_t need, PyObject *like, PyObject *allocate) : held(nullptr) {
+    const bool own = given == Py_None;
+    held = own ? Owned(new_tensor({need}, at::kByte, like, allocate)).release() : Py_NewRef(given);
+    try {
+      bytes = own ? (size_t)need : tensor(held, "workspace").nbytes();
+      p = pointer(held);
+    } catch (...) {
+      Py_DECREF(held);
+      throw;
+    }
+  }
+  Scratch(const Scratch &) = delete;
+  ~Scratch() { Py_XDECREF(held); }
+};
+// The stream of a call, current while this lives.
+struct OnStream {
+  c10::hip::HIPStream s;
+  c10::OptionalStreamGuard guard;
+  OnStream(PyObject *o, const at::Tensor &like)
+      : s(o == Py_None ? c10::hip::getCurrentHIPStream(like.device().index())
+                       : c10::hip::getStreamFromExternal(static_cast<hipStream_t>(reinterpret_cast<void *>(word(o))),
+                                                         like.device().index())) {
+    if (o != Py_None) guard.reset_stream(s.unwrap());
+  }
+  void *handle() const { return s.stream(); }
+};
+
+// x, base or None, a, b, which, scales, want_h, out or None, workspace or None, allocate, stream
+PyObject *adapters_forward(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 11);
+  const at::Tensor &x = tensor(v[0], "x"), &a = tensor(v[2], "a"), &b = tensor(v[3], "b");
+  if (x.dim() != 2 || a.dim() != 3 || b.dim() != 3) fail(PyExc_AssertionError, "x must be a matrix, a and b one for each adapter");
+  nvfp4_adapters_params p{};
+  p.tokens = x.size(0), p.inp = x.size(1), p.out = b.size(1), p.adapters = a.size(0), p.rank = a.size(1);
+  const void *const px = rows_of(v[0], "x", x, p.tokens, p.inp, at::kBFloat16, &p.ld_x);
+  const void *const pa = dense(v[2], "a", x, {p.adapters, p.rank, p.inp}, at::kBFloat16);
+  const void *const pb = dense(v[3], "b", x, {p.adapters, p.out, p.rank}, at::kBFloat16);
+  const auto *const pw = static_cast<const int32_t *>(dense(v[4], "which", x, {p.tokens}, at::kInt));
+  const auto *const ps = static_cast<const float *>(dense(v[5], "scales", x, {p.adapters}, at::kFloat));
+  PyObject *const typed = v[1] != Py_None ? v[1] : v[7];
+  const at::ScalarType type = typed != Py_None && tensor(typed, "base").scalar_type() == at::kFloat ? at::kFloat : at::kBFloat16;
+  p.out_dtype = type == at::kFloat ? NVFP4_OUT_F32 : NVFP4_OUT_BF16;
+  const void *const base = v[1] == Py_None ? nullptr : rows_of(v[1], "base", x, p.tokens, p.out, type, &p.ld_base);
+  const int want_h = PyObject_IsTrue(v[6]);
+  if (want_h < 0) return nullptr;
+  const OnStream on(v[10], x);
+  Owned out = v[7] == Py_None ? Owned(new_tensor({p.tokens, p.out}, type, v[0], v[9])) : Owned(Py_NewRef(v[7]));
+  void *const po = rows_of(out.o, "out", x, p.tokens, p.out, type, &p.ld_out);
+  Owned h = want_h ? Owned(new_tensor({p.tokens, p.rank}, at::kFloat, v[0], v[9])) : Owned(Py_NewRef(Py_None));
+  float *const ph = static_cast<float *>(pointer(h.o));
+  const Scratch w(v[8], (int64_t)finetune.adapters_workspace_bytes(&p, 0), v[0], v[9]);
+  run("nvfp4_adapters_forward", [&] {
+    return finetune.adapters_forward(px, &p, base, pa, pb, pw, ps, ph, po, w.p, w.bytes, on.handle());
+  });
+  return want_h ? PyTuple_Pack(2, out.o, h.o) : out.release();
+}
+
+// dy, x, h, a, b, which, scales, dx_base or None, want_dx, out or None, workspace or None, allocate, stream
+PyObject *adapters_backward(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 13);
+  const at::Tensor &x = tensor(v[1], "x"), &a = tensor(v[3], "a"), &b = tensor(v[4], "b");
+  if (x.dim() != 2 || a.dim() != 3 || b.dim() != 3) fail(PyExc_AssertionError, "x must be a matrix, a and b one for each adapter");
+  nvfp4_adapters_params p{};
+  p.tokens = x.size(0), p.inp = x.size(1), p.out = b.size(1), p.adapters = a.size(0), p.rank = a.size(1);
+  const void *const pdy = rows_of(v[0], "dy", x, p.tokens, p.out, at::kBFloat16, &p.ld_dy);
+  const void *const px = rows_of(v[1], "x", x, p.tokens, p.inp, at::kBFloat16, &p.ld_x);
+  const auto *const ph = static_cast<const float *>(dense(v[2], "h", x, {p.tokens, p.rank}, at::kFloat));
+  const void *const pa = dense(v[3], "a", x, {p.adapters, p.rank, p.inp}, at::kBFloat16);
+  const void *const pb = dense(v[4], "b", x, {p.adapters, p.out, p.rank}, at::kBFloat16);
+  const auto *const pw = static_cast<const int32_t *>(dense(v[5], "which", x, {p.tokens}, at::kInt));
+  const auto *const ps = static_cast<const float *>(dense(v[6], "scales", x, {p.adapters}, at::kFloat));
+  const int want_dx = PyObject_IsTrue(v[8]);
+  if (want_dx < 0) return nullptr;
+  const void *const base = v[7] == Py_None ? nullptr : rows_of(v[7], "dx_base", x, p.tokens, p.inp, at::kBFloat16, &p.ld_base);
+  const OnStream on(v[12], x);
+  Owned dx = !want_dx ? Owned(Py_NewRef(Py_None))
+             : v[9] == Py_None ? Owned(new_tensor({p.tokens, p.inp}, at::kBFloat16, v[1], v[11])) : Owned(Py_NewRef(v[9]));
+  void *const pdx = want_dx ? rows_of(dx.o, "out", x, p.tokens, p.inp, at::kBFloat16, &p.ld_out) : nullptr;
+  Owned da(new_tensor({p.adapters, p.rank, p.inp}, at::kFloat, v[1], v[11]));
+  Owned db(new_tensor({p.adapters, p.out, p.rank}, at::kFloat, v[1], v[11]));
+  float *const pda = static_cast<float *>(pointer(da.o)), *const pdb = static_cast<float *>(pointer(db.o));
+  const Scratch w(v[10], (int64_t)finetune.adapters_workspace_bytes(&p, 1), v[1], v[11]);
+  run("nvfp4_adapters_backward", [&] {
+    return finetune.adapters_backward(pdy, &p, px, ph, pa, pb, pw, ps, base, pdx, pda, pdb, w.p, w.bytes, on.handle());
+  });
+  return PyTuple_Pack(3, dx.o, da.o, db.o);
+}
+
+// What the three distillation calls have in common: logits, teacher, index, temperature
+struct Distill {
+  nvfp4_distill_params p{};
+  const at::Tensor &x;
+  const void *logits, *teacher, *index;
+  explicit Distill(PyObject *const *v) : x(tensor(v[0], "logits")) {
+    const at::Tensor &t = tensor(v[1], "teacher"), &i = tensor(v[2], "index");
+    if (x.dim() != 2 || t.dim() != 2) fail(PyExc_AssertionError, "logits and teacher must be matrices");
+    const auto known = [](at::ScalarType s) { return s == at::kFloat || s == at::kBFloat16; };
+    if (!known(x.scalar_type()) || !known(t.scalar_type())) fail(PyExc_AssertionError, "logits and teacher must be BF16 or fp32");
+    if (i.scalar_type() != at::kInt && i.scalar_type() != at::kLong) fail(PyExc_AssertionError, "index must be int32 or int64");
+    p.rows = x.size(0), p.vocab = x.size(1), p.top = t.size(1);
+    p.x_dtype = x.scalar_type() == at::kFloat ? NVFP4_X_F32 : NVFP4_X_BF16;
+    p.teacher_dtype = t.scalar_type() == at::kFloat ? NVFP4_X_F32 : NVFP4_X_BF16;
+    p.index_dtype = i.scalar_type() == at::kLong ? NVFP4_INDEX_I64 : NVFP4_INDEX_I32;
+    p.temperature = number(v[3]);
+    logits = rows_of(v[0], "logits", x, p.rows, p.vocab, x.scalar_type(), &p.ld);
+    teacher = dense(v[1], "teacher", x, {p.rows, p.top}, t.scalar_type());
+    index = dense(v[2], "index", x, {p.rows, p.top}, i.scalar_type());
+  }
+  const float *per_row(PyObject *o, const char *what) const {
+    return o == Py_None ? nullptr : static_cast<const float *>(dense(o, what, x, {p.rows}, at::kFloat));
+  }
+  // The gradient has the logits' strides and begins where they do within 16 bytes, so that its rows can be written as theirs are read.
+  Owned gradient(PyObject *given, PyObject *like, PyObject *allocate) const {
+    if (given != Py_None) return Owned(Py_NewRef(given));
+    const int64_t first = (int64_t)(reinterpret_cast<uintptr_t>(logits) % 16 / x.element_size());
+    if (p.ld == p.vocab && first == 0) return Owned(new_tensor({p.rows, p.vocab}, x.scalar_type(), like, allocate));
+    const Owned all(new_tensor({first + p.rows * p.ld}, x.scalar_type(), like, allocate));
+    const at::Tensor &t = THPVariable_Unpack(all.o);
+    return Owned(THPVariable_Wrap(t.as_strided({p.rows, p.vocab}, {p.ld, 1}, t.storage_offset() + first)));
+  }
+  void *gradient_rows(PyObject *o) const {
+    int64_t ld;
+    void *const d = rows_of(o, "out", x, p.rows, p.vocab, x.scalar_type(), &ld);
+    if (ld != p.ld) misfit("out", "of the logits' strides");
+    return d;
+  }
+};
+
+// logits, teacher, index, temperature, allocate, stream -> loss, lse
+PyObject *distill_forward(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 6);
+  const Distill d(v);
+  const OnStream on(v[5], d.x);
+  Owned loss(new_tensor({d.p.rows}, at::kFloat, v[0], v[4])), lse(new_tensor({d.p.rows}, at::kFloat, v[0], v[4]));
+  float *const pl = static_cast<float *>(pointer(loss.o)), *const pe = static_cast<float *>(pointer(lse.o));
+  run("nvfp4_distill_forward", [&] { return finetune.distill_forward(d.logits, &d.p, d.teacher, d.index, pl, pe, on.handle()); });
+  return PyTuple_Pack(2, loss.o, lse.o);
+}
+
+// logits, teacher, index, temperature, lse, weight or None, out or None, allocate, stream -> dlogits
+PyObject *distill_backward(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 9);
+  const Distill d(v);
+  if (v[4] == Py_None) misfit("lse", "a tensor");
+  const float *const lse = d.per_row(v[4], "lse"), *const weight = d.per_row(v[5], "weight");
+  const OnStream on(v[8], d.x);
+  Owned out = d.gradient(v[6], v[0], v[7]);
+  void *const po = d.gradient_rows(out.o);
+  run("nvfp4_distill_backward",
+      [&] { return finetune.distill_backward(d.logits, &d.p, d.teacher, d.index, lse, weight, po, on.handle()); });
+  return out.release();
+}
+
+// logits, teacher, index, temperature, weight or None, out or None, allocate, stream -> loss, dlogits
+PyObject *distill_step(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 8);
+  const Distill d(v);
+  const float *const weight = d.per_row(v[4], "weight");
+  const OnStream on(v[7], d.x);
+  Owned out = d.gradient(v[5], v[0], v[6]);
+  void *const po = d.gradient_rows(out.o);
+  Owned loss(new_tensor({d.p.rows}, at::kFloat, v[0], v[6]));
+  float *const pl = static_cast<float *>(pointer(loss.o));
+  run("nvfp4_distill_step",
+      [&] { return finetune.distill_step(d.logits, &d.p, d.teacher, d.index, weight, pl, po, on.handle()); });
+  return PyTuple_Pack(2, loss.o, out.o);
+}
+
 template <typename Points>
 void take_addresses(Points &points, PyObject *const *a, Py_ssize_t n) {
   constexpr Py_ssize_t kEntries = sizeof(Points) / sizeof(void *);
@@ -525,12 +743,18 @@ PyObject *connect_layer(PyObject *const *a, Py_ssize_t n) {
   take_addresses(layer, a, n);
   Py_RETURN_NONE;
 }
+PyObject *connect_finetune(PyObject *const *a, Py_ssize_t n) {
+  take_addresses(finetune, a, n);
+  Py_RETURN_NONE;
+}
 
 #define NV_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(guarded<f>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {NV_METHOD(connect), NV_METHOD(connect_layer),
                            NV_METHOD(tensor_scale), NV_METHOD(tensor_scale_ws), NV_METHOD(quantize),
                          NV_METHOD(scale_quantize), NV_METHOD(dequantize), NV_METHOD(fake_quant), NV_METHOD(gemm),
                          NV_METHOD(product_of_rows), NV_METHOD(product_of_columns),
+                         NV_METHOD(connect_finetune), NV_METHOD(adapters_forward), NV_METHOD(adapters_backward),
+                         NV_METHOD(distill_forward), NV_METHOD(distill_backward), NV_METHOD(distill_step),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "nvfp4_46_python", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
