@@ -34,15 +34,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct Tile {
-  int32_t start, count, adapter, unused;
+  int32_t adapter, count;      // (tokens without an adapter come last, as tiles of adapter -1)
 };
 
-// What k_plan writes.  Tokens without an adapter come last, as tiles of adapter -1.
+// What k_plan writes.
 struct Plan {
   int32_t *count;                               // tiles
   int32_t *tile_begin;                          // [L + 2]: the first tile of every adapter, of those without, the end
-  int32_t *order;                               // [T]
   Tile *tiles;
+  int32_t *order;                               // [tiles][32]: their tokens, -1 past a tile's last
 };
 
 // Where tiles come from: a plan, or (few tokens) `which` itself.
@@ -70,16 +70,15 @@ struct TileTokens {
 // the tokens before it have its adapter, and the next of them go with it.
 template <int NT>
 __device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t index, int rows) {
-  Tile t{0, 0, -1, 0};
+  Tile t{-1, 0};
   if (!k.few) {
     const int halves = kTile / rows;
     if (index / halves >= *k.plan.count) return t;
     t = k.plan.tiles[index / halves];
-    const int32_t skip = index % halves * rows;
-    t.start += skip;
-    t.count = t.count - skip < rows ? t.count - skip : rows;
-    if (t.count <= 0) return {0, 0, -1, 0};
-    if ((int)threadIdx.x < t.count) shared.token[threadIdx.x] = k.plan.order[t.start + threadIdx.x];
+    t.count -= index % halves * rows;
+    if (t.count <= 0) return {-1, 0};
+    if (t.count > rows) t.count = rows;
+    if ((int)threadIdx.x < t.count) shared.token[threadIdx.x] = k.plan.order[(int64_t)index * rows + threadIdx.x];
     __syncthreads();
     return t;
   }
@@ -96,7 +95,7 @@ __device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t in
     return n;
   };
   const int32_t mine = before(index);
-  if (mine % kFewTile) return {0, 0, -1, 0};
+  if (mine % kFewTile) return {-1, 0};
   int32_t all = 0;
   for (int w = 0; w < kFewTokens / 64; ++w) all += __popcll(shared.same[w]);
   t.count = all - mine < kFewTile ? all - mine : kFewTile;
@@ -112,6 +111,9 @@ __device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t in
 // ---- pieces ---------------------------------------------------------------------------------------------------------
 
 __device__ inline bf16x8 load8(const __bf16 *p) { return *reinterpret_cast<const bf16x8 *>(p); }
+// A wave's number as the one value that it is: conditions on it become branches.  Lanes that are masked off do not keep the matrix
+// unit from writing, so a product under a condition has to be jumped over, not masked.
+__device__ inline int wave_of(uint32_t thread) { return __builtin_amdgcn_readfirstlane(thread / 64); }
 __device__ inline f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 // v as a sum of BF16 terms: two leave 2^-16 of it, three 2^-24.  Of an infinity or NaN the first term is all there is.
@@ -125,32 +127,43 @@ __device__ inline __bf16 term(float v, int which) {
   return which == 1 ? mid : (__bf16)(rest - (float)mid);
 }
 
+// Eight ranks of a token, from `first`: their three terms where k_outer looks for them, [tile][term][rank][token].
+__device__ inline void put_terms(__bf16 *terms, int64_t tile, int32_t ranks, int token, int first, const float *v) {
+  if (first >= ranks) return;
+  for (int which = 0; which < 3; ++which)
+    for (int k = 0; k < 8; ++k) terms[((tile * 3 + which) * ranks + first + k) * kTile + token] = term(v[k], which);
+}
+
 // ---- k_shrink ---------------------------------------------------------------------------------------------------------
 
 struct ShrinkArgs {
   Tokens tokens;
   const __bf16 *x, *w;         // [T] rows of `width`, and [L][rank][width]
-  float *h;                    // [splits][T][rank]
+  float *parts;                // [splits][T][pitch]
+  float *h;                    // [T][rank], where one split is all and it is wanted; 0 for tokens without an adapter
+  // backwards: the forward pass' h [T][rank], whose terms go to k_outer from here
+  const float *terms_of, *scales;
+  __bf16 *terms;
   int64_t ld, width;
-  int32_t rank, steps;         // steps of 64 columns of a split
-  bool zero;                   // rows without an adapter get zeros
+  int32_t rank, pitch, steps;  // steps of 64 columns of a split
+  int32_t term_ranks;
 };
 
 // D[token][rank]: rows of x against rows of w, both adjacent in the summed index.  A lane takes 16 columns of a step, of row
-// lane % 16 of each side: 128 bytes of a row lie in one step.  The waves of a workgroup take every W-th step of its split.
-template <int MT, int RT, int W>
+// lane % 16 of each side: 128 bytes of a row lie in one step.  The waves of a workgroup take every W-th step of its split, D of them
+// on their way at a time.
+template <int MT, int RT, int W, int D>
 __global__ void __launch_bounds__(W * 64) k_shrink(ShrinkArgs a) {
   __shared__ TileTokens shared;
   __shared__ float part[W][MT * RT * 256];
   const Tile t = find_tile<W * 64>(a.tokens, shared, blockIdx.x, MT * 16);
   if (t.count == 0) return;
-  float *const h = a.h + (int64_t)blockIdx.y * a.tokens.T * a.rank;
   if (t.adapter < 0) {
-    if (a.zero)
-      for (int i = threadIdx.x; i < t.count * a.rank; i += W * 64) h[(int64_t)shared.token[i / a.rank] * a.rank + i % a.rank] = 0.0f;
+    if (a.h)
+      for (int i = threadIdx.x; i < t.count * a.rank; i += W * 64) a.h[(int64_t)shared.token[i / a.rank] * a.rank + i % a.rank] = 0.0f;
     return;
   }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row = lane & 15, group = lane / 16;
+  const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   const __bf16 *x[MT], *w[RT];
   for (int i = 0; i < MT; ++i) {
     const int n = i * 16 + row < t.count ? i * 16 + row : t.count - 1;            // (rows past the tile's are not kept)
@@ -161,58 +174,67 @@ __global__ void __launch_bounds__(W * 64) k_shrink(ShrinkArgs a) {
     w[i] = a.w + ((int64_t)t.adapter * a.rank + n) * a.width + group * 16;
   }
   f32x4 acc[MT][RT] = {};
-  const int64_t first = (int64_t)blockIdx.y * a.steps, all = (a.width + kBlock - 1) / kBlock;
-  const int64_t last = first + a.steps < all ? first + a.steps : all;
-  for (int64_t s = first + wave; s < last; s += W) {
-    const int64_t k = s * kBlock;
-    bf16x8 xs[MT][2], ws[RT][2];
-    if (k + kBlock <= a.width) {
-      for (int i = 0; i < MT; ++i)
-        for (int c = 0; c < 2; ++c) xs[i][c] = load8(x[i] + k + c * 8);
-      for (int i = 0; i < RT; ++i)
-        for (int c = 0; c < 2; ++c) ws[i][c] = load8(w[i] + k + c * 8);
-    } else {
-      for (int c = 0; c < 2; ++c) {
-        const bool in = k + group * 16 + c * 8 < a.width;
-        for (int i = 0; i < MT; ++i) xs[i][c] = in ? load8(x[i] + k + c * 8) : bf16x8{};
-        for (int i = 0; i < RT; ++i) ws[i][c] = in ? load8(w[i] + k + c * 8) : bf16x8{};
-      }
+  bf16x8 xs[D][MT][2], ws[D][RT][2];
+  const int32_t all = (int32_t)((a.width + kBlock - 1) / kBlock), first = (int32_t)blockIdx.y * a.steps + wave;
+  const int32_t last = ((int32_t)blockIdx.y + 1) * a.steps < all ? ((int32_t)blockIdx.y + 1) * a.steps : all;
+  const auto fetch = [&](int d, int32_t s) {
+    if (s >= last) return;
+    const int64_t k = (int64_t)s * kBlock;
+    for (int c = 0; c < 2; ++c) {
+      const bool in = k + kBlock <= a.width || k + group * 16 + c * 8 < a.width;
+      for (int i = 0; i < MT; ++i) xs[d][i][c] = in ? load8(x[i] + k + c * 8) : bf16x8{};
+      for (int i = 0; i < RT; ++i) ws[d][i][c] = in ? load8(w[i] + k + c * 8) : bf16x8{};
     }
-    for (int c = 0; c < 2; ++c)
-      for (int i = 0; i < MT; ++i)
-        for (int j = 0; j < RT; ++j) acc[i][j] = multiply(xs[i][c], ws[j][c], acc[i][j]);
-  }
+  };
+#pragma unroll
+  for (int d = 0; d < D - 1; ++d) fetch(d, first + d * W);
+  for (int32_t s = first; s < last; s += D * W)
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      fetch((d + D - 1) % D, s + (d + D - 1) * W);
+      if (s + d * W < last)
+        for (int c = 0; c < 2; ++c)
+          for (int i = 0; i < MT; ++i)
+            for (int j = 0; j < RT; ++j) acc[i][j] = multiply(xs[d][i][c], ws[d][j][c], acc[i][j]);
+    }
   for (int i = 0; i < MT; ++i)
     for (int j = 0; j < RT; ++j)
       for (int v = 0; v < 4; ++v) part[wave][(i * RT + j) * 256 + (group * 4 + v) * 16 + row] = acc[i][j][v];
   __syncthreads();
+  float *const parts = a.parts + (int64_t)blockIdx.y * a.tokens.T * a.pitch;
   for (int e = threadIdx.x; e < MT * RT * 256; e += W * 64) {
     const int n = e / (RT * 256) * 16 + e % 256 / 16, rank = e / 256 % RT * 16 + e % 16;
     float s = 0.0f;
     for (int i = 0; i < W; ++i) s += part[i][e];
-    if (n < t.count && rank < a.rank) h[(int64_t)shared.token[n] * a.rank + rank] = s;
+    if (n < t.count && rank < a.pitch) {
+      parts[(int64_t)shared.token[n] * a.pitch + rank] = rank < a.rank ? s : 0.0f;
+      if (a.h && rank < a.rank) a.h[(int64_t)shared.token[n] * a.rank + rank] = s;
+    }
   }
+  if (a.terms_of && blockIdx.y == 0)
+    for (int e = threadIdx.x; e < kTile * a.term_ranks / 8; e += W * 64) {
+      const int n = e % kTile, from = e / kTile * 8;
+      float v[8];
+      for (int k = 0; k < 8; ++k)
+        v[k] = n < t.count && from + k < a.rank ? a.scales[t.adapter] * a.terms_of[(int64_t)shared.token[n] * a.rank + from + k] : 0.0f;
+      put_terms(a.terms, blockIdx.x, a.term_ranks, n, from, v);
+    }
 }
 
 // ---- k_expand ---------------------------------------------------------------------------------------------------------
 
 struct ExpandArgs {
   Tokens tokens;
-  const float *h;              // [parts][T][rank]
-  float *h_out;                // their sum, where it is wanted and k_shrink has not written it; or nullptr
+  const float *parts;          // [splits][T][h_pitch]
+  float *h;                    // their sum [T][rank], where it is wanted and k_shrink has not written it; or nullptr
+  __bf16 *terms;               // backwards: the terms of s h for k_outer; or nullptr
   const __bf16 *w;             // [L][width] rows of `rank`, `pitch` apart
   const float *scales;
   const void *base;
-  void *out;
+  void *out;                   // nullptr: only the terms
   int64_t ld_base, ld_out, width;
-  int32_t rank, pitch, parts;
+  int32_t rank, pitch, h_pitch, splits, term_ranks;
 };
-
-__device__ inline float h_of(const float *h, int32_t parts, int64_t stride) {
-  float s = h[0];
-  for (int p = 1; p < parts; ++p) s += h[p * stride];
-  return s;
-}
 
 // Eight ranks of a row of w; where rows are not whole pieces of 16 bytes, one by one.
 __device__ inline bf16x8 load_ranks(const __bf16 *row, int first, int rank, int pitch) {
@@ -247,25 +269,24 @@ __device__ inline void store_columns(T *p, const float *v) {
   }
 }
 
-// D[column][token]: rows of w against h.  The summed index runs over pieces of eight ranks of every term of h (term), four pieces to a
-// product: piece q is term q / pieces of ranks q % pieces, against the same ranks of w.  Row 4 a + b of product m of a block is column
-// 16 a + 4 m + b, so that a lane ends up with 16 adjacent columns of its token.
-template <typename T, int MT, int TERMS, int NM>
+// D[column][token]: rows of w against s h, which enters as terms (term).  Row 4 a + b of product p of a block is column
+// 16 a + 4 p + b, so that a lane ends up with 16 adjacent columns of its token.  The summed index of a product is four pieces of
+// eight ranks: F > 0: 32 ranks of one term, F times.  F == 0, rank <= 16: the one or two pieces of every term side by side.
+// The workgroup sums the parts of h and splits them once, into LDS.
+template <typename T, int MT, int F>
 __global__ void __launch_bounds__(256) k_expand(ExpandArgs a) {
+  constexpr int kTerms = sizeof(T) == 4 ? 3 : 2, kSpans = F ? F : 1, kProducts = F ? kTerms : kTerms - 1;
   __shared__ TileTokens shared;
+  __shared__ bf16x8 split[MT * 16][kTerms * kSpans * 4 + 1];        // (an odd number of pieces: a row a bank further)
   const Tile t = find_tile<256>(a.tokens, shared, blockIdx.x, MT * 16);
   if (t.count == 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row = lane & 15, group = lane / 16;
+  const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   const T *const base = static_cast<const T *>(a.base);
   T *const out = static_cast<T *>(a.out);
-  const int64_t stride = (int64_t)a.tokens.T * a.rank, blocks = (a.width + kBlock - 1) / kBlock;
-  if (a.h_out && blockIdx.y == 0)
-    for (int i = threadIdx.x; i < t.count * a.rank; i += 256) {
-      const int64_t at = (int64_t)shared.token[i / a.rank] * a.rank + i % a.rank;
-      a.h_out[at] = t.adapter < 0 ? 0.0f : h_of(a.h + at, a.parts, stride);
-    }
   if (t.adapter < 0) {
-    if (base == out) return;
+    if (a.h && blockIdx.y == 0)
+      for (int i = threadIdx.x; i < t.count * a.rank; i += 256) a.h[(int64_t)shared.token[i / a.rank] * a.rank + i % a.rank] = 0.0f;
+    if (!out || base == out) return;
     for (int n = wave; n < t.count; n += 4)
       for (int64_t c = ((int64_t)blockIdx.y * 64 + lane) * 8; c < a.width; c += (int64_t)gridDim.y * 512) {
         float v[8] = {};
@@ -274,44 +295,78 @@ __global__ void __launch_bounds__(256) k_expand(ExpandArgs a) {
       }
     return;
   }
-  const int pieces = (a.rank + 7) / 8;
   const float scale = a.scales[t.adapter];
-  bf16x8 h[MT][NM];
-  int ranks[NM];                                 // the first rank of a lane's piece, -1: none
-#pragma unroll
-  for (int m = 0; m < NM; ++m) {
-    const int q = m * 4 + group, which = q / pieces, first = q % pieces * 8;
-    ranks[m] = which < TERMS ? first : -1;
-    for (int i = 0; i < MT; ++i) {
-      const int n = i * 16 + row < t.count ? i * 16 + row : t.count - 1;
-      const float *const from = a.h + (int64_t)shared.token[n] * a.rank + first;
-      for (int k = 0; k < 8; ++k)
-        h[i][m][k] = which < TERMS && first + k < a.rank ? term(scale * h_of(from + k, a.parts, stride), which) : (__bf16)0.0f;
+  for (int e = threadIdx.x; e < MT * 16 * kSpans * 4; e += 256) {
+    const int n = e / (kSpans * 4), piece = e % (kSpans * 4), first = piece * 8;
+    float v[8] = {};
+    if (n < t.count && first < a.rank) {
+      const float *const from = a.parts + (int64_t)shared.token[n] * a.h_pitch + first;
+      for (int p = 0; p < a.splits; ++p) {
+        const f32x4 *const q = reinterpret_cast<const f32x4 *>(from + (int64_t)p * a.tokens.T * a.h_pitch);
+        for (int k = 0; k < 8; ++k) v[k] += q[k / 4][k % 4];
+      }
+      if (a.h && blockIdx.y == 0)
+        for (int k = 0; k < 8; ++k)
+          if (first + k < a.rank) a.h[(int64_t)shared.token[n] * a.rank + first + k] = v[k];
+    }
+    for (int k = 0; k < 8; ++k) v[k] *= scale;
+    for (int which = 0; which < kTerms; ++which) {
+      bf16x8 q;
+      for (int k = 0; k < 8; ++k) q[k] = term(v[k], which);
+      split[n][which * kSpans * 4 + piece] = q;
+    }
+    if (a.terms && blockIdx.y == 0) {
+      if (n >= t.count)
+        for (int k = 0; k < 8; ++k) v[k] = 0.0f;                     // (0 times an infinite scale)
+      put_terms(a.terms, blockIdx.x, a.term_ranks, n, first, v);
     }
   }
+  if (!out) return;
+  __syncthreads();
+  const int pieces = (a.rank + 7) / 8;
+  bf16x8 h[MT][kSpans][kProducts];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+    for (int f = 0; f < kSpans; ++f)
+      for (int n = 0; n < kProducts; ++n) {
+        if (F) {
+          h[i][f][n] = split[i * 16 + row][n * kSpans * 4 + f * 4 + group];
+        } else {
+          const int q = n * 4 + group, which = q / pieces;
+          h[i][f][n] = which < kTerms ? split[i * 16 + row][which * 4 + q % pieces] : bf16x8{};
+        }
+      }
+  int64_t in[MT];                                // this lane's token of each 16; rows past the tile's are read again and not kept
+  for (int i = 0; i < MT; ++i) in[i] = shared.token[i * 16 + row < t.count ? i * 16 + row : t.count - 1];
   const __bf16 *const w = a.w + (int64_t)t.adapter * a.width * a.pitch;
+  const int64_t blocks = (a.width + kBlock - 1) / kBlock;
   for (int64_t b = (int64_t)blockIdx.y * 4 + wave; b < blocks; b += (int64_t)gridDim.y * 4) {
     const int64_t c0 = b * kBlock;
+    float v[MT][2][8] = {};
+    if (base)
+      for (int i = 0; i < MT; ++i)
+        for (int half = 0; half < 2; ++half) {
+          const int64_t c = c0 + group * 16 + half * 8;
+          load_columns(base + in[i] * a.ld_base + (c < a.width ? c : a.width - 8), v[i][half]);
+        }
     f32x4 acc[MT][4] = {};
-#pragma unroll
-    for (int m = 0; m < NM; ++m)
-      for (int p = 0; p < 4; ++p) {
-        const int64_t c = c0 + row / 4 * 16 + p * 4 + row % 4;
-        const bf16x8 ws = ranks[m] >= 0 && c < a.width ? load_ranks(w + c * a.pitch, ranks[m], a.rank, a.pitch) : bf16x8{};
-        for (int i = 0; i < MT; ++i) acc[i][p] = multiply(ws, h[i][m], acc[i][p]);
-      }
-    for (int i = 0; i < MT; ++i) {
-      if (i * 16 + row >= t.count) continue;
-      const int64_t n = shared.token[i * 16 + row];
-      for (int half = 0; half < 2; ++half) {
-        const int64_t c = c0 + group * 16 + half * 8;
-        if (c >= a.width) continue;
-        float v[8] = {};
-        if (base) load_columns(base + n * a.ld_base + c, v);
-        for (int k = 0; k < 8; ++k) v[k] += acc[i][half * 2 + k / 4][k % 4];
-        store_columns(out + n * a.ld_out + c, v);
+    for (int p = 0; p < 4; ++p) {
+      int64_t c = c0 + row / 4 * 16 + p * 4 + row % 4;
+      if (c >= a.width) c = a.width - 1;
+      for (int f = 0; f < kSpans; ++f) {
+        const int piece = F ? f * 4 + group : group % pieces;
+        const bf16x8 ws = piece < pieces ? load_ranks(w + c * a.pitch, piece * 8, a.rank, a.pitch) : bf16x8{};
+        for (int n = 0; n < kProducts; ++n)
+          for (int i = 0; i < MT; ++i) acc[i][p] = multiply(ws, h[i][f][n], acc[i][p]);
       }
     }
+    for (int i = 0; i < MT; ++i)
+      for (int half = 0; half < 2; ++half) {
+        const int64_t c = c0 + group * 16 + half * 8;
+        if (i * 16 + row >= t.count || c >= a.width) continue;
+        for (int k = 0; k < 8; ++k) v[i][half][k] += acc[i][half * 2 + k / 4][k % 4];
+        store_columns(out + in[i] * a.ld_out + c, v[i][half]);
+      }
   }
 }
 
@@ -328,11 +383,13 @@ struct PlanArgs {
   int32_t rank, pitch;
 };
 
+// Stable counting sort by one workgroup, each wave its own stretch of the tokens, 64 at a time.
 __device__ inline void plan_tokens(const PlanArgs &p) {
-  extern __shared__ int32_t counts[];            // [16][L + 1]: of each wave's tokens; then where its next token of an adapter goes
-  __shared__ int32_t waves[2][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  extern __shared__ int32_t counts[];            // [16][groups]: each wave's tokens of a group, then how many come before them
   const int32_t groups = p.L + 1;
+  int32_t *const tile_begin = counts + 16 * groups, *const members = tile_begin + groups + 1;
+  __shared__ int32_t waves[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   for (int32_t i = threadIdx.x; i < 16 * groups; i += kPlanThreads) counts[i] = 0;
   __syncthreads();
   int32_t *const mine = counts + wave * groups;
@@ -347,61 +404,72 @@ __device__ inline void plan_tokens(const PlanArgs &p) {
     }
     return m;
   };
+  constexpr int kAhead = 16;                     // loads on their way
   for (int pass = 0; pass < 2; ++pass) {
-    for (int32_t t0 = begin; t0 < end; t0 += 64) {
-      const int32_t t = t0 + lane;
-      int32_t l = t < end ? adapter_of(p.which, t, p.L) : groups;       // (past the end: a group of its own, not counted)
-      if (l < 0) l = p.L;
-      const uint64_t m = alike(l);
-      const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1)), at = t < end ? mine[l] : 0;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // (all lanes have read before one writes, and the other way)
-      if (pass == 1 && t < end) p.plan.order[at + before] = t;
-      if (before == 0 && t < end) mine[l] = at + __popcll(m);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
-    if (pass == 1) break;
-    __syncthreads();
-    // tokens and tiles of every group, summed up over the groups before it: each thread its adjacent groups
-    const int32_t per = (groups + kPlanThreads - 1) / kPlanThreads, g0 = threadIdx.x * per;
-    int32_t n[2] = {0, 0};
-    for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
-      int32_t c = 0;
-      for (int w = 0; w < 16; ++w) c += counts[w * groups + g];
-      n[0] += c;
-      n[1] += (c + kTile - 1) / kTile;
-    }
-    int32_t upto[2] = {n[0], n[1]};
-    for (int d = 1; d < 64; d <<= 1)
-      for (int k = 0; k < 2; ++k) {
-        const int32_t other = __shfl_up(upto[k], d);
-        if (lane >= d) upto[k] += other;
+    for (int32_t t0 = begin; t0 < end; t0 += 64 * kAhead) {
+      int32_t group[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int32_t t = t0 + i * 64 + lane;
+        group[i] = t < end ? p.which[t] : 0;
       }
-    if (lane == 63)
-      for (int k = 0; k < 2; ++k) waves[k][wave] = upto[k];
-    __syncthreads();
-    int32_t at[2];
-    for (int k = 0; k < 2; ++k) {
-      at[k] = upto[k] - n[k];
-      for (int w = 0; w < wave; ++w) at[k] += waves[k][w];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int32_t t = t0 + i * 64 + lane;
+        if (t0 + i * 64 >= end) break;
+        // (past the end: a group of its own, not counted)
+        const int32_t l = t >= end ? groups : group[i] >= 0 && group[i] < p.L ? group[i] : p.L;
+        const uint64_t m = alike(l);
+        const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1)), at = t < end ? mine[l] : 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");        // (all lanes have read before one writes, and the other way)
+        if (pass == 1 && t < end) p.plan.order[(int64_t)tile_begin[l] * kTile + at + before] = t;
+        if (before == 0 && t < end) mine[l] = at + __popcll(m);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
     }
+    __syncthreads();
+    if (pass == 1) break;
+    // the waves' tokens of a group one after the other, the groups' tiles one after the other: each thread its adjacent groups
+    const int32_t per = (groups + kPlanThreads - 1) / kPlanThreads, g0 = threadIdx.x * per;
+    int32_t tiles = 0;
     for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
-      int32_t c = 0;
+      int32_t n = 0;
       for (int w = 0; w < 16; ++w) {
         const int32_t of = counts[w * groups + g];
-        counts[w * groups + g] = at[0] + c;
-        c += of;
+        counts[w * groups + g] = n;
+        n += of;
       }
-      p.plan.tile_begin[g] = at[1];
-      for (int32_t i = 0; i * kTile < c; ++i)
-        p.plan.tiles[at[1] + i] = {at[0] + i * kTile, c - i * kTile < kTile ? c - i * kTile : kTile, g < p.L ? g : -1, 0};
-      at[0] += c;
-      at[1] += (c + kTile - 1) / kTile;
-      if (g == groups - 1) {
-        p.plan.tile_begin[groups] = at[1];
-        *p.plan.count = at[1];
-      }
+      members[g] = n;
+      tiles += (n + kTile - 1) / kTile;
+    }
+    int32_t upto = tiles;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int32_t other = __shfl_up(upto, d);
+      if (lane >= d) upto += other;
+    }
+    if (lane == 63) waves[wave] = upto;
+    __syncthreads();
+    int32_t at = upto - tiles;
+    for (int w = 0; w < wave; ++w) at += waves[w];
+    for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
+      tile_begin[g] = at;
+      at += (members[g] + kTile - 1) / kTile;
+      if (g == groups - 1) tile_begin[groups] = at;
     }
     __syncthreads();
+    for (int32_t g = threadIdx.x; g <= groups; g += kPlanThreads) p.plan.tile_begin[g] = tile_begin[g];
+    if (threadIdx.x == 0) *p.plan.count = tile_begin[groups];
+    for (int32_t i = threadIdx.x; i < tile_begin[groups]; i += kPlanThreads) {
+      int32_t lo = 0, hi = groups - 1;           // the last group that begins at tile i or before (those without tiles begin there too)
+      while (lo < hi) {
+        const int32_t mid = (lo + hi + 1) / 2;
+        if (tile_begin[mid] <= i) lo = mid;
+        else hi = mid - 1;
+      }
+      const int32_t left = members[lo] - (i - tile_begin[lo]) * kTile;
+      p.plan.tiles[i] = {lo < p.L ? lo : -1, left < kTile ? left : kTile};
+      for (int32_t n = left; n < kTile; ++n) p.plan.order[(int64_t)i * kTile + n] = -1;
+    }
   }
 }
 
@@ -446,17 +514,16 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs p) {
 
 struct OuterHalf {
   const __bf16 *x;             // [T] rows of `width`
-  const float *h;              // [parts][T][rank]
+  const __bf16 *terms;         // [tiles][3][term_ranks][32]: of s h (put_terms)
   float *out;                  // [L][rank][width], or with `by_rank` [L][width][rank]
   float *parted;               // [2 ranges] of the same
   int64_t ld, width;
-  int32_t parts, chunks;
+  int32_t chunks;
   bool by_rank;
 };
 struct OuterArgs {
   Plan plan;
-  const float *scales;
-  int32_t T, L, rank, tiles;   // tiles of a range
+  int32_t rank, term_ranks, tiles;   // tiles of a range
   OuterHalf half[2];
 };
 
@@ -474,11 +541,11 @@ __global__ void __launch_bounds__(256) k_outer(OuterArgs a) {
   const bool second = (int32_t)blockIdx.x >= a.half[0].chunks;
   const OuterHalf f = second ? a.half[1] : a.half[0];
   const int32_t chunk = (int32_t)blockIdx.x - (second ? a.half[0].chunks : 0), range = blockIdx.y, rank0 = blockIdx.z * RT * 16;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row = lane & 15, group = lane / 16;
+  const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   const int64_t c0 = (int64_t)chunk * kOuterWidth + wave * 128, c = c0 + row * 8;
   if (c0 >= f.width) return;
   const bool in = c < f.width;
-  const int64_t stride = (int64_t)a.T * a.rank, size = f.width * a.rank;
+  const int64_t size = f.width * a.rank;
   const int32_t count = *a.plan.count, first = range * a.tiles, last = first + a.tiles < count ? first + a.tiles : count;
   f32x4 acc[RT][8] = {};
   int32_t adapter = -1;
@@ -503,36 +570,43 @@ __global__ void __launch_bounds__(256) k_outer(OuterArgs a) {
     for (int r = 0; r < RT; ++r)
       for (int j = 0; j < 8; ++j) acc[r][j] = f32x4{};
   };
+  // tile i's columns and terms are on their way while tile i - 1 is multiplied, its tokens' numbers one tile earlier still
+  int32_t token[8];
+  u32x4 x[8];
+  bf16x8 hs[RT][3];
+  const auto fetch_tokens = [&](int32_t i) {
+    if (i >= last) return;
+    for (int q = 0; q < 8; ++q) token[q] = a.plan.order[(int64_t)i * kTile + group * 8 + q];
+  };
+  const auto fetch = [&](int32_t i) {
+    if (i >= last) return;
+    for (int q = 0; q < 8; ++q)
+      x[q] = in && token[q] >= 0 ? *reinterpret_cast<const u32x4 *>(f.x + token[q] * f.ld + c) : u32x4{};
+    for (int r = 0; r < RT; ++r)
+      for (int which = 0; which < 3; ++which)
+        hs[r][which] = load8(f.terms + ((i * (int64_t)3 + which) * a.term_ranks + rank0 + r * 16 + row) * kTile + group * 8);
+  };
+  fetch_tokens(first);
+  fetch(first);
+  fetch_tokens(first + 1);
   for (int32_t i = first; i < last; ++i) {
-    const Tile t = a.plan.tiles[i];
-    if (t.adapter < 0) break;                    // (they come last)
-    if (t.adapter != adapter) flush();
-    adapter = t.adapter;
-    const float scale = a.scales[adapter];
-    int64_t token[8];
-    u32x4 x[8];
-    for (int q = 0; q < 8; ++q) {
-      const int n = group * 8 + q;
-      token[q] = a.plan.order[t.start + (n < t.count ? n : 0)];
-      x[q] = in && n < t.count ? *reinterpret_cast<const u32x4 *>(f.x + token[q] * f.ld + c) : u32x4{};
-    }
-    bf16x8 xt[8];
+    const int32_t l = a.plan.tiles[i].adapter;
+    if (l < 0) break;                            // (they come last)
+    if (l != adapter) flush();
+    adapter = l;
+    bf16x8 xt[8], now[RT][3];
     for (int j = 0; j < 8; ++j) {
       u32x4 p;
       for (int q = 0; q < 4; ++q) p[q] = __builtin_amdgcn_perm(x[2 * q + 1][j / 2], x[2 * q][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
       xt[j] = __builtin_bit_cast(bf16x8, p);
     }
-    for (int r = 0; r < RT; ++r) {
-      const int rank = rank0 + r * 16 + row;
-      float v[8];
-      for (int q = 0; q < 8; ++q)
-        v[q] = rank < a.rank && group * 8 + q < t.count ? scale * h_of(f.h + token[q] * a.rank + rank, f.parts, stride) : 0.0f;
-      for (int which = 0; which < 3; ++which) {
-        bf16x8 hs;
-        for (int q = 0; q < 8; ++q) hs[q] = term(v[q], which);
-        for (int j = 0; j < 8; ++j) acc[r][j] = multiply(xt[j], hs, acc[r][j]);
-      }
-    }
+    for (int r = 0; r < RT; ++r)
+      for (int which = 0; which < 3; ++which) now[r][which] = hs[r][which];
+    fetch(i + 1);
+    fetch_tokens(i + 2);
+    for (int r = 0; r < RT; ++r)
+      for (int which = 0; which < 3; ++which)
+        for (int j = 0; j < 8; ++j) acc[r][j] = multiply(xt[j], now[r][which], acc[r][j]);
   }
   flush();
 }
@@ -577,7 +651,7 @@ struct Layout {
   int64_t tiles;               // at most so many planned tiles
   int64_t splits_in, splits_out;     // of the sum over inp (h), over out (dh)
   int64_t ranges, range_tiles; // of k_outer
-  int64_t count, tile_begin, order, table, h, at, bt, parted_a, parted_b, bytes;   // byte offsets
+  int64_t count, tile_begin, order, table, parts, at, bt, terms_a, terms_b, parted_a, parted_b, bytes;   // byte offsets
 
   // Splits of a sum so that there are workgroups for the compute units, each with two steps a wave at least
   static int64_t splits(int64_t tokens, bool few, int64_t width) {
@@ -605,22 +679,25 @@ struct Layout {
     count = take(4);
     if (!few) {
       tile_begin = take((p.adapters + 2) * 4);
-      order = take(p.tokens * 4);
+      order = take(tiles * kTile * 4);
       table = take(tiles * (int64_t)sizeof(Tile));
     }
-    h = take((backward ? splits_out : splits_in) * p.tokens * p.rank * 4);
+    parts = take((backward ? splits_out : splits_in) * p.tokens * pitch(p) * 4);
     if (backward) {
       at = take(p.adapters * p.inp * pitch(p) * 2);
       bt = take(p.adapters * p.out * p.rank * 2);
+      terms_a = take(tiles * 3 * term_ranks(p) * kTile * 2);
+      terms_b = take(tiles * 3 * term_ranks(p) * kTile * 2);
       parted_a = take(2 * ranges * p.rank * p.inp * 4);
       parted_b = take(2 * ranges * p.rank * p.out * 4);
     }
     bytes = end;
   }
   static int64_t pitch(const nvfp4_adapters_params &p) { return divide_up(p.rank, 8) * 8; }
+  static int64_t term_ranks(const nvfp4_adapters_params &p) { return p.rank <= 16 ? 16 : p.rank <= 32 ? 32 : p.rank <= 64 ? 64 : 128; }
   Plan plan(char *w) const {
-    return {reinterpret_cast<int32_t *>(w + count), reinterpret_cast<int32_t *>(w + tile_begin), reinterpret_cast<int32_t *>(w + order),
-            reinterpret_cast<Tile *>(w + table)};
+    return {reinterpret_cast<int32_t *>(w + count), reinterpret_cast<int32_t *>(w + tile_begin), reinterpret_cast<Tile *>(w + table),
+            reinterpret_cast<int32_t *>(w + order)};
   }
 };
 
@@ -629,52 +706,45 @@ int run_plan(const nvfp4_adapters_params &p, const Layout &d, char *w, const int
   PlanArgs g{which, d.plan(w), (int32_t)p.tokens, (int32_t)p.adapters, static_cast<const __bf16 *>(a), static_cast<const __bf16 *>(b),
              reinterpret_cast<__bf16 *>(w + d.at), reinterpret_cast<__bf16 *>(w + d.bt), p.inp, p.out,
              a ? p.adapters * (divide_up(p.inp, 64) + divide_up(p.out, 64)) : 0, (int32_t)p.rank, (int32_t)Layout::pitch(p)};
-  const size_t counts = 16 * (size_t)(p.adapters + 1) * 4, tile = a ? 64 * (size_t)(p.rank + 2) * 2 : 0;
-  constexpr size_t kMostLds = 16 * (kMostAdapters + 1) * 4;
+  const size_t counts = (18 * (size_t)(p.adapters + 1) + 1) * 4, tile = a ? 64 * (size_t)(p.rank + 2) * 2 : 0;
+  constexpr size_t kMostLds = (18 * (kMostAdapters + 1) + 1) * 4;
   if (counts > 48 * 1024 &&
       hipFuncSetAttribute(reinterpret_cast<const void *>(k_plan), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds) != hipSuccess)
     return NVFP4_ERR_HIP;
   return launch(k_plan, dim3((uint32_t)(1 + (g.units < 65536 ? g.units : 65536))), dim3(kPlanThreads), counts > tile ? counts : tile, s, g);
 }
 
-template <int MT, int RT, int W>
+template <int MT, int RT, int W, int D>
 int run_shrink_of(const ShrinkArgs &g, int64_t tiles, int64_t splits, hipStream_t s) {
-  return launch(k_shrink<MT, RT, W>, dim3((uint32_t)tiles, (uint32_t)splits), dim3(W * 64), 0, s, g);
+  return launch(k_shrink<MT, RT, W, D>, dim3((uint32_t)tiles, (uint32_t)splits), dim3(W * 64), 0, s, g);
 }
 int run_shrink(ShrinkArgs g, const Layout &d, int64_t splits, hipStream_t s) {
   g.steps = (int32_t)divide_up(divide_up(g.width, kBlock), splits);
   const int64_t tiles = d.few ? g.tokens.T : d.tiles;
   if (d.few) {
-    if (g.rank <= 16) return run_shrink_of<1, 1, 8>(g, tiles, splits, s);
-    if (g.rank <= 32) return run_shrink_of<1, 2, 8>(g, tiles, splits, s);
-    if (g.rank <= 64) return run_shrink_of<1, 4, 8>(g, tiles, splits, s);
-    return run_shrink_of<1, 8, 4>(g, tiles, splits, s);
+    if (g.rank <= 16) return run_shrink_of<1, 1, 8, 4>(g, tiles, splits, s);
+    if (g.rank <= 32) return run_shrink_of<1, 2, 8, 3>(g, tiles, splits, s);
+    if (g.rank <= 64) return run_shrink_of<1, 4, 8, 2>(g, tiles, splits, s);
+    return run_shrink_of<1, 8, 4, 2>(g, tiles, splits, s);
   }
-  if (g.rank <= 16) return run_shrink_of<2, 1, 8>(g, tiles, splits, s);
-  if (g.rank <= 32) return run_shrink_of<2, 2, 8>(g, tiles, splits, s);
-  if (g.rank <= 64) return run_shrink_of<2, 4, 4>(g, tiles, splits, s);
-  return run_shrink_of<2, 8, 4>(g, tiles, splits, s);
+  if (g.rank <= 16) return run_shrink_of<2, 1, 8, 4>(g, tiles, splits, s);
+  if (g.rank <= 32) return run_shrink_of<2, 2, 8, 3>(g, tiles, splits, s);
+  if (g.rank <= 64) return run_shrink_of<2, 4, 4, 2>(g, tiles, splits, s);
+  return run_shrink_of<2, 8, 4, 2>(g, tiles, splits, s);
 }
 
-template <typename T, int TERMS, int NM>
+template <typename T, int F>
 int run_expand_of(const ExpandArgs &g, const Layout &d, hipStream_t s) {
-  const int64_t blocks = divide_up(g.width, kBlock * 4), tiles = d.few ? g.tokens.T : d.tiles;
-  const int64_t want = divide_up(2048, tiles);
+  const int64_t blocks = divide_up(g.width, kBlock * 4), tiles = d.few ? g.tokens.T : d.tiles, want = g.out ? divide_up(2048, tiles) : 1;
   const dim3 grid((uint32_t)tiles, (uint32_t)(want < blocks ? want : blocks));
-  return d.few ? launch(k_expand<T, 1, TERMS, NM>, grid, dim3(256), 0, s, g) : launch(k_expand<T, 2, TERMS, NM>, grid, dim3(256), 0, s, g);
+  return d.few ? launch(k_expand<T, 1, F>, grid, dim3(256), 0, s, g) : launch(k_expand<T, 2, F>, grid, dim3(256), 0, s, g);
 }
-int run_expand(const ExpandArgs &g, const Layout &d, bool f32, hipStream_t s) {
-  const int64_t products = divide_up((f32 ? 3 : 2) * divide_up(g.rank, 8), 4);
-  if (f32) {
-    if (products <= 2) return run_expand_of<float, 3, 2>(g, d, s);
-    if (products <= 3) return run_expand_of<float, 3, 3>(g, d, s);
-    if (products <= 6) return run_expand_of<float, 3, 6>(g, d, s);
-    return run_expand_of<float, 3, 12>(g, d, s);
-  }
-  if (products <= 1) return run_expand_of<__bf16, 2, 1>(g, d, s);
-  if (products <= 2) return run_expand_of<__bf16, 2, 2>(g, d, s);
-  if (products <= 4) return run_expand_of<__bf16, 2, 4>(g, d, s);
-  return run_expand_of<__bf16, 2, 8>(g, d, s);
+template <typename T>
+int run_expand(const ExpandArgs &g, const Layout &d, hipStream_t s) {
+  if (g.rank <= 16) return run_expand_of<T, 0>(g, d, s);
+  if (g.rank <= 32) return run_expand_of<T, 1>(g, d, s);
+  if (g.rank <= 64) return run_expand_of<T, 2>(g, d, s);
+  return run_expand_of<T, 4>(g, d, s);
 }
 
 }  // namespace
@@ -705,13 +775,22 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
   if (!d.few)
     if (const int rc = run_plan(*p, d, w, which, nullptr, nullptr, s)) return rc;
   const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters, d.few};
-  const bool direct = h && d.splits_in == 1;                 // k_shrink's one part is h itself
-  float *const parts = direct ? h : reinterpret_cast<float *>(w + d.h);
-  if (const int rc = run_shrink({tokens, static_cast<const __bf16 *>(x), static_cast<const __bf16 *>(a), parts, p->ld_x, p->inp,
-                                 (int32_t)p->rank, 0, direct}, d, d.splits_in, s))
-    return rc;
-  return run_expand({tokens, parts, direct ? nullptr : h, static_cast<const __bf16 *>(b), scales, base, out, p->ld_base, p->ld_out,
-                     p->out, (int32_t)p->rank, (int32_t)p->rank, (int32_t)d.splits_in}, d, p->out_dtype == NVFP4_OUT_F32, s);
+  float *const parts = reinterpret_cast<float *>(w + d.parts);
+  const int32_t rank = (int32_t)p->rank, pitch = (int32_t)Layout::pitch(*p);
+  ShrinkArgs g{};
+  g.tokens = tokens;
+  g.x = static_cast<const __bf16 *>(x);
+  g.w = static_cast<const __bf16 *>(a);
+  g.parts = parts;
+  g.h = d.splits_in == 1 ? h : nullptr;
+  g.ld = p->ld_x;
+  g.width = p->inp;
+  g.rank = rank;
+  g.pitch = pitch;
+  if (const int rc = run_shrink(g, d, d.splits_in, s)) return rc;
+  const ExpandArgs e{tokens, parts, d.splits_in == 1 ? nullptr : h, nullptr, static_cast<const __bf16 *>(b), scales, base, out,
+                     p->ld_base, p->ld_out, p->out, rank, rank, pitch, (int32_t)d.splits_in, 0};
+  return p->out_dtype == NVFP4_OUT_F32 ? run_expand<float>(e, d, s) : run_expand<__bf16>(e, d, s);
 }
 
 extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_params *p, const void *x, const float *h, const void *a,
@@ -733,24 +812,23 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
   const bool any = p->tokens != 0;
   if (const int rc = run_plan(*p, d, w, which, any ? a : nullptr, b, s)) return rc;
   const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters, false};
-  float *const parts = reinterpret_cast<float *>(w + d.h);
-  const int32_t rank = (int32_t)p->rank;
-  OuterArgs g{d.plan(w), scales, (int32_t)p->tokens, (int32_t)p->adapters, rank, (int32_t)d.range_tiles,
-              {{static_cast<const __bf16 *>(x), parts, da, reinterpret_cast<float *>(w + d.parted_a), p->ld_x, p->inp,
-                (int32_t)d.splits_out, (int32_t)divide_up(p->inp, kOuterWidth), false},
-               {static_cast<const __bf16 *>(dy), h, db, reinterpret_cast<float *>(w + d.parted_b), p->ld_dy, p->out, 1,
-                (int32_t)divide_up(p->out, kOuterWidth), true}}};
+  float *const parts = reinterpret_cast<float *>(w + d.parts);
+  __bf16 *const terms_a = reinterpret_cast<__bf16 *>(w + d.terms_a), *const terms_b = reinterpret_cast<__bf16 *>(w + d.terms_b);
+  const int32_t rank = (int32_t)p->rank, pitch = (int32_t)Layout::pitch(*p), term_ranks = (int32_t)Layout::term_ranks(*p);
+  const OuterArgs g{d.plan(w), rank, term_ranks, (int32_t)d.range_tiles,
+                    {{static_cast<const __bf16 *>(x), terms_a, da, reinterpret_cast<float *>(w + d.parted_a), p->ld_x, p->inp,
+                      (int32_t)divide_up(p->inp, kOuterWidth), false},
+                     {static_cast<const __bf16 *>(dy), terms_b, db, reinterpret_cast<float *>(w + d.parted_b), p->ld_dy, p->out,
+                      (int32_t)divide_up(p->out, kOuterWidth), true}}};
   if (any) {
-    if (const int rc = run_shrink({tokens, static_cast<const __bf16 *>(dy), reinterpret_cast<const __bf16 *>(w + d.bt), parts, p->ld_dy,
-                                   p->out, rank, 0, false}, d, d.splits_out, s))
-      return rc;
-    if (dx)
-      if (const int rc = run_expand({tokens, parts, nullptr, reinterpret_cast<const __bf16 *>(w + d.at), scales, dx_base, dx,
-                                     p->ld_base, p->ld_out, p->inp, rank, (int32_t)Layout::pitch(*p), (int32_t)d.splits_out}, d, false, s))
-        return rc;
+    const ShrinkArgs dh{tokens, static_cast<const __bf16 *>(dy), reinterpret_cast<const __bf16 *>(w + d.bt), parts, nullptr, h, scales,
+                        terms_b, p->ld_dy, p->out, rank, pitch, 0, term_ranks};
+    if (const int rc = run_shrink(dh, d, d.splits_out, s)) return rc;
+    const ExpandArgs e{tokens, parts, nullptr, terms_a, reinterpret_cast<const __bf16 *>(w + d.at), scales, dx_base, dx,
+                       p->ld_base, p->ld_out, p->inp, rank, pitch, pitch, (int32_t)d.splits_out, term_ranks};
+    if (const int rc = run_expand<__bf16>(e, d, s)) return rc;
     const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, rank <= 64 ? 1 : 2);
-    if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g))
-      return rc;
+    if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
   }
   const int64_t most = divide_up(p->rank * (p->inp > p->out ? p->inp : p->out), 1024);
   return launch(k_join, dim3((uint32_t)(most < 256 ? most : 256), (uint32_t)p->adapters), dim3(256), 0, s, g);
