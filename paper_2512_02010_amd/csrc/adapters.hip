@@ -50,7 +50,6 @@ struct Tokens {
   const int32_t *which;
   Plan plan;
   int32_t T, L;
-  bool few;
 };
 
 __device__ inline int32_t adapter_of(const int32_t *which, int32_t t, int32_t L) {
@@ -68,10 +67,10 @@ struct TileTokens {
 // The tile of `index` in `shared`, as (count, adapter); count 0: there is none.  All threads of the workgroup call it.  With a plan
 // the index is that of a tile (rows == 16: of half a tile).  Without, it is a token's: the token leads a tile if a multiple of 16 of
 // the tokens before it have its adapter, and the next of them go with it.
-template <int NT>
+template <bool FEW, int NT>
 __device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t index, int rows) {
   Tile t{-1, 0};
-  if (!k.few) {
+  if constexpr (!FEW) {
     const int halves = kTile / rows;
     if (index / halves >= *k.plan.count) return t;
     t = k.plan.tiles[index / halves];
@@ -149,14 +148,14 @@ struct ShrinkArgs {
   int32_t term_ranks;
 };
 
-// D[token][rank]: rows of x against rows of w, both adjacent in the summed index.  A lane takes 16 columns of a step, of row
-// lane % 16 of each side: 128 bytes of a row lie in one step.  The waves of a workgroup take every W-th step of its split, D of them
+// D[token][rank]: rows of x against rows of w, both adjacent in the summed index.  A lane takes twice 8 columns of a step, of row
+// lane % 16 of each side: a load has 64 adjacent bytes of 16 rows, a step 128.  The waves of a workgroup take every W-th step of its split, D of them
 // on their way at a time.
-template <int MT, int RT, int W, int D>
+template <bool FEW, int MT, int RT, int W, int D>
 __global__ void __launch_bounds__(W * 64) k_shrink(ShrinkArgs a) {
   __shared__ TileTokens shared;
   __shared__ float part[W][MT * RT * 256];
-  const Tile t = find_tile<W * 64>(a.tokens, shared, blockIdx.x, MT * 16);
+  const Tile t = find_tile<FEW, W * 64>(a.tokens, shared, blockIdx.x, MT * 16);
   if (t.count == 0) return;
   if (t.adapter < 0) {
     if (a.h)
@@ -167,36 +166,52 @@ __global__ void __launch_bounds__(W * 64) k_shrink(ShrinkArgs a) {
   const __bf16 *x[MT], *w[RT];
   for (int i = 0; i < MT; ++i) {
     const int n = i * 16 + row < t.count ? i * 16 + row : t.count - 1;            // (rows past the tile's are not kept)
-    x[i] = a.x + shared.token[n] * a.ld + group * 16;
+    x[i] = a.x + shared.token[n] * a.ld + group * 8;
   }
   for (int i = 0; i < RT; ++i) {
     const int n = i * 16 + row < a.rank ? i * 16 + row : a.rank - 1;
-    w[i] = a.w + ((int64_t)t.adapter * a.rank + n) * a.width + group * 16;
+    w[i] = a.w + ((int64_t)t.adapter * a.rank + n) * a.width + group * 8;
   }
   f32x4 acc[MT][RT] = {};
   bf16x8 xs[D][MT][2], ws[D][RT][2];
-  const int32_t all = (int32_t)((a.width + kBlock - 1) / kBlock), first = (int32_t)blockIdx.y * a.steps + wave;
-  const int32_t last = ((int32_t)blockIdx.y + 1) * a.steps < all ? ((int32_t)blockIdx.y + 1) * a.steps : all;
-  const auto fetch = [&](int d, int32_t s) {
-    if (s >= last) return;
-    const int64_t k = (int64_t)s * kBlock;
+  const int32_t whole = (int32_t)(a.width / kBlock), first = (int32_t)blockIdx.y * a.steps, end = first + a.steps;
+  // this wave's steps: first + wave + i W, i < n
+  const int32_t n = ((end < whole ? end : whole) - first - wave + W - 1) / W;
+  const auto fetch = [&](int d, int32_t i) {
+    const int64_t k = (int64_t)(first + wave + (i < n ? i : n - 1) * W) * kBlock;        // (past the end: once more what it had)
     for (int c = 0; c < 2; ++c) {
-      const bool in = k + kBlock <= a.width || k + group * 16 + c * 8 < a.width;
-      for (int i = 0; i < MT; ++i) xs[d][i][c] = in ? load8(x[i] + k + c * 8) : bf16x8{};
-      for (int i = 0; i < RT; ++i) ws[d][i][c] = in ? load8(w[i] + k + c * 8) : bf16x8{};
+      for (int m = 0; m < MT; ++m) xs[d][m][c] = load8(x[m] + k + c * 32);
+      for (int r = 0; r < RT; ++r) ws[d][r][c] = load8(w[r] + k + c * 32);
     }
   };
+  const auto product = [&](int d) {
+    for (int c = 0; c < 2; ++c)
+      for (int m = 0; m < MT; ++m)
+        for (int r = 0; r < RT; ++r) acc[m][r] = multiply(xs[d][m][c], ws[d][r][c], acc[m][r]);
+  };
+  if (n > 0) {
 #pragma unroll
-  for (int d = 0; d < D - 1; ++d) fetch(d, first + d * W);
-  for (int32_t s = first; s < last; s += D * W)
+    for (int d = 0; d < D - 1; ++d) fetch(d, d);
+    int32_t i = 0;
+    for (; i + D <= n; i += D)
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      fetch((d + D - 1) % D, s + (d + D - 1) * W);
-      if (s + d * W < last)
-        for (int c = 0; c < 2; ++c)
-          for (int i = 0; i < MT; ++i)
-            for (int j = 0; j < RT; ++j) acc[i][j] = multiply(xs[d][i][c], ws[d][j][c], acc[i][j]);
+      for (int d = 0; d < D; ++d) {
+        fetch((d + D - 1) % D, i + d + D - 1);
+        product(d);
+      }
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d)
+      if (i + d < n) product(d);
+  }
+  if (a.width % kBlock && whole >= first && whole < end && whole % W == wave) {        // the last columns, fewer than a step's
+    for (int c = 0; c < 2; ++c) {
+      const int64_t k = (int64_t)whole * kBlock + c * 32;
+      const bool in = k + group * 8 < a.width;
+      for (int m = 0; m < MT; ++m) xs[0][m][c] = in ? load8(x[m] + k) : bf16x8{};
+      for (int r = 0; r < RT; ++r) ws[0][r][c] = in ? load8(w[r] + k) : bf16x8{};
     }
+    product(0);
+  }
   for (int i = 0; i < MT; ++i)
     for (int j = 0; j < RT; ++j)
       for (int v = 0; v < 4; ++v) part[wave][(i * RT + j) * 256 + (group * 4 + v) * 16 + row] = acc[i][j][v];
@@ -211,14 +226,19 @@ __global__ void __launch_bounds__(W * 64) k_shrink(ShrinkArgs a) {
       if (a.h && rank < a.rank) a.h[(int64_t)shared.token[n] * a.rank + rank] = s;
     }
   }
-  if (a.terms_of && blockIdx.y == 0)
+  constexpr int kParts = kTile / (MT * 16);      // workgroups of a planned tile: the first sees to the terms of all of it
+  if (a.terms_of && blockIdx.y == 0 && blockIdx.x % kParts == 0) {
+    const int64_t tile = blockIdx.x / kParts;
+    const float scale = a.scales[t.adapter];
     for (int e = threadIdx.x; e < kTile * a.term_ranks / 8; e += W * 64) {
-      const int n = e % kTile, from = e / kTile * 8;
+      const int n = e % kTile, from = e / kTile * 8, token = a.tokens.plan.order[tile * kTile + n];
+      const float *const h = a.terms_of + (int64_t)(token < 0 ? 0 : token) * a.rank;
       float v[8];
-      for (int k = 0; k < 8; ++k)
-        v[k] = n < t.count && from + k < a.rank ? a.scales[t.adapter] * a.terms_of[(int64_t)shared.token[n] * a.rank + from + k] : 0.0f;
-      put_terms(a.terms, blockIdx.x, a.term_ranks, n, from, v);
+      for (int k = 0; k < 8; ++k) v[k] = h[from + k < a.rank ? from + k : a.rank - 1];
+      for (int k = 0; k < 8; ++k) v[k] = token >= 0 && from + k < a.rank ? scale * v[k] : 0.0f;
+      put_terms(a.terms, tile, a.term_ranks, n, from, v);
     }
+  }
 }
 
 // ---- k_expand ---------------------------------------------------------------------------------------------------------
@@ -236,9 +256,10 @@ struct ExpandArgs {
   int32_t rank, pitch, h_pitch, splits, term_ranks;
 };
 
-// Eight ranks of a row of w; where rows are not whole pieces of 16 bytes, one by one.
-__device__ inline bf16x8 load_ranks(const __bf16 *row, int first, int rank, int pitch) {
-  if (pitch % 8 == 0) return load8(row + first);
+// Eight ranks of a row of w, from `first`; where rows are not WHOLE pieces of 16 bytes, one by one.
+template <bool WHOLE>
+__device__ inline bf16x8 load_ranks(const __bf16 *row, int first, int rank) {
+  if constexpr (WHOLE) return load8(row + first);
   bf16x8 v{};
   for (int i = 0; i < 8; ++i)
     if (first + i < rank) v[i] = row[first + i];
@@ -270,15 +291,15 @@ __device__ inline void store_columns(T *p, const float *v) {
 }
 
 // D[column][token]: rows of w against s h, which enters as terms (term).  Row 4 a + b of product p of a block is column
-// 16 a + 4 p + b, so that a lane ends up with 16 adjacent columns of its token.  The summed index of a product is four pieces of
+// 32 (p / 2) + 8 a + 4 (p % 2) + b, so that a lane ends up with twice 8 adjacent columns of its token, 64 bytes in four lanes.  The summed index of a product is four pieces of
 // eight ranks: F > 0: 32 ranks of one term, F times.  F == 0, rank <= 16: the one or two pieces of every term side by side.
 // The workgroup sums the parts of h and splits them once, into LDS.
-template <typename T, int MT, int F>
+template <bool FEW, bool WHOLE, typename T, int MT, int F>
 __global__ void __launch_bounds__(256) k_expand(ExpandArgs a) {
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 2, kSpans = F ? F : 1, kProducts = F ? kTerms : kTerms - 1;
   __shared__ TileTokens shared;
   __shared__ bf16x8 split[MT * 16][kTerms * kSpans * 4 + 1];        // (an odd number of pieces: a row a bank further)
-  const Tile t = find_tile<256>(a.tokens, shared, blockIdx.x, MT * 16);
+  const Tile t = find_tile<FEW, 256>(a.tokens, shared, blockIdx.x, MT * 16);
   if (t.count == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   const T *const base = static_cast<const T *>(a.base);
@@ -346,23 +367,24 @@ __global__ void __launch_bounds__(256) k_expand(ExpandArgs a) {
     if (base)
       for (int i = 0; i < MT; ++i)
         for (int half = 0; half < 2; ++half) {
-          const int64_t c = c0 + group * 16 + half * 8;
+          const int64_t c = c0 + half * 32 + group * 8;
           load_columns(base + in[i] * a.ld_base + (c < a.width ? c : a.width - 8), v[i][half]);
         }
     f32x4 acc[MT][4] = {};
     for (int p = 0; p < 4; ++p) {
-      int64_t c = c0 + row / 4 * 16 + p * 4 + row % 4;
+      int64_t c = c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4;
       if (c >= a.width) c = a.width - 1;
       for (int f = 0; f < kSpans; ++f) {
         const int piece = F ? f * 4 + group : group % pieces;
-        const bf16x8 ws = piece < pieces ? load_ranks(w + c * a.pitch, piece * 8, a.rank, a.pitch) : bf16x8{};
+        bf16x8 ws = load_ranks<WHOLE>(w + c * a.pitch, piece < pieces ? piece * 8 : 0, a.rank);
+        if (F && pieces % 4 && piece >= pieces) ws = bf16x8{};
         for (int n = 0; n < kProducts; ++n)
           for (int i = 0; i < MT; ++i) acc[i][p] = multiply(ws, h[i][f][n], acc[i][p]);
       }
     }
     for (int i = 0; i < MT; ++i)
       for (int half = 0; half < 2; ++half) {
-        const int64_t c = c0 + group * 16 + half * 8;
+        const int64_t c = c0 + half * 32 + group * 8;
         if (i * 16 + row >= t.count || c >= a.width) continue;
         for (int k = 0; k < 8; ++k) v[i][half][k] += acc[i][half * 2 + k / 4][k % 4];
         store_columns(out + in[i] * a.ld_out + c, v[i][half]);
@@ -376,28 +398,29 @@ struct PlanArgs {
   const int32_t *which;
   Plan plan;
   int32_t T, L;
-  // backwards: A [L][rank][K] -> [L][K][pitch] and B [L][N][rank] -> [L][rank][N], a workgroup for 64 columns (rows) of one
+  // backwards: A [L][rank][K] -> [L][K][pitch] and B [L][N][rank] -> [L][rank][N], in units of `columns` of K or N
   const __bf16 *a, *b;
   __bf16 *at, *bt;
   int64_t K, N, units;
-  int32_t rank, pitch;
+  int32_t rank, pitch, columns;
 };
 
 // Stable counting sort by one workgroup, each wave its own stretch of the tokens, 64 at a time.
 __device__ inline void plan_tokens(const PlanArgs &p) {
-  extern __shared__ int32_t counts[];            // [16][groups]: each wave's tokens of a group, then how many come before them
-  const int32_t groups = p.L + 1;
-  int32_t *const tile_begin = counts + 16 * groups, *const members = tile_begin + groups + 1;
+  extern __shared__ int32_t counts[];            // [16][groups + 1]: each wave's tokens of a group, then how many come before them
+  const int32_t groups = p.L + 1, line = groups + 1;
+  int32_t *const tile_begin = counts + 16 * line, *const members = tile_begin + groups + 1;
   __shared__ int32_t waves[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  for (int32_t i = threadIdx.x; i < 16 * groups; i += kPlanThreads) counts[i] = 0;
+  for (int32_t i = threadIdx.x; i < 16 * line; i += kPlanThreads) counts[i] = 0;
   __syncthreads();
-  int32_t *const mine = counts + wave * groups;
+  int32_t *const mine = counts + wave * line;
   const int32_t slice = (p.T + 1023) / 1024 * 64, begin = wave * slice;
   const int32_t end = begin + slice < p.T ? begin + slice : p.T;
   // the lanes with this lane's group
   const auto alike = [&](int32_t l) {
     uint64_t m = ~(uint64_t)0;
+    if (__ballot(l == __builtin_amdgcn_readfirstlane(l)) == m) return m;       // (requests one after the other: nearly always)
     for (int32_t bit = 1; bit <= groups; bit <<= 1) {
       const uint64_t set = __ballot((l & bit) != 0);
       m &= l & bit ? set : ~set;
@@ -405,25 +428,32 @@ __device__ inline void plan_tokens(const PlanArgs &p) {
     return m;
   };
   constexpr int kAhead = 16;                     // loads on their way
+  int32_t group[kAhead];
   for (int pass = 0; pass < 2; ++pass) {
     for (int32_t t0 = begin; t0 < end; t0 += 64 * kAhead) {
-      int32_t group[kAhead];
+      if (pass == 0 || slice > 64 * kAhead) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int32_t t = t0 + i * 64 + lane;
-        group[i] = t < end ? p.which[t] : 0;
+        for (int i = 0; i < kAhead; ++i) {
+          const int32_t t = t0 + i * 64 + lane;
+          group[i] = t < end ? p.which[t] : 0;
+        }
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int32_t t = t0 + i * 64 + lane;
-        if (t0 + i * 64 >= end) break;
-        // (past the end: a group of its own, not counted)
+        // (past the end: a group of its own, which nobody reads)
         const int32_t l = t >= end ? groups : group[i] >= 0 && group[i] < p.L ? group[i] : p.L;
+        if (t0 + i * 64 >= end) break;
         const uint64_t m = alike(l);
-        const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1)), at = t < end ? mine[l] : 0;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");        // (all lanes have read before one writes, and the other way)
-        if (pass == 1 && t < end) p.plan.order[(int64_t)tile_begin[l] * kTile + at + before] = t;
-        if (before == 0 && t < end) mine[l] = at + __popcll(m);
+        const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1));
+        // A wave's LDS instructions run in their order, so the lanes have all read before the first of each group adds; the fences keep
+        // the compiler to it.
+        if (pass == 1) {
+          const int32_t at = mine[l];
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          if (t < end) p.plan.order[(int64_t)tile_begin[l] * kTile + at + before] = t;
+        }
+        if (before == 0) __hip_atomic_fetch_add(mine + l, __popcll(m), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
@@ -435,8 +465,8 @@ __device__ inline void plan_tokens(const PlanArgs &p) {
     for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
       int32_t n = 0;
       for (int w = 0; w < 16; ++w) {
-        const int32_t of = counts[w * groups + g];
-        counts[w * groups + g] = n;
+        const int32_t of = counts[w * line + g];
+        counts[w * line + g] = n;
         n += of;
       }
       members[g] = n;
@@ -473,30 +503,51 @@ __device__ inline void plan_tokens(const PlanArgs &p) {
   }
 }
 
+// One unit: p.columns columns of an A, or rows of a B, through LDS.
 __device__ inline void transpose(const PlanArgs &p, int64_t unit) {
   extern __shared__ int32_t space[];
-  __bf16 *const tile = reinterpret_cast<__bf16 *>(space);              // [64][rank + 2]
-  const int64_t of_a = (p.K + 63) / 64, of_b = (p.N + 63) / 64, l = unit / (of_a + of_b);
-  int64_t c = unit % (of_a + of_b);
-  const int lines = p.rank + 2;
-  if (c < of_a) {
-    c *= 64;
-    const __bf16 *const from = p.a + l * p.rank * p.K;
-    for (int i = threadIdx.x; i < p.rank * 64; i += kPlanThreads)
-      if (c + i % 64 < p.K) tile[i % 64 * lines + i / 64] = from[i / 64 * p.K + c + i % 64];
+  __bf16 *const tile = reinterpret_cast<__bf16 *>(space);              // [columns][line]
+  const int64_t of_a = (p.K + p.columns - 1) / p.columns, of_b = (p.N + p.columns - 1) / p.columns, l = unit / (of_a + of_b);
+  const int64_t u = unit % (of_a + of_b);
+  const int line = p.pitch + 2, eights = p.columns / 8, pieces = p.pitch / 8;
+  if (u < of_a) {
+    const int64_t c = u * p.columns;
+    const int n = (int)(p.K - c < p.columns ? p.K - c : p.columns);    // (a multiple of 8)
+    const __bf16 *const from = p.a + l * p.rank * p.K + c;
+    for (int i = threadIdx.x; i < p.pitch * eights; i += kPlanThreads) {
+      const int rank = i / eights, k0 = i % eights * 8;
+      if (k0 >= n) continue;
+      const bf16x8 v = rank < p.rank ? load8(from + rank * p.K + k0) : bf16x8{};
+      for (int k = 0; k < 8; ++k) tile[(k0 + k) * line + rank] = v[k];
+    }
     __syncthreads();
     __bf16 *const to = p.at + (l * p.K + c) * p.pitch;
-    for (int i = threadIdx.x; i < 64 * p.pitch; i += kPlanThreads)
-      if (c + i / p.pitch < p.K) to[i] = i % p.pitch < p.rank ? tile[i / p.pitch * lines + i % p.pitch] : (__bf16)0.0f;
+    for (int i = threadIdx.x; i < n * pieces; i += kPlanThreads) {
+      bf16x8 v;
+      for (int k = 0; k < 8; ++k) v[k] = tile[i / pieces * line + i % pieces * 8 + k];
+      *reinterpret_cast<bf16x8 *>(to + (int64_t)i * 8) = v;
+    }
   } else {
-    c = (c - of_a) * 64;
+    const int64_t c = (u - of_a) * p.columns;
+    const int n = (int)(p.N - c < p.columns ? p.N - c : p.columns);
     const __bf16 *const from = p.b + (l * p.N + c) * p.rank;
-    for (int i = threadIdx.x; i < 64 * p.rank; i += kPlanThreads)
-      if (c + i / p.rank < p.N) tile[i / p.rank * lines + i % p.rank] = from[i];
+    if (p.rank % 8 == 0) {
+      for (int i = threadIdx.x; i < n * pieces; i += kPlanThreads) {
+        const bf16x8 v = load8(from + (int64_t)i * 8);
+        for (int k = 0; k < 8; ++k) tile[i / pieces * line + i % pieces * 8 + k] = v[k];
+      }
+    } else {
+      for (int i = threadIdx.x; i < n * p.rank; i += kPlanThreads) tile[i / p.rank * line + i % p.rank] = from[i];
+    }
     __syncthreads();
     __bf16 *const to = p.bt + l * p.rank * p.N + c;
-    for (int i = threadIdx.x; i < p.rank * 64; i += kPlanThreads)
-      if (c + i % 64 < p.N) to[i / 64 * p.N + i % 64] = tile[i % 64 * lines + i / 64];
+    for (int i = threadIdx.x; i < p.rank * eights; i += kPlanThreads) {
+      const int rank = i / eights, k0 = i % eights * 8;
+      if (k0 >= n) continue;
+      bf16x8 v;
+      for (int k = 0; k < 8; ++k) v[k] = tile[(k0 + k) * line + rank];
+      *reinterpret_cast<bf16x8 *>(to + rank * p.N + k0) = v;
+    }
   }
 }
 
@@ -544,7 +595,7 @@ __global__ void __launch_bounds__(256) k_outer(OuterArgs a) {
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   const int64_t c0 = (int64_t)chunk * kOuterWidth + wave * 128, c = c0 + row * 8;
   if (c0 >= f.width) return;
-  const bool in = c < f.width;
+  const __bf16 *const from = f.x + (c < f.width ? c : f.width - 8);          // (columns past the last are not kept)
   const int64_t size = f.width * a.rank;
   const int32_t count = *a.plan.count, first = range * a.tiles, last = first + a.tiles < count ? first + a.tiles : count;
   f32x4 acc[RT][8] = {};
@@ -580,8 +631,7 @@ __global__ void __launch_bounds__(256) k_outer(OuterArgs a) {
   };
   const auto fetch = [&](int32_t i) {
     if (i >= last) return;
-    for (int q = 0; q < 8; ++q)
-      x[q] = in && token[q] >= 0 ? *reinterpret_cast<const u32x4 *>(f.x + token[q] * f.ld + c) : u32x4{};
+    for (int q = 0; q < 8; ++q) x[q] = *reinterpret_cast<const u32x4 *>(from + (token[q] < 0 ? 0 : token[q]) * f.ld);
     for (int r = 0; r < RT; ++r)
       for (int which = 0; which < 3; ++which)
         hs[r][which] = load8(f.terms + ((i * (int64_t)3 + which) * a.term_ranks + rank0 + r * 16 + row) * kTile + group * 8);
@@ -590,10 +640,13 @@ __global__ void __launch_bounds__(256) k_outer(OuterArgs a) {
   fetch(first);
   fetch_tokens(first + 1);
   for (int32_t i = first; i < last; ++i) {
-    const int32_t l = a.plan.tiles[i].adapter;
-    if (l < 0) break;                            // (they come last)
-    if (l != adapter) flush();
-    adapter = l;
+    const Tile t = a.plan.tiles[i];
+    if (t.adapter < 0) break;                    // (they come last)
+    if (t.adapter != adapter) flush();
+    adapter = t.adapter;
+    if (t.count < kTile)                         // (the terms there are 0, but what was loaded need not be finite)
+      for (int q = 0; q < 8; ++q)
+        if (group * 8 + q >= t.count) x[q] = u32x4{};
     bf16x8 xt[8], now[RT][3];
     for (int j = 0; j < 8; ++j) {
       u32x4 p;
@@ -701,43 +754,49 @@ struct Layout {
   }
 };
 
+// LDS words of plan_tokens
+constexpr size_t plan_words(int64_t adapters) { return 16 * (size_t)(adapters + 2) + (size_t)(adapters + 2) + (size_t)(adapters + 1); }
+
 int run_plan(const nvfp4_adapters_params &p, const Layout &d, char *w, const int32_t *which, const void *a, const void *b,
              hipStream_t s) {
-  PlanArgs g{which, d.plan(w), (int32_t)p.tokens, (int32_t)p.adapters, static_cast<const __bf16 *>(a), static_cast<const __bf16 *>(b),
-             reinterpret_cast<__bf16 *>(w + d.at), reinterpret_cast<__bf16 *>(w + d.bt), p.inp, p.out,
-             a ? p.adapters * (divide_up(p.inp, 64) + divide_up(p.out, 64)) : 0, (int32_t)p.rank, (int32_t)Layout::pitch(p)};
-  const size_t counts = (18 * (size_t)(p.adapters + 1) + 1) * 4, tile = a ? 64 * (size_t)(p.rank + 2) * 2 : 0;
-  constexpr size_t kMostLds = (18 * (kMostAdapters + 1) + 1) * 4;
+  const int32_t pitch = (int32_t)Layout::pitch(p), columns = (pitch <= 8 ? 1024 : pitch <= 16 ? 512 : pitch <= 32 ? 256 : pitch <= 64 ? 128 : 64);
+  const PlanArgs g{which, d.plan(w), (int32_t)p.tokens, (int32_t)p.adapters, static_cast<const __bf16 *>(a), static_cast<const __bf16 *>(b),
+                   reinterpret_cast<__bf16 *>(w + d.at), reinterpret_cast<__bf16 *>(w + d.bt), p.inp, p.out,
+                   a ? p.adapters * (divide_up(p.inp, columns) + divide_up(p.out, columns)) : 0, (int32_t)p.rank, pitch, columns};
+  const size_t counts = plan_words(p.adapters) * 4, tile = a ? (size_t)columns * (pitch + 2) * 2 : 0;
+  constexpr size_t kMostLds = plan_words(kMostAdapters) * 4;
   if (counts > 48 * 1024 &&
       hipFuncSetAttribute(reinterpret_cast<const void *>(k_plan), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds) != hipSuccess)
     return NVFP4_ERR_HIP;
   return launch(k_plan, dim3((uint32_t)(1 + (g.units < 65536 ? g.units : 65536))), dim3(kPlanThreads), counts > tile ? counts : tile, s, g);
 }
 
-template <int MT, int RT, int W, int D>
+template <bool FEW, int MT, int RT, int W, int D>
 int run_shrink_of(const ShrinkArgs &g, int64_t tiles, int64_t splits, hipStream_t s) {
-  return launch(k_shrink<MT, RT, W, D>, dim3((uint32_t)tiles, (uint32_t)splits), dim3(W * 64), 0, s, g);
+  return launch(k_shrink<FEW, MT, RT, W, D>, dim3((uint32_t)tiles, (uint32_t)splits), dim3(W * 64), 0, s, g);
 }
 int run_shrink(ShrinkArgs g, const Layout &d, int64_t splits, hipStream_t s) {
   g.steps = (int32_t)divide_up(divide_up(g.width, kBlock), splits);
-  const int64_t tiles = d.few ? g.tokens.T : d.tiles;
   if (d.few) {
-    if (g.rank <= 16) return run_shrink_of<1, 1, 8, 4>(g, tiles, splits, s);
-    if (g.rank <= 32) return run_shrink_of<1, 2, 8, 3>(g, tiles, splits, s);
-    if (g.rank <= 64) return run_shrink_of<1, 4, 8, 2>(g, tiles, splits, s);
-    return run_shrink_of<1, 8, 4, 2>(g, tiles, splits, s);
+    const int64_t tiles = g.tokens.T;
+    if (g.rank <= 16) return run_shrink_of<true, 1, 1, 8, 4>(g, tiles, splits, s);
+    if (g.rank <= 32) return run_shrink_of<true, 1, 2, 8, 3>(g, tiles, splits, s);
+    if (g.rank <= 64) return run_shrink_of<true, 1, 4, 8, 2>(g, tiles, splits, s);
+    return run_shrink_of<true, 1, 8, 4, 2>(g, tiles, splits, s);
   }
-  if (g.rank <= 16) return run_shrink_of<2, 1, 8, 4>(g, tiles, splits, s);
-  if (g.rank <= 32) return run_shrink_of<2, 2, 8, 3>(g, tiles, splits, s);
-  if (g.rank <= 64) return run_shrink_of<2, 4, 4, 2>(g, tiles, splits, s);
-  return run_shrink_of<2, 8, 4, 2>(g, tiles, splits, s);
+  if (g.rank <= 16) return run_shrink_of<false, 1, 1, 4, 4>(g, 2 * d.tiles, splits, s);
+  if (g.rank <= 32) return run_shrink_of<false, 2, 2, 4, 3>(g, d.tiles, splits, s);
+  if (g.rank <= 64) return run_shrink_of<false, 2, 4, 4, 2>(g, d.tiles, splits, s);
+  return run_shrink_of<false, 2, 8, 4, 2>(g, d.tiles, splits, s);
 }
 
 template <typename T, int F>
 int run_expand_of(const ExpandArgs &g, const Layout &d, hipStream_t s) {
   const int64_t blocks = divide_up(g.width, kBlock * 4), tiles = d.few ? g.tokens.T : d.tiles, want = g.out ? divide_up(2048, tiles) : 1;
   const dim3 grid((uint32_t)tiles, (uint32_t)(want < blocks ? want : blocks));
-  return d.few ? launch(k_expand<T, 1, F>, grid, dim3(256), 0, s, g) : launch(k_expand<T, 2, F>, grid, dim3(256), 0, s, g);
+  if (g.pitch % 8)
+    return d.few ? launch(k_expand<true, false, T, 1, F>, grid, dim3(256), 0, s, g) : launch(k_expand<false, false, T, 2, F>, grid, dim3(256), 0, s, g);
+  return d.few ? launch(k_expand<true, true, T, 1, F>, grid, dim3(256), 0, s, g) : launch(k_expand<false, true, T, 2, F>, grid, dim3(256), 0, s, g);
 }
 template <typename T>
 int run_expand(const ExpandArgs &g, const Layout &d, hipStream_t s) {
@@ -774,7 +833,7 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (!d.few)
     if (const int rc = run_plan(*p, d, w, which, nullptr, nullptr, s)) return rc;
-  const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters, d.few};
+  const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters};
   float *const parts = reinterpret_cast<float *>(w + d.parts);
   const int32_t rank = (int32_t)p->rank, pitch = (int32_t)Layout::pitch(*p);
   ShrinkArgs g{};
@@ -811,7 +870,7 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool any = p->tokens != 0;
   if (const int rc = run_plan(*p, d, w, which, any ? a : nullptr, b, s)) return rc;
-  const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters, false};
+  const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters};
   float *const parts = reinterpret_cast<float *>(w + d.parts);
   __bf16 *const terms_a = reinterpret_cast<__bf16 *>(w + d.terms_a), *const terms_b = reinterpret_cast<__bf16 *>(w + d.terms_b);
   const int32_t rank = (int32_t)p->rank, pitch = (int32_t)Layout::pitch(*p), term_ranks = (int32_t)Layout::term_ranks(*p);
