@@ -27,9 +27,10 @@ constexpr int kFewTile = 16;                    // ... and of a tile that a work
 constexpr int kFewTokens = 256;                 // up to here there is no plan (find_tile)
 constexpr int kPlanThreads = 1024;
 constexpr int kOuterWidth = 512;                // columns of a workgroup of k_outer, 128 a wave
-constexpr int kBlock = 64;                      // columns of a step of k_shrink, of a block of k_expand
+constexpr int kBlock = 64;                      // columns of a block of k_expand
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -71,13 +72,15 @@ template <bool FEW, int NT>
 __device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t index, int rows) {
   Tile t{-1, 0};
   if constexpr (!FEW) {
-    const int halves = kTile / rows;
-    if (index / halves >= *k.plan.count) return t;
-    t = k.plan.tiles[index / halves];
+    // (the three are asked for together; past the last tile they hold anything)
+    const int halves = kTile / rows, tile = index / halves;
+    const int32_t tiles = *k.plan.count, token = (int)threadIdx.x < rows ? k.plan.order[(int64_t)index * rows + threadIdx.x] : 0;
+    t = k.plan.tiles[tile];
+    if (tile >= tiles) return {-1, 0};
     t.count -= index % halves * rows;
     if (t.count <= 0) return {-1, 0};
     if (t.count > rows) t.count = rows;
-    if ((int)threadIdx.x < t.count) shared.token[threadIdx.x] = k.plan.order[(int64_t)index * rows + threadIdx.x];
+    if ((int)threadIdx.x < rows) shared.token[threadIdx.x] = token;
     __syncthreads();
     return t;
   }
@@ -126,13 +129,6 @@ __device__ inline __bf16 term(float v, int which) {
   return which == 1 ? mid : (__bf16)(rest - (float)mid);
 }
 
-// Eight ranks of a token, from `first`: their three terms where k_outer looks for them, [tile][term][rank][token].
-__device__ inline void put_terms(__bf16 *terms, int64_t tile, int32_t ranks, int token, int first, const float *v) {
-  if (first >= ranks) return;
-  for (int which = 0; which < 3; ++which)
-    for (int k = 0; k < 8; ++k) terms[((tile * 3 + which) * ranks + first + k) * kTile + token] = term(v[k], which);
-}
-
 // ---- k_shrink ---------------------------------------------------------------------------------------------------------
 
 struct ShrinkArgs {
@@ -144,99 +140,122 @@ struct ShrinkArgs {
   const float *terms_of, *scales;
   __bf16 *terms;
   int64_t ld, width;
-  int32_t rank, pitch, steps;  // steps of 64 columns of a split
+  int32_t rank, pitch;
+  int32_t steps;               // 32 columns each, of a wave: at most NF
   int32_t term_ranks;
 };
 
-// D[token][rank]: rows of x against rows of w, both adjacent in the summed index.  A lane takes twice 8 columns of a step, of row
-// lane % 16 of each side: a load has 64 adjacent bytes of 16 rows, a step 128.  The waves of a workgroup take every W-th step of its split, D of them
-// on their way at a time.
-template <bool FEW, int MT, int RT, int W, int D>
-__global__ void __launch_bounds__(W * 64) k_shrink(ShrinkArgs a) {
+constexpr int kShrinkWaves = 8;
+
+// D[token][rank]: rows of x against rows of w, both adjacent in the summed index.  A wave has its own columns and keeps their part of w
+// in registers while it goes through 16 tokens at a time of the workgroup's stretch of the plan; the waves' sums meet in LDS.  A load has
+// 64 adjacent bytes of 16 rows; the columns of the next tokens are on their way while these are multiplied.
+template <bool FEW, int RT, int NF>
+__global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shrink(ShrinkArgs a) {
+  constexpr int kThreads = kShrinkWaves * 64, kBuffers = RT <= 4 ? 2 : 1;
   __shared__ TileTokens shared;
-  __shared__ float part[W][MT * RT * 256];
-  const Tile t = find_tile<FEW, W * 64>(a.tokens, shared, blockIdx.x, MT * 16);
-  if (t.count == 0) return;
-  if (t.adapter < 0) {
-    if (a.h)
-      for (int i = threadIdx.x; i < t.count * a.rank; i += W * 64) a.h[(int64_t)shared.token[i / a.rank] * a.rank + i % a.rank] = 0.0f;
-    return;
-  }
+  __shared__ float part[kBuffers][kShrinkWaves][RT * 256];
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
-  const __bf16 *x[MT], *w[RT];
-  for (int i = 0; i < MT; ++i) {
-    const int n = i * 16 + row < t.count ? i * 16 + row : t.count - 1;            // (rows past the tile's are not kept)
-    x[i] = a.x + shared.token[n] * a.ld + group * 8;
+  int32_t first = 0, last = 1;                   // 16 tokens each
+  Tile only{};
+  if constexpr (FEW) {
+    only = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, 16);
+    if (only.count == 0) return;
+  } else {
+    const int32_t all = 2 * *a.tokens.plan.count, per = (all + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
+    first = (int32_t)blockIdx.x * per;
+    last = first + per < all ? first + per : all;
   }
-  for (int i = 0; i < RT; ++i) {
-    const int n = i * 16 + row < a.rank ? i * 16 + row : a.rank - 1;
-    w[i] = a.w + ((int64_t)t.adapter * a.rank + n) * a.width + group * 8;
+  const auto tile_of = [&](int32_t i) {          // the 16 tokens i
+    if constexpr (FEW) return only;
+    Tile t = a.tokens.plan.tiles[i / 2];
+    t.count -= i % 2 * 16;
+    if (t.count > 16) t.count = 16;
+    return t;
+  };
+  const auto token_of = [&](int32_t i, int n) -> int32_t {      // -1: there is none
+    if constexpr (FEW) return n < only.count ? shared.token[n] : -1;
+    return a.tokens.plan.order[(int64_t)i * 16 + n];
+  };
+  const int32_t all_steps = (int32_t)((a.width + 31) / 32), step0 = ((int32_t)blockIdx.y * kShrinkWaves + wave) * a.steps;
+  const int32_t mine = all_steps - step0 < a.steps ? all_steps - step0 : a.steps;
+  const int32_t width = (int32_t)a.width, c0 = step0 * 32 + group * 8;
+  const bool whole = mine == NF && (step0 + NF) * 32 <= width;
+  const auto fetch = [&](bf16x8 *to, const __bf16 *from) {      // (where there is no such column, another)
+#pragma unroll
+    for (int f = 0; f < NF; ++f) to[f] = load8(from + (c0 + f * 32 < width ? c0 + f * 32 : width - 8));
+  };
+  const auto clear = [&](bf16x8 *to) {           // what is no column of this wave's counts as 0, whatever was loaded
+    if (whole) return;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+      if (f >= mine || c0 + f * 32 >= width) to[f] = bf16x8{};
+  };
+  const auto row_of = [&](int32_t token) { return a.x + (int64_t)(token < 0 ? 0 : token) * a.ld; };
+  bf16x8 w[RT][NF], x[NF];
+  int32_t token = 0, buffer = 0;
+  if (first < last) {
+    fetch(x, row_of(token_of(first, row)));
+    if (first + 1 < last) token = token_of(first + 1, row);
   }
-  f32x4 acc[MT][RT] = {};
-  bf16x8 xs[D][MT][2], ws[D][RT][2];
-  const int32_t whole = (int32_t)(a.width / kBlock), first = (int32_t)blockIdx.y * a.steps, end = first + a.steps;
-  // this wave's steps: first + wave + i W, i < n
-  const int32_t n = ((end < whole ? end : whole) - first - wave + W - 1) / W;
-  const auto fetch = [&](int d, int32_t i) {
-    const int64_t k = (int64_t)(first + wave + (i < n ? i : n - 1) * W) * kBlock;        // (past the end: once more what it had)
-    for (int c = 0; c < 2; ++c) {
-      for (int m = 0; m < MT; ++m) xs[d][m][c] = load8(x[m] + k + c * 32);
-      for (int r = 0; r < RT; ++r) ws[d][r][c] = load8(w[r] + k + c * 32);
+  for (int32_t i = first; i < last;) {           // one adapter after the other
+    const int32_t adapter = tile_of(i).adapter;
+    if (adapter < 0) break;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int n = r * 16 + row < a.rank ? r * 16 + row : a.rank - 1;            // (ranks past the last are not kept)
+      fetch(w[r], a.w + ((int64_t)adapter * a.rank + n) * a.width);
+      clear(w[r]);
     }
-  };
-  const auto product = [&](int d) {
-    for (int c = 0; c < 2; ++c)
-      for (int m = 0; m < MT; ++m)
-        for (int r = 0; r < RT; ++r) acc[m][r] = multiply(xs[d][m][c], ws[d][r][c], acc[m][r]);
-  };
-  if (n > 0) {
+    for (; i < last; ++i) {
+      const Tile t = tile_of(i);
+      if (t.adapter != adapter) break;
+      clear(x);
+      f32x4 acc[RT] = {};
 #pragma unroll
-    for (int d = 0; d < D - 1; ++d) fetch(d, d);
-    int32_t i = 0;
-    for (; i + D <= n; i += D)
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-      for (int d = 0; d < D; ++d) {
-        fetch((d + D - 1) % D, i + d + D - 1);
-        product(d);
+        for (int r = 0; r < RT; ++r) acc[r] = multiply(x[f], w[r][f], acc[r]);
+      __builtin_amdgcn_sched_barrier(0);         // (the next columns go where these were: a second place for them costs a workgroup a CU)
+      if (i + 1 < last) {
+        fetch(x, row_of(token));
+        if (i + 2 < last) token = token_of(i + 2, row);
       }
+      if (t.count <= 0) continue;                // (the second half of a tile of 16)
+      // (a buffer is written again only after the barrier of the tile in between, which all waves reach done with reading it)
+      float(*const p)[RT * 256] = part[buffer];
+      if (kBuffers == 1) __syncthreads();
+      else buffer ^= 1;
 #pragma unroll
-    for (int d = 0; d < D - 1; ++d)
-      if (i + d < n) product(d);
-  }
-  if (a.width % kBlock && whole >= first && whole < end && whole % W == wave) {        // the last columns, fewer than a step's
-    for (int c = 0; c < 2; ++c) {
-      const int64_t k = (int64_t)whole * kBlock + c * 32;
-      const bool in = k + group * 8 < a.width;
-      for (int m = 0; m < MT; ++m) xs[0][m][c] = in ? load8(x[m] + k) : bf16x8{};
-      for (int r = 0; r < RT; ++r) ws[0][r][c] = in ? load8(w[r] + k) : bf16x8{};
-    }
-    product(0);
-  }
-  for (int i = 0; i < MT; ++i)
-    for (int j = 0; j < RT; ++j)
-      for (int v = 0; v < 4; ++v) part[wave][(i * RT + j) * 256 + (group * 4 + v) * 16 + row] = acc[i][j][v];
-  __syncthreads();
-  float *const parts = a.parts + (int64_t)blockIdx.y * a.tokens.T * a.pitch;
-  for (int e = threadIdx.x; e < MT * RT * 256; e += W * 64) {
-    const int n = e / (RT * 256) * 16 + e % 256 / 16, rank = e / 256 % RT * 16 + e % 16;
-    float s = 0.0f;
-    for (int i = 0; i < W; ++i) s += part[i][e];
-    if (n < t.count && rank < a.pitch) {
-      parts[(int64_t)shared.token[n] * a.pitch + rank] = rank < a.rank ? s : 0.0f;
-      if (a.h && rank < a.rank) a.h[(int64_t)shared.token[n] * a.rank + rank] = s;
+      for (int r = 0; r < RT; ++r)
+        for (int v = 0; v < 4; ++v) p[wave][r * 256 + (group * 4 + v) * 16 + row] = acc[r][v];
+      __syncthreads();
+      for (int e = threadIdx.x; e < RT * 256; e += kThreads) {
+        const int n = e % 256 / 16, rank = e / 256 * 16 + e % 16;
+        const int32_t to = token_of(i, n);
+        float s = 0.0f;
+        for (int k = 0; k < kShrinkWaves; ++k) s += p[k][e];
+        if (to >= 0 && rank < a.pitch) {
+          a.parts[((int64_t)blockIdx.y * a.tokens.T + to) * a.pitch + rank] = rank < a.rank ? s : 0.0f;
+          if (a.h && rank < a.rank) a.h[(int64_t)to * a.rank + rank] = s;
+        }
+      }
     }
   }
-  constexpr int kParts = kTile / (MT * 16);      // workgroups of a planned tile: the first sees to the terms of all of it
-  if (a.terms_of && blockIdx.y == 0 && blockIdx.x % kParts == 0) {
-    const int64_t tile = blockIdx.x / kParts;
-    const float scale = a.scales[t.adapter];
-    for (int e = threadIdx.x; e < kTile * a.term_ranks / 8; e += W * 64) {
-      const int n = e % kTile, from = e / kTile * 8, token = a.tokens.plan.order[tile * kTile + n];
-      const float *const h = a.terms_of + (int64_t)(token < 0 ? 0 : token) * a.rank;
-      float v[8];
-      for (int k = 0; k < 8; ++k) v[k] = h[from + k < a.rank ? from + k : a.rank - 1];
-      for (int k = 0; k < 8; ++k) v[k] = token >= 0 && from + k < a.rank ? scale * v[k] : 0.0f;
-      put_terms(a.terms, tile, a.term_ranks, n, from, v);
+  if (a.h)                                       // tokens without an adapter come last
+    for (int32_t i = last; i-- > first && tile_of(i).adapter < 0;)
+      for (int e = threadIdx.x; e < tile_of(i).count * a.rank; e += kThreads)
+        a.h[(int64_t)token_of(i, e / a.rank) * a.rank + e % a.rank] = 0.0f;
+  if (FEW || !a.terms_of || blockIdx.y != 0) return;
+  for (int32_t tile = (first + 1) / 2; tile < (last + 1) / 2; ++tile) {             // those that begin in this stretch
+    const int32_t l = a.tokens.plan.tiles[tile].adapter;
+    if (l < 0) break;
+    for (int e = threadIdx.x; e < kTile * a.term_ranks; e += kThreads) {
+      const int n = e % kTile, rank = e / kTile;
+      const int32_t of = a.tokens.plan.order[(int64_t)tile * kTile + n];
+      const bool is = of >= 0 && rank < a.rank;
+      const float h = a.terms_of[(int64_t)(is ? of : 0) * a.rank + (is ? rank : 0)], v = is ? a.scales[l] * h : 0.0f;
+      for (int which = 0; which < 3; ++which) a.terms[(((int64_t)tile * 3 + which) * a.term_ranks + rank) * kTile + n] = term(v, which);
     }
   }
 }
@@ -247,7 +266,7 @@ struct ExpandArgs {
   Tokens tokens;
   const float *parts;          // [splits][T][h_pitch]
   float *h;                    // their sum [T][rank], where it is wanted and k_shrink has not written it; or nullptr
-  __bf16 *terms;               // backwards: the terms of s h for k_outer; or nullptr
+  __bf16 *terms;               // backwards: the three terms of s h for k_outer, [tile][term][rank][token]; or nullptr
   const __bf16 *w;             // [L][width] rows of `rank`, `pitch` apart
   const float *scales;
   const void *base;
@@ -266,129 +285,180 @@ __device__ inline bf16x8 load_ranks(const __bf16 *row, int first, int rank) {
   return v;
 }
 
-// Eight columns of a row, as fp32.
+// Eight columns of a row as they are in memory, and as fp32.
 template <typename T>
-__device__ inline void load_columns(const T *p, float *v) {
-  if constexpr (sizeof(T) == 4) {
-    for (int i = 0; i < 2; ++i) {
-      const f32x4 q = reinterpret_cast<const f32x4 *>(p)[i];
-      for (int k = 0; k < 4; ++k) v[i * 4 + k] = q[k];
+struct Columns {
+  u32x4 raw[sizeof(T) / 2];
+  __device__ void load(const T *p) {
+    for (size_t i = 0; i < sizeof(T) / 2; ++i) raw[i] = reinterpret_cast<const u32x4 *>(p)[i];
+  }
+  __device__ float at(int k) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[k / 4][k % 4]);
+    const uint32_t w = raw[0][k / 2];
+    return __uint_as_float(k % 2 ? w & 0xffff0000u : w << 16);
+  }
+  __device__ void add(int k0, f32x4 v) {         // to columns k0 .. k0 + 3
+    if constexpr (sizeof(T) == 4) {
+      for (int k = 0; k < 4; ++k) raw[k0 / 4][k] = __float_as_uint(at(k0 + k) + v[k]);
+    } else {
+      for (int k = 0; k < 4; k += 2) {
+        const bf16x2 q{(__bf16)(at(k0 + k) + v[k]), (__bf16)(at(k0 + k + 1) + v[k + 1])};
+        raw[0][(k0 + k) / 2] = __builtin_bit_cast(uint32_t, q);
+      }
     }
-  } else {
-    const bf16x8 q = load8(p);
-    for (int k = 0; k < 8; ++k) v[k] = (float)q[k];
   }
-}
-template <typename T>
-__device__ inline void store_columns(T *p, const float *v) {
-  if constexpr (sizeof(T) == 4) {
-    for (int i = 0; i < 2; ++i) reinterpret_cast<f32x4 *>(p)[i] = f32x4{v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]};
-  } else {
-    bf16x8 q;
-    for (int k = 0; k < 8; ++k) q[k] = (__bf16)v[k];
-    *reinterpret_cast<bf16x8 *>(p) = q;
+  __device__ void store(T *p) const {
+    for (size_t i = 0; i < sizeof(T) / 2; ++i) reinterpret_cast<u32x4 *>(p)[i] = raw[i];
   }
-}
+};
 
 // D[column][token]: rows of w against s h, which enters as terms (term).  Row 4 a + b of product p of a block is column
 // 32 (p / 2) + 8 a + 4 (p % 2) + b, so that a lane ends up with twice 8 adjacent columns of its token, 64 bytes in four lanes.  The summed index of a product is four pieces of
 // eight ranks: F > 0: 32 ranks of one term, F times.  F == 0, rank <= 16: the one or two pieces of every term side by side.
-// The workgroup sums the parts of h and splits them once, into LDS.
-template <bool FEW, bool WHOLE, typename T, int MT, int F>
-__global__ void __launch_bounds__(256) k_expand(ExpandArgs a) {
+// A wave has a block of columns of its own and keeps their part of w in registers while it goes through the workgroup's stretch of the
+// plan; per tile the workgroup sums the parts of s h and splits them once, into LDS, while the tile's columns of base are on their way.
+template <bool FEW, bool WHOLE, typename T, int F>
+__global__ void __launch_bounds__(FEW ? 256 : 512, F < 4 ? 4 : 2) k_expand(ExpandArgs a) {
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 2, kSpans = F ? F : 1, kProducts = F ? kTerms : kTerms - 1;
+  constexpr int MT = FEW ? 1 : 2, kThreads = FEW ? 256 : 512, kWaves = kThreads / 64, kRows = MT * 16;
   __shared__ TileTokens shared;
-  __shared__ bf16x8 split[MT * 16][kTerms * kSpans * 4 + 1];        // (an odd number of pieces: a row a bank further)
-  const Tile t = find_tile<FEW, 256>(a.tokens, shared, blockIdx.x, MT * 16);
-  if (t.count == 0) return;
+  __shared__ bf16x8 split[FEW ? 1 : 2][kRows][kTerms * kSpans * 4 + 1];      // (an odd number of pieces: a row a bank further)
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
+  int32_t first = 0, last = 1;
+  Tile only{};
+  if constexpr (FEW) {
+    only = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, kRows);
+    if (only.count == 0) return;
+  } else {
+    const int32_t all = *a.tokens.plan.count, per = (all + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
+    first = (int32_t)blockIdx.x * per;
+    last = first + per < all ? first + per : all;
+  }
+  const auto tile_of = [&](int32_t i) {
+    if constexpr (FEW) return only;
+    return a.tokens.plan.tiles[i];
+  };
+  const auto token_of = [&](int32_t i, int n) -> int32_t {       // -1: there is none
+    if constexpr (FEW) return n < only.count ? shared.token[n] : -1;
+    return a.tokens.plan.order[(int64_t)i * kRows + n];
+  };
   const T *const base = static_cast<const T *>(a.base);
   T *const out = static_cast<T *>(a.out);
-  if (t.adapter < 0) {
-    if (a.h && blockIdx.y == 0)
-      for (int i = threadIdx.x; i < t.count * a.rank; i += 256) a.h[(int64_t)shared.token[i / a.rank] * a.rank + i % a.rank] = 0.0f;
-    if (!out || base == out) return;
-    for (int n = wave; n < t.count; n += 4)
-      for (int64_t c = ((int64_t)blockIdx.y * 64 + lane) * 8; c < a.width; c += (int64_t)gridDim.y * 512) {
-        float v[8] = {};
-        if (base) load_columns(base + shared.token[n] * a.ld_base + c, v);
-        store_columns(out + shared.token[n] * a.ld_out + c, v);
-      }
-    return;
-  }
-  const float scale = a.scales[t.adapter];
-  for (int e = threadIdx.x; e < MT * 16 * kSpans * 4; e += 256) {
-    const int n = e / (kSpans * 4), piece = e % (kSpans * 4), first = piece * 8;
-    float v[8] = {};
-    if (n < t.count && first < a.rank) {
-      const float *const from = a.parts + (int64_t)shared.token[n] * a.h_pitch + first;
-      for (int p = 0; p < a.splits; ++p) {
-        const f32x4 *const q = reinterpret_cast<const f32x4 *>(from + (int64_t)p * a.tokens.T * a.h_pitch);
-        for (int k = 0; k < 8; ++k) v[k] += q[k / 4][k % 4];
-      }
-      if (a.h && blockIdx.y == 0)
-        for (int k = 0; k < 8; ++k)
-          if (first + k < a.rank) a.h[(int64_t)shared.token[n] * a.rank + first + k] = v[k];
-    }
-    for (int k = 0; k < 8; ++k) v[k] *= scale;
-    for (int which = 0; which < kTerms; ++which) {
-      bf16x8 q;
-      for (int k = 0; k < 8; ++k) q[k] = term(v[k], which);
-      split[n][which * kSpans * 4 + piece] = q;
-    }
-    if (a.terms && blockIdx.y == 0) {
-      if (n >= t.count)
-        for (int k = 0; k < 8; ++k) v[k] = 0.0f;                     // (0 times an infinite scale)
-      put_terms(a.terms, blockIdx.x, a.term_ranks, n, first, v);
-    }
-  }
-  if (!out) return;
-  __syncthreads();
   const int pieces = (a.rank + 7) / 8;
-  bf16x8 h[MT][kSpans][kProducts];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-    for (int f = 0; f < kSpans; ++f)
-      for (int n = 0; n < kProducts; ++n) {
-        if (F) {
-          h[i][f][n] = split[i * 16 + row][n * kSpans * 4 + f * 4 + group];
-        } else {
-          const int q = n * 4 + group, which = q / pieces;
-          h[i][f][n] = which < kTerms ? split[i * 16 + row][which * 4 + q % pieces] : bf16x8{};
+  const int32_t width = (int32_t)a.width, c0 = ((int32_t)blockIdx.y * kWaves + wave) * kBlock;
+  const bool idle = c0 >= width || !out;         // a wave past the last column only helps with h
+  const auto column = [&](int half) { return c0 + half * 32 + group * 8; };
+
+  const auto prepare = [&](int32_t i, int buffer) {
+    const Tile t = tile_of(i);
+    if (t.adapter < 0) return;
+    const float scale = a.scales[t.adapter];
+    const bool mine = FEW ? blockIdx.y == 0 : i % (int32_t)gridDim.y == (int32_t)blockIdx.y;      // whose h or terms it is to write
+    for (int e = threadIdx.x; e < kRows * kSpans * 4; e += kThreads) {
+      const int n = e / (kSpans * 4), piece = e % (kSpans * 4), from = piece * 8;
+      const int32_t token = token_of(i, n);
+      float v[8] = {};
+      if (token >= 0 && piece < pieces) {
+        const float *const part = a.parts + (int64_t)token * a.h_pitch + from;
+        for (int p = 0; p < a.splits; ++p) {
+          const f32x4 *const q = reinterpret_cast<const f32x4 *>(part + (int64_t)p * a.tokens.T * a.h_pitch);
+          for (int k = 0; k < 8; ++k) v[k] += q[k / 4][k % 4];
         }
+        if (a.h && mine)
+          for (int k = 0; k < 8; ++k)
+            if (from + k < a.rank) a.h[(int64_t)token * a.rank + from + k] = v[k];
+        for (int k = 0; k < 8; ++k) v[k] *= scale;
       }
-  int64_t in[MT];                                // this lane's token of each 16; rows past the tile's are read again and not kept
-  for (int i = 0; i < MT; ++i) in[i] = shared.token[i * 16 + row < t.count ? i * 16 + row : t.count - 1];
-  const __bf16 *const w = a.w + (int64_t)t.adapter * a.width * a.pitch;
-  const int64_t blocks = (a.width + kBlock - 1) / kBlock;
-  for (int64_t b = (int64_t)blockIdx.y * 4 + wave; b < blocks; b += (int64_t)gridDim.y * 4) {
-    const int64_t c0 = b * kBlock;
-    float v[MT][2][8] = {};
+      for (int which = 0; which < kTerms; ++which) {
+        bf16x8 q;
+        for (int k = 0; k < 8; ++k) q[k] = term(v[k], which);
+        split[buffer][n][which * kSpans * 4 + piece] = q;
+      }
+      if (a.terms && mine && from < a.term_ranks)
+        for (int which = 0; which < 3; ++which)
+          for (int k = 0; k < 8; ++k) a.terms[(((int64_t)i * 3 + which) * a.term_ranks + from + k) * kTile + n] = term(v[k], which);
+    }
+  };
+
+  int32_t in[MT];                                // this lane's token of each 16, -1: there is none
+  Columns<T> v[MT][2] = {};                      // (without a base 0)
+  const auto fetch = [&](int32_t i) {            // (rows and columns that there are not: others, which are not kept)
+    for (int m = 0; m < MT; ++m) in[m] = token_of(i, m * 16 + row);
     if (base)
-      for (int i = 0; i < MT; ++i)
-        for (int half = 0; half < 2; ++half) {
-          const int64_t c = c0 + half * 32 + group * 8;
-          load_columns(base + in[i] * a.ld_base + (c < a.width ? c : a.width - 8), v[i][half]);
+      for (int m = 0; m < MT; ++m)
+        for (int half = 0; half < 2; ++half)
+          v[m][half].load(base + (int64_t)(in[m] < 0 ? 0 : in[m]) * a.ld_base + (column(half) < width ? column(half) : width - 8));
+    else
+      for (int m = 0; m < MT; ++m)
+        for (int half = 0; half < 2; ++half) v[m][half] = {};
+  };
+  int buffer = 0;
+  if (first < last) {
+    if (!idle) fetch(first);
+    prepare(first, 0);
+  }
+  __syncthreads();
+  int32_t i = first;
+  while (i < last) {                             // one adapter after the other
+    const int32_t adapter = tile_of(i).adapter;
+    if (adapter < 0) break;
+    bf16x8 w[4][kSpans];
+    if (!idle) {
+      const __bf16 *const of = a.w + (int64_t)adapter * a.width * a.pitch;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const int32_t c = c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4;
+#pragma unroll
+        for (int f = 0; f < kSpans; ++f) {
+          const int piece = F ? f * 4 + group : group % pieces;
+          w[p][f] = load_ranks<WHOLE>(of + (int64_t)(c < width ? c : width - 1) * a.pitch, piece < pieces ? piece * 8 : 0, a.rank);
+          if (F && pieces % 4 && piece >= pieces) w[p][f] = bf16x8{};
         }
-    f32x4 acc[MT][4] = {};
-    for (int p = 0; p < 4; ++p) {
-      int64_t c = c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4;
-      if (c >= a.width) c = a.width - 1;
-      for (int f = 0; f < kSpans; ++f) {
-        const int piece = F ? f * 4 + group : group % pieces;
-        bf16x8 ws = load_ranks<WHOLE>(w + c * a.pitch, piece < pieces ? piece * 8 : 0, a.rank);
-        if (F && pieces % 4 && piece >= pieces) ws = bf16x8{};
-        for (int n = 0; n < kProducts; ++n)
-          for (int i = 0; i < MT; ++i) acc[i][p] = multiply(ws, h[i][f][n], acc[i][p]);
       }
     }
-    for (int i = 0; i < MT; ++i)
-      for (int half = 0; half < 2; ++half) {
-        const int64_t c = c0 + half * 32 + group * 8;
-        if (i * 16 + row >= t.count || c >= a.width) continue;
-        for (int k = 0; k < 8; ++k) v[i][half][k] += acc[i][half * 2 + k / 4][k % 4];
-        store_columns(out + in[i] * a.ld_out + c, v[i][half]);
+    for (; i < last && tile_of(i).adapter == adapter; ++i) {
+      if (!idle) {
+        f32x4 acc[MT][4] = {};
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int f = 0; f < kSpans; ++f)
+#pragma unroll
+            for (int n = 0; n < kProducts; ++n) {
+              bf16x8 h;
+              if (F) {
+                h = split[buffer][m * 16 + row][n * kSpans * 4 + f * 4 + group];
+              } else {
+                const int q = n * 4 + group, which = q / pieces;
+                h = which < kTerms ? split[buffer][m * 16 + row][which * 4 + q % pieces] : bf16x8{};
+              }
+#pragma unroll
+              for (int p = 0; p < 4; ++p) acc[m][p] = multiply(w[p][f], h, acc[m][p]);
+            }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+          for (int half = 0; half < 2; ++half) {
+            for (int k = 0; k < 2; ++k) v[m][half].add(4 * k, acc[m][half * 2 + k]);
+            if (in[m] >= 0 && column(half) < width) v[m][half].store(out + (int64_t)in[m] * a.ld_out + column(half));
+          }
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + 1 < last) fetch(i + 1);
       }
+      if (i + 1 < last) prepare(i + 1, FEW ? 0 : buffer ^ 1);
+      if (!FEW) __syncthreads();                 // (each buffer is written again a barrier after it was read)
+      buffer ^= 1;
+    }
+  }
+  // Tokens without an adapter come last.
+  for (; i < last; ++i) {
+    const Tile t = tile_of(i);
+    if (a.h && blockIdx.y == 0)
+      for (int e = threadIdx.x; e < t.count * a.rank; e += kThreads) a.h[(int64_t)token_of(i, e / a.rank) * a.rank + e % a.rank] = 0.0f;
+    if (idle || base == out) continue;
+    fetch(i);
+    for (int m = 0; m < MT; ++m)
+      for (int half = 0; half < 2; ++half)
+        if (in[m] >= 0 && column(half) < width) v[m][half].store(out + (int64_t)in[m] * a.ld_out + column(half));
   }
 }
 
@@ -565,7 +635,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs p) {
 
 struct OuterHalf {
   const __bf16 *x;             // [T] rows of `width`
-  const __bf16 *terms;         // [tiles][3][term_ranks][32]: of s h (put_terms)
+  const __bf16 *terms;         // [tiles][3][term_ranks][32]: of s h
   float *out;                  // [L][rank][width], or with `by_rank` [L][width][rank]
   float *parted;               // [2 ranges] of the same
   int64_t ld, width;
@@ -702,22 +772,27 @@ int64_t divide_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct Layout {
   bool few;
   int64_t tiles;               // at most so many planned tiles
-  int64_t splits_in, splits_out;     // of the sum over inp (h), over out (dh)
+  int64_t steps_in, steps_out, splits_in, splits_out;        // of k_shrink's sums over inp (h), over out (dh)
   int64_t ranges, range_tiles; // of k_outer
   int64_t count, tile_begin, order, table, parts, at, bt, terms_a, terms_b, parted_a, parted_b, bytes;   // byte offsets
 
-  // Splits of a sum so that there are workgroups for the compute units, each with two steps a wave at least
-  static int64_t splits(int64_t tokens, bool few, int64_t width) {
-    const int64_t steps = divide_up(width, kBlock), groups = few ? divide_up(tokens, 4) : divide_up(tokens, kTile);
-    const int64_t want = divide_up(512, groups > 0 ? groups : 1), most = divide_up(steps, 16);
-    const int64_t n = want < most ? want : most;
-    return n < 1 ? 1 : n > 16 ? 16 : n;
+  // Steps of 32 columns that a wave of k_shrink keeps w of in registers: as many as fit (ranks), fewer where there would not be
+  // workgroups for the compute units, but not below two.  The splits of the sum follow.
+  static int64_t shrink_steps(int64_t tokens, bool few, int64_t width, int64_t rank) {
+    const int64_t all = divide_up(width, 32), groups = few ? divide_up(tokens, 4) : divide_up(tokens, 16);
+    int64_t steps = rank <= 64 ? 8 : 4;
+    while (steps > 2 && groups * divide_up(all, steps * kShrinkWaves) < 256) steps /= 2;
+    const int64_t splits = divide_up(all, steps * kShrinkWaves);
+    return divide_up(all, splits * kShrinkWaves);            // evenly
   }
+  static int64_t splits(int64_t steps, int64_t width) { return divide_up(divide_up(width, 32), steps * kShrinkWaves); }
   Layout(const nvfp4_adapters_params &p, bool backward) {
     few = !backward && p.tokens <= kFewTokens;
     tiles = p.tokens / kTile + (p.adapters + 1 < p.tokens ? p.adapters + 1 : p.tokens);
-    splits_in = splits(p.tokens, few, p.inp);
-    splits_out = splits(p.tokens, few, p.out);
+    steps_in = shrink_steps(p.tokens, few, p.inp, p.rank);
+    steps_out = shrink_steps(p.tokens, few, p.out, p.rank);
+    splits_in = splits(steps_in, p.inp);
+    splits_out = splits(steps_out, p.out);
     const int64_t chunks = divide_up(p.inp, kOuterWidth) + divide_up(p.out, kOuterWidth);
     ranges = divide_up(512, chunks);
     range_tiles = divide_up(tiles, ranges);
@@ -771,32 +846,35 @@ int run_plan(const nvfp4_adapters_params &p, const Layout &d, char *w, const int
   return launch(k_plan, dim3((uint32_t)(1 + (g.units < 65536 ? g.units : 65536))), dim3(kPlanThreads), counts > tile ? counts : tile, s, g);
 }
 
-template <bool FEW, int MT, int RT, int W, int D>
-int run_shrink_of(const ShrinkArgs &g, int64_t tiles, int64_t splits, hipStream_t s) {
-  return launch(k_shrink<FEW, MT, RT, W, D>, dim3((uint32_t)tiles, (uint32_t)splits), dim3(W * 64), 0, s, g);
+template <int RT, int NF>
+int run_shrink_of(const ShrinkArgs &g, const Layout &d, int64_t splits, hipStream_t s) {
+  // two workgroups a compute unit where registers allow it
+  const int64_t most = divide_up(RT * NF <= 8 ? 512 : 256, splits), stretches = 2 * d.tiles < most ? 2 * d.tiles : most;
+  return d.few ? launch(k_shrink<true, RT, NF>, dim3((uint32_t)g.tokens.T, (uint32_t)splits), dim3(kShrinkWaves * 64), 0, s, g)
+               : launch(k_shrink<false, RT, NF>, dim3((uint32_t)stretches, (uint32_t)splits), dim3(kShrinkWaves * 64), 0, s, g);
 }
-int run_shrink(ShrinkArgs g, const Layout &d, int64_t splits, hipStream_t s) {
-  g.steps = (int32_t)divide_up(divide_up(g.width, kBlock), splits);
-  if (d.few) {
-    const int64_t tiles = g.tokens.T;
-    if (g.rank <= 16) return run_shrink_of<true, 1, 1, 8, 4>(g, tiles, splits, s);
-    if (g.rank <= 32) return run_shrink_of<true, 1, 2, 8, 3>(g, tiles, splits, s);
-    if (g.rank <= 64) return run_shrink_of<true, 1, 4, 8, 2>(g, tiles, splits, s);
-    return run_shrink_of<true, 1, 8, 4, 2>(g, tiles, splits, s);
-  }
-  if (g.rank <= 16) return run_shrink_of<false, 1, 1, 4, 4>(g, 2 * d.tiles, splits, s);
-  if (g.rank <= 32) return run_shrink_of<false, 2, 2, 4, 3>(g, d.tiles, splits, s);
-  if (g.rank <= 64) return run_shrink_of<false, 2, 4, 4, 2>(g, d.tiles, splits, s);
-  return run_shrink_of<false, 2, 8, 4, 2>(g, d.tiles, splits, s);
+int run_shrink(const ShrinkArgs &g, const Layout &d, int64_t splits, hipStream_t s) {
+  if (g.rank <= 16)
+    return g.steps <= 2 ? run_shrink_of<1, 2>(g, d, splits, s) : g.steps <= 4 ? run_shrink_of<1, 4>(g, d, splits, s)
+                                                                             : run_shrink_of<1, 8>(g, d, splits, s);
+  if (g.rank <= 32)
+    return g.steps <= 2 ? run_shrink_of<2, 2>(g, d, splits, s) : g.steps <= 4 ? run_shrink_of<2, 4>(g, d, splits, s)
+                                                                             : run_shrink_of<2, 8>(g, d, splits, s);
+  if (g.rank <= 64)
+    return g.steps <= 2 ? run_shrink_of<4, 2>(g, d, splits, s) : g.steps <= 4 ? run_shrink_of<4, 4>(g, d, splits, s)
+                                                                             : run_shrink_of<4, 8>(g, d, splits, s);
+  return g.steps <= 2 ? run_shrink_of<8, 2>(g, d, splits, s) : run_shrink_of<8, 4>(g, d, splits, s);
 }
 
 template <typename T, int F>
 int run_expand_of(const ExpandArgs &g, const Layout &d, hipStream_t s) {
-  const int64_t blocks = divide_up(g.width, kBlock * 4), tiles = d.few ? g.tokens.T : d.tiles, want = g.out ? divide_up(2048, tiles) : 1;
-  const dim3 grid((uint32_t)tiles, (uint32_t)(want < blocks ? want : blocks));
-  if (g.pitch % 8)
-    return d.few ? launch(k_expand<true, false, T, 1, F>, grid, dim3(256), 0, s, g) : launch(k_expand<false, false, T, 2, F>, grid, dim3(256), 0, s, g);
-  return d.few ? launch(k_expand<true, true, T, 1, F>, grid, dim3(256), 0, s, g) : launch(k_expand<false, true, T, 2, F>, grid, dim3(256), 0, s, g);
+  if (d.few) {
+    const dim3 grid((uint32_t)g.tokens.T, (uint32_t)divide_up(g.width, kBlock * 4));
+    return launch(g.pitch % 8 ? k_expand<true, false, T, F> : k_expand<true, true, T, F>, grid, dim3(256), 0, s, g);
+  }
+  const int64_t across = g.out ? divide_up(g.width, kBlock * 8) : 1, most = divide_up(F <= 1 ? 2048 : F == 2 ? 1024 : 512, across);
+  const dim3 grid((uint32_t)(d.tiles < most ? d.tiles : most), (uint32_t)across);
+  return launch(g.pitch % 8 ? k_expand<false, false, T, F> : k_expand<false, true, T, F>, grid, dim3(512), 0, s, g);
 }
 template <typename T>
 int run_expand(const ExpandArgs &g, const Layout &d, hipStream_t s) {
@@ -846,6 +924,7 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
   g.width = p->inp;
   g.rank = rank;
   g.pitch = pitch;
+  g.steps = (int32_t)d.steps_in;
   if (const int rc = run_shrink(g, d, d.splits_in, s)) return rc;
   const ExpandArgs e{tokens, parts, d.splits_in == 1 ? nullptr : h, nullptr, static_cast<const __bf16 *>(b), scales, base, out,
                      p->ld_base, p->ld_out, p->out, rank, rank, pitch, (int32_t)d.splits_in, 0};
@@ -881,7 +960,7 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
                       (int32_t)divide_up(p->out, kOuterWidth), true}}};
   if (any) {
     const ShrinkArgs dh{tokens, static_cast<const __bf16 *>(dy), reinterpret_cast<const __bf16 *>(w + d.bt), parts, nullptr, h, scales,
-                        terms_b, p->ld_dy, p->out, rank, pitch, 0, term_ranks};
+                        terms_b, p->ld_dy, p->out, rank, pitch, (int32_t)d.steps_out, term_ranks};
     if (const int rc = run_shrink(dh, d, d.splits_out, s)) return rc;
     const ExpandArgs e{tokens, parts, nullptr, terms_a, reinterpret_cast<const __bf16 *>(w + d.at), scales, dx_base, dx,
                        p->ld_base, p->ld_out, p->inp, rank, pitch, pitch, (int32_t)d.splits_out, term_ranks};
