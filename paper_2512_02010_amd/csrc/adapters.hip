@@ -31,6 +31,7 @@ constexpr int kBlock = 64;                      // columns of a block of k_expan
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -317,10 +318,14 @@ struct Columns {
 // eight ranks: F > 0: 32 ranks of one term, F times.  F == 0, rank <= 16: the one or two pieces of every term side by side.
 // A wave has a block of columns of its own and keeps their part of w in registers while it goes through the workgroup's stretch of the
 // plan; per tile the workgroup sums the parts of s h and splits them once, into LDS, while the tile's columns of base are on their way.
+// Eight waves a workgroup, two workgroups a compute unit, where 128 registers are enough for it; else four waves and three.
+template <bool FEW, typename T, int F>
+constexpr int expand_waves = !FEW && sizeof(T) == 2 && F <= 1 ? 8 : 4;
+
 template <bool FEW, bool WHOLE, typename T, int F>
-__global__ void __launch_bounds__(FEW ? 256 : 512, F < 4 ? 4 : 2) k_expand(ExpandArgs a) {
+__global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, (expand_waves<FEW, T, F>) == 8 ? 4 : F < 4 ? 3 : 2) k_expand(ExpandArgs a) {
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 2, kSpans = F ? F : 1, kProducts = F ? kTerms : kTerms - 1;
-  constexpr int MT = FEW ? 1 : 2, kThreads = FEW ? 256 : 512, kWaves = kThreads / 64, kRows = MT * 16;
+  constexpr int MT = FEW ? 1 : 2, kWaves = expand_waves<FEW, T, F>, kThreads = kWaves * 64, kRows = MT * 16;
   __shared__ TileTokens shared;
   __shared__ bf16x8 split[FEW ? 1 : 2][kRows][kTerms * kSpans * 4 + 1];      // (an odd number of pieces: a row a bank further)
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
@@ -354,29 +359,34 @@ __global__ void __launch_bounds__(FEW ? 256 : 512, F < 4 ? 4 : 2) k_expand(Expan
     if (t.adapter < 0) return;
     const float scale = a.scales[t.adapter];
     const bool mine = FEW ? blockIdx.y == 0 : i % (int32_t)gridDim.y == (int32_t)blockIdx.y;      // whose h or terms it is to write
-    for (int e = threadIdx.x; e < kRows * kSpans * 4; e += kThreads) {
-      const int n = e / (kSpans * 4), piece = e % (kSpans * 4), from = piece * 8;
+    for (int e = threadIdx.x; e < kRows * kSpans * 8; e += kThreads) {          // four ranks of a token each
+      const int n = e / (kSpans * 8), from = e % (kSpans * 8) * 4;
       const int32_t token = token_of(i, n);
-      float v[8] = {};
-      if (token >= 0 && piece < pieces) {
+      f32x4 v{};
+      if (token >= 0 && from < a.h_pitch) {
         const float *const part = a.parts + (int64_t)token * a.h_pitch + from;
-        for (int p = 0; p < a.splits; ++p) {
-          const f32x4 *const q = reinterpret_cast<const f32x4 *>(part + (int64_t)p * a.tokens.T * a.h_pitch);
-          for (int k = 0; k < 8; ++k) v[k] += q[k / 4][k % 4];
+        for (int p0 = 0; p0 < a.splits; p0 += 4) {                  // (four on their way; past the last once more the last)
+          f32x4 q[4];
+          for (int p = 0; p < 4; ++p)
+            q[p] = *reinterpret_cast<const f32x4 *>(part + (int64_t)(p0 + p < a.splits ? p0 + p : a.splits - 1) * a.tokens.T * a.h_pitch);
+          for (int p = 0; p < 4; ++p)
+            if (p0 + p < a.splits) v += q[p];
         }
         if (a.h && mine)
-          for (int k = 0; k < 8; ++k)
+          for (int k = 0; k < 4; ++k)
             if (from + k < a.rank) a.h[(int64_t)token * a.rank + from + k] = v[k];
-        for (int k = 0; k < 8; ++k) v[k] *= scale;
+        v *= scale;
       }
       for (int which = 0; which < kTerms; ++which) {
-        bf16x8 q;
-        for (int k = 0; k < 8; ++k) q[k] = term(v[k], which);
-        split[buffer][n][which * kSpans * 4 + piece] = q;
+        bf16x4 q;
+        for (int k = 0; k < 4; ++k) q[k] = term(v[k], which);
+        reinterpret_cast<bf16x4 *>(&split[buffer][n][which * kSpans * 4])[from / 4] = q;
       }
-      if (a.terms && mine && from < a.term_ranks)
+      if (a.terms && mine && from < a.term_ranks) {
+        __bf16 *const to = a.terms + ((int64_t)i * 3 * a.term_ranks + from) * kTile + n;
         for (int which = 0; which < 3; ++which)
-          for (int k = 0; k < 8; ++k) a.terms[(((int64_t)i * 3 + which) * a.term_ranks + from + k) * kTile + n] = term(v[k], which);
+          for (int k = 0; k < 4; ++k) to[(which * a.term_ranks + k) * kTile] = term(v[k], which);
+      }
     }
   };
 
@@ -392,30 +402,32 @@ __global__ void __launch_bounds__(FEW ? 256 : 512, F < 4 ? 4 : 2) k_expand(Expan
       for (int m = 0; m < MT; ++m)
         for (int half = 0; half < 2; ++half) v[m][half] = {};
   };
-  int buffer = 0;
+  bf16x8 w[4][kSpans];
+  const auto fetch_w = [&](int32_t adapter) {
+    const __bf16 *const of = a.w + (int64_t)adapter * a.width * a.pitch;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int32_t c = c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4;
+#pragma unroll
+      for (int f = 0; f < kSpans; ++f) {
+        const int piece = F ? f * 4 + group : group % pieces;
+        w[p][f] = load_ranks<WHOLE>(of + (int64_t)(c < width ? c : width - 1) * a.pitch, piece < pieces ? piece * 8 : 0, a.rank);
+        if (F && pieces % 4 && piece >= pieces) w[p][f] = bf16x8{};
+      }
+    }
+  };
+  int buffer = 0, i = first;
+  int32_t adapter = -1;
   if (first < last) {
-    if (!idle) fetch(first);
+    adapter = tile_of(first).adapter;
+    if (!idle) {
+      fetch(first);
+      if (adapter >= 0) fetch_w(adapter);
+    }
     prepare(first, 0);
   }
   __syncthreads();
-  int32_t i = first;
-  while (i < last) {                             // one adapter after the other
-    const int32_t adapter = tile_of(i).adapter;
-    if (adapter < 0) break;
-    bf16x8 w[4][kSpans];
-    if (!idle) {
-      const __bf16 *const of = a.w + (int64_t)adapter * a.width * a.pitch;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const int32_t c = c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4;
-#pragma unroll
-        for (int f = 0; f < kSpans; ++f) {
-          const int piece = F ? f * 4 + group : group % pieces;
-          w[p][f] = load_ranks<WHOLE>(of + (int64_t)(c < width ? c : width - 1) * a.pitch, piece < pieces ? piece * 8 : 0, a.rank);
-          if (F && pieces % 4 && piece >= pieces) w[p][f] = bf16x8{};
-        }
-      }
-    }
+  while (i < last && adapter >= 0) {             // one adapter after the other
     for (; i < last && tile_of(i).adapter == adapter; ++i) {
       if (!idle) {
         f32x4 acc[MT][4] = {};
@@ -447,6 +459,10 @@ __global__ void __launch_bounds__(FEW ? 256 : 512, F < 4 ? 4 : 2) k_expand(Expan
       if (i + 1 < last) prepare(i + 1, FEW ? 0 : buffer ^ 1);
       if (!FEW) __syncthreads();                 // (each buffer is written again a barrier after it was read)
       buffer ^= 1;
+    }
+    if (i < last) {
+      adapter = tile_of(i).adapter;
+      if (adapter >= 0 && !idle) fetch_w(adapter);
     }
   }
   // Tokens without an adapter come last.
@@ -506,25 +522,40 @@ __device__ inline void plan_tokens(const PlanArgs &p) {
         for (int i = 0; i < kAhead; ++i) {
           const int32_t t = t0 + i * 64 + lane;
           group[i] = t < end ? p.which[t] : 0;
+          // (past the end: a group of its own, which nobody reads)
+          group[i] = t >= end ? groups : group[i] >= 0 && group[i] < p.L ? group[i] : p.L;
         }
       }
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int32_t t = t0 + i * 64 + lane;
-        // (past the end: a group of its own, which nobody reads)
-        const int32_t l = t >= end ? groups : group[i] >= 0 && group[i] < p.L ? group[i] : p.L;
-        if (t0 + i * 64 >= end) break;
-        const uint64_t m = alike(l);
-        const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1));
+      for (int i0 = 0; i0 < kAhead; i0 += 4) {
+        if (t0 + i0 * 64 >= end) break;
         // A wave's LDS instructions run in their order, so the lanes have all read before the first of each group adds; the fences keep
         // the compiler to it.
-        if (pass == 1) {
-          const int32_t at = mine[l];
+        const int32_t one = __builtin_amdgcn_readfirstlane(group[i0]);
+        if (__ballot(group[i0] == one && group[i0 + 1] == one && group[i0 + 2] == one && group[i0 + 3] == one) == ~(uint64_t)0) {
+          if (pass == 1) {                       // requests one after the other: nearly always
+            int32_t *const to = p.plan.order + (int64_t)tile_begin[one] * kTile + mine[one] + lane;
+            for (int i = 0; i < 4; ++i) to[i * 64] = t0 + (i0 + i) * 64 + lane;
+          }
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          if (t < end) p.plan.order[(int64_t)tile_begin[l] * kTile + at + before] = t;
+          if (lane == 0) __hip_atomic_fetch_add(mine + one, 256, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          continue;
         }
-        if (before == 0) __hip_atomic_fetch_add(mine + l, __popcll(m), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int i = i0; i < i0 + 4; ++i) {
+          const int32_t t = t0 + i * 64 + lane, l = group[i];
+          if (t0 + i * 64 >= end) break;
+          const uint64_t m = alike(l);
+          const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1));
+          if (pass == 1) {
+            const int32_t at = mine[l];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (t < end) p.plan.order[(int64_t)tile_begin[l] * kTile + at + before] = t;
+          }
+          if (before == 0) __hip_atomic_fetch_add(mine + l, __popcll(m), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
       }
     }
     __syncthreads();
@@ -781,7 +812,7 @@ struct Layout {
   static int64_t shrink_steps(int64_t tokens, bool few, int64_t width, int64_t rank) {
     const int64_t all = divide_up(width, 32), groups = few ? divide_up(tokens, 4) : divide_up(tokens, 16);
     int64_t steps = rank <= 64 ? 8 : 4;
-    while (steps > 2 && groups * divide_up(all, steps * kShrinkWaves) < 256) steps /= 2;
+    while (steps > 2 && groups * divide_up(all, steps * kShrinkWaves) < 128) steps /= 2;
     const int64_t splits = divide_up(all, steps * kShrinkWaves);
     return divide_up(all, splits * kShrinkWaves);            // evenly
   }
@@ -872,9 +903,10 @@ int run_expand_of(const ExpandArgs &g, const Layout &d, hipStream_t s) {
     const dim3 grid((uint32_t)g.tokens.T, (uint32_t)divide_up(g.width, kBlock * 4));
     return launch(g.pitch % 8 ? k_expand<true, false, T, F> : k_expand<true, true, T, F>, grid, dim3(256), 0, s, g);
   }
-  const int64_t across = g.out ? divide_up(g.width, kBlock * 8) : 1, most = divide_up(F <= 1 ? 2048 : F == 2 ? 1024 : 512, across);
+  constexpr int kWaves = expand_waves<false, T, F>;
+  const int64_t across = g.out ? divide_up(g.width, kBlock * kWaves) : 1, most = divide_up(F <= 1 ? 2048 : F == 2 ? 1536 : 1024, across);
   const dim3 grid((uint32_t)(d.tiles < most ? d.tiles : most), (uint32_t)across);
-  return launch(g.pitch % 8 ? k_expand<false, false, T, F> : k_expand<false, true, T, F>, grid, dim3(512), 0, s, g);
+  return launch(g.pitch % 8 ? k_expand<false, false, T, F> : k_expand<false, true, T, F>, grid, dim3(kWaves * 64), 0, s, g);
 }
 template <typename T>
 int run_expand(const ExpandArgs &g, const Layout &d, hipStream_t s) {
