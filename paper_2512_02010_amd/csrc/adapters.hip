@@ -47,6 +47,14 @@ struct Plan {
   int32_t *order;                               // [tiles][32]: their tokens, -1 past a tile's last
 };
 
+// A workgroup's stretch of `units` (tiles, or halves of them).  Where there is a workgroup for each that there can be, it is known before
+// the plan's count has been read.
+__device__ inline void stretch(const Plan &plan, int32_t per_tile, bool single, int32_t &first, int32_t &last) {
+  const int32_t all = per_tile * *plan.count, per = single ? 1 : (all + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
+  first = (int32_t)blockIdx.x * per;
+  last = first + per < all ? first + per : all;
+}
+
 // Where tiles come from: a plan, or (few tokens) `which` itself.
 struct Tokens {
   const int32_t *which;
@@ -143,7 +151,8 @@ struct ShrinkArgs {
   int64_t ld, width;
   int32_t rank, pitch;
   int32_t steps;               // 32 columns each, of a wave: at most NF
-  int32_t term_ranks;
+  int32_t term_ranks, splits;
+  bool single;                 // a workgroup for every 16 tokens
 };
 
 constexpr int kShrinkWaves = 8;
@@ -157,19 +166,21 @@ __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shr
   __shared__ TileTokens shared;
   __shared__ float part[kBuffers][kShrinkWaves][RT * 256];
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
-  int32_t first = 0, last = 1;                   // 16 tokens each
+  int32_t first = 0, last = 1, token = 0;        // 16 tokens each
   Tile only{};
   if constexpr (FEW) {
     only = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, 16);
     if (only.count == 0) return;
   } else {
-    const int32_t all = 2 * *a.tokens.plan.count, per = (all + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
-    first = (int32_t)blockIdx.x * per;
-    last = first + per < all ? first + per : all;
+    if (a.single) {                              // asked for together with the count
+      only = a.tokens.plan.tiles[blockIdx.x / 2];
+      token = a.tokens.plan.order[(int64_t)blockIdx.x * 16 + row];
+    }
+    stretch(a.tokens.plan, 2, a.single, first, last);
   }
   const auto tile_of = [&](int32_t i) {          // the 16 tokens i
     if constexpr (FEW) return only;
-    Tile t = a.tokens.plan.tiles[i / 2];
+    Tile t = a.single ? only : a.tokens.plan.tiles[i / 2];
     t.count -= i % 2 * 16;
     if (t.count > 16) t.count = 16;
     return t;
@@ -192,11 +203,27 @@ __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shr
     for (int f = 0; f < NF; ++f)
       if (f >= mine || c0 + f * 32 >= width) to[f] = bf16x8{};
   };
+  if constexpr (!FEW) {
+    if ((int32_t)blockIdx.y == a.splits) {       // backwards there is one more row of workgroups, for the terms of h
+      for (int32_t tile = (first + 1) / 2; tile < (last + 1) / 2; ++tile) {       // those that begin in this stretch
+        const int32_t l = a.tokens.plan.tiles[tile].adapter;
+        if (l < 0) break;
+        for (int e = threadIdx.x; e < kTile * a.term_ranks; e += kThreads) {
+          const int n = e % kTile, rank = e / kTile;
+          const int32_t of = a.tokens.plan.order[(int64_t)tile * kTile + n];
+          const bool is = of >= 0 && rank < a.rank;
+          const float h = a.terms_of[(int64_t)(is ? of : 0) * a.rank + (is ? rank : 0)], v = is ? a.scales[l] * h : 0.0f;
+          for (int which = 0; which < 3; ++which) a.terms[(((int64_t)tile * 3 + which) * a.term_ranks + rank) * kTile + n] = term(v, which);
+        }
+      }
+      return;
+    }
+  }
   const auto row_of = [&](int32_t token) { return a.x + (int64_t)(token < 0 ? 0 : token) * a.ld; };
   bf16x8 w[RT][NF], x[NF];
-  int32_t token = 0, buffer = 0;
+  int32_t buffer = 0;
   if (first < last) {
-    fetch(x, row_of(token_of(first, row)));
+    fetch(x, row_of(!FEW && a.single ? token : token_of(first, row)));
     if (first + 1 < last) token = token_of(first + 1, row);
   }
   for (int32_t i = first; i < last;) {           // one adapter after the other
@@ -211,6 +238,7 @@ __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shr
     for (; i < last; ++i) {
       const Tile t = tile_of(i);
       if (t.adapter != adapter) break;
+      const int32_t to = token_of(i, threadIdx.x % 256 / 16);         // (where this thread's sums go, the same for all of them)
       clear(x);
       f32x4 acc[RT] = {};
 #pragma unroll
@@ -232,8 +260,7 @@ __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shr
         for (int v = 0; v < 4; ++v) p[wave][r * 256 + (group * 4 + v) * 16 + row] = acc[r][v];
       __syncthreads();
       for (int e = threadIdx.x; e < RT * 256; e += kThreads) {
-        const int n = e % 256 / 16, rank = e / 256 * 16 + e % 16;
-        const int32_t to = token_of(i, n);
+        const int rank = e / 256 * 16 + e % 16;
         float s = 0.0f;
         for (int k = 0; k < kShrinkWaves; ++k) s += p[k][e];
         if (to >= 0 && rank < a.pitch) {
@@ -247,18 +274,6 @@ __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shr
     for (int32_t i = last; i-- > first && tile_of(i).adapter < 0;)
       for (int e = threadIdx.x; e < tile_of(i).count * a.rank; e += kThreads)
         a.h[(int64_t)token_of(i, e / a.rank) * a.rank + e % a.rank] = 0.0f;
-  if (FEW || !a.terms_of || blockIdx.y != 0) return;
-  for (int32_t tile = (first + 1) / 2; tile < (last + 1) / 2; ++tile) {             // those that begin in this stretch
-    const int32_t l = a.tokens.plan.tiles[tile].adapter;
-    if (l < 0) break;
-    for (int e = threadIdx.x; e < kTile * a.term_ranks; e += kThreads) {
-      const int n = e % kTile, rank = e / kTile;
-      const int32_t of = a.tokens.plan.order[(int64_t)tile * kTile + n];
-      const bool is = of >= 0 && rank < a.rank;
-      const float h = a.terms_of[(int64_t)(is ? of : 0) * a.rank + (is ? rank : 0)], v = is ? a.scales[l] * h : 0.0f;
-      for (int which = 0; which < 3; ++which) a.terms[(((int64_t)tile * 3 + which) * a.term_ranks + rank) * kTile + n] = term(v, which);
-    }
-  }
 }
 
 // ---- k_expand ---------------------------------------------------------------------------------------------------------
@@ -274,6 +289,7 @@ struct ExpandArgs {
   void *out;                   // nullptr: only the terms
   int64_t ld_base, ld_out, width;
   int32_t rank, pitch, h_pitch, splits, term_ranks;
+  bool single;                 // a workgroup for every tile
 };
 
 // Eight ranks of a row of w, from `first`; where rows are not WHOLE pieces of 16 bytes, one by one.
@@ -320,28 +336,30 @@ struct Columns {
 // plan; per tile the workgroup sums the parts of s h and splits them once, into LDS, while the tile's columns of base are on their way.
 // Eight waves a workgroup, two workgroups a compute unit, where 128 registers are enough for it; else four waves and three.
 template <bool FEW, typename T, int F>
-constexpr int expand_waves = !FEW && sizeof(T) == 2 && F <= 1 ? 8 : 4;
+constexpr int expand_waves = !FEW && sizeof(T) == 2 ? 8 : 4;
 
 template <bool FEW, bool WHOLE, typename T, int F>
-__global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, (expand_waves<FEW, T, F>) == 8 ? 4 : F < 4 ? 3 : 2) k_expand(ExpandArgs a) {
+__global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (expand_waves<FEW, T, F>) == 8 ? 4 : 3) k_expand(ExpandArgs a) {
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 2, kSpans = F ? F : 1, kProducts = F ? kTerms : kTerms - 1;
   constexpr int MT = FEW ? 1 : 2, kWaves = expand_waves<FEW, T, F>, kThreads = kWaves * 64, kRows = MT * 16;
   __shared__ TileTokens shared;
   __shared__ bf16x8 split[FEW ? 1 : 2][kRows][kTerms * kSpans * 4 + 1];      // (an odd number of pieces: a row a bank further)
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
-  int32_t first = 0, last = 1;
+  int32_t first = 0, last = 1, in[MT];           // in: this lane's token of each 16, -1: there is none
   Tile only{};
   if constexpr (FEW) {
     only = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, kRows);
     if (only.count == 0) return;
   } else {
-    const int32_t all = *a.tokens.plan.count, per = (all + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
-    first = (int32_t)blockIdx.x * per;
-    last = first + per < all ? first + per : all;
+    if (a.single) {                              // asked for together with the count
+      only = a.tokens.plan.tiles[blockIdx.x];
+      for (int m = 0; m < MT; ++m) in[m] = a.tokens.plan.order[(int64_t)blockIdx.x * kRows + m * 16 + row];
+    }
+    stretch(a.tokens.plan, 1, a.single, first, last);
   }
   const auto tile_of = [&](int32_t i) {
     if constexpr (FEW) return only;
-    return a.tokens.plan.tiles[i];
+    return a.single ? only : a.tokens.plan.tiles[i];
   };
   const auto token_of = [&](int32_t i, int n) -> int32_t {       // -1: there is none
     if constexpr (FEW) return n < only.count ? shared.token[n] : -1;
@@ -390,10 +408,10 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, (expand_waves<FE
     }
   };
 
-  int32_t in[MT];                                // this lane's token of each 16, -1: there is none
   Columns<T> v[MT][2] = {};                      // (without a base 0)
   const auto fetch = [&](int32_t i) {            // (rows and columns that there are not: others, which are not kept)
-    for (int m = 0; m < MT; ++m) in[m] = token_of(i, m * 16 + row);
+    if (FEW || !a.single)
+      for (int m = 0; m < MT; ++m) in[m] = token_of(i, m * 16 + row);
     if (base)
       for (int m = 0; m < MT; ++m)
         for (int half = 0; half < 2; ++half)
@@ -878,11 +896,15 @@ int run_plan(const nvfp4_adapters_params &p, const Layout &d, char *w, const int
 }
 
 template <int RT, int NF>
-int run_shrink_of(const ShrinkArgs &g, const Layout &d, int64_t splits, hipStream_t s) {
+int run_shrink_of(ShrinkArgs g, const Layout &d, int64_t splits, hipStream_t s) {
+  g.splits = (int32_t)splits;
+  if (d.few)
+    return launch(k_shrink<true, RT, NF>, dim3((uint32_t)g.tokens.T, (uint32_t)splits), dim3(kShrinkWaves * 64), 0, s, g);
   // two workgroups a compute unit where registers allow it
-  const int64_t most = divide_up(RT * NF <= 8 ? 512 : 256, splits), stretches = 2 * d.tiles < most ? 2 * d.tiles : most;
-  return d.few ? launch(k_shrink<true, RT, NF>, dim3((uint32_t)g.tokens.T, (uint32_t)splits), dim3(kShrinkWaves * 64), 0, s, g)
-               : launch(k_shrink<false, RT, NF>, dim3((uint32_t)stretches, (uint32_t)splits), dim3(kShrinkWaves * 64), 0, s, g);
+  const int64_t most = divide_up(RT * NF <= 8 ? 512 : 256, splits);
+  g.single = 2 * d.tiles <= most;
+  const dim3 grid((uint32_t)(g.single ? 2 * d.tiles : most), (uint32_t)(splits + (g.terms_of ? 1 : 0)));
+  return launch(k_shrink<false, RT, NF>, grid, dim3(kShrinkWaves * 64), 0, s, g);
 }
 int run_shrink(const ShrinkArgs &g, const Layout &d, int64_t splits, hipStream_t s) {
   if (g.rank <= 16)
@@ -898,14 +920,16 @@ int run_shrink(const ShrinkArgs &g, const Layout &d, int64_t splits, hipStream_t
 }
 
 template <typename T, int F>
-int run_expand_of(const ExpandArgs &g, const Layout &d, hipStream_t s) {
+int run_expand_of(ExpandArgs g, const Layout &d, hipStream_t s) {
   if (d.few) {
     const dim3 grid((uint32_t)g.tokens.T, (uint32_t)divide_up(g.width, kBlock * 4));
     return launch(g.pitch % 8 ? k_expand<true, false, T, F> : k_expand<true, true, T, F>, grid, dim3(256), 0, s, g);
   }
   constexpr int kWaves = expand_waves<false, T, F>;
-  const int64_t across = g.out ? divide_up(g.width, kBlock * kWaves) : 1, most = divide_up(F <= 1 ? 2048 : F == 2 ? 1536 : 1024, across);
-  const dim3 grid((uint32_t)(d.tiles < most ? d.tiles : most), (uint32_t)across);
+  const int64_t across = g.out ? divide_up(g.width, kBlock * kWaves) : 1;
+  const int64_t most = divide_up(F <= 1 ? 2048 : (F == 2 ? 1024 : 512) * (sizeof(T) == 4 ? 2 : 1), across);
+  g.single = d.tiles <= most;
+  const dim3 grid((uint32_t)(g.single ? d.tiles : most), (uint32_t)across);
   return launch(g.pitch % 8 ? k_expand<false, false, T, F> : k_expand<false, true, T, F>, grid, dim3(kWaves * 64), 0, s, g);
 }
 template <typename T>
@@ -959,7 +983,7 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
   g.steps = (int32_t)d.steps_in;
   if (const int rc = run_shrink(g, d, d.splits_in, s)) return rc;
   const ExpandArgs e{tokens, parts, d.splits_in == 1 ? nullptr : h, nullptr, static_cast<const __bf16 *>(b), scales, base, out,
-                     p->ld_base, p->ld_out, p->out, rank, rank, pitch, (int32_t)d.splits_in, 0};
+                     p->ld_base, p->ld_out, p->out, rank, rank, pitch, (int32_t)d.splits_in, 0, false};
   return p->out_dtype == NVFP4_OUT_F32 ? run_expand<float>(e, d, s) : run_expand<__bf16>(e, d, s);
 }
 
@@ -992,10 +1016,10 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
                       (int32_t)divide_up(p->out, kOuterWidth), true}}};
   if (any) {
     const ShrinkArgs dh{tokens, static_cast<const __bf16 *>(dy), reinterpret_cast<const __bf16 *>(w + d.bt), parts, nullptr, h, scales,
-                        terms_b, p->ld_dy, p->out, rank, pitch, (int32_t)d.steps_out, term_ranks};
+                        terms_b, p->ld_dy, p->out, rank, pitch, (int32_t)d.steps_out, term_ranks, 0, false};
     if (const int rc = run_shrink(dh, d, d.splits_out, s)) return rc;
     const ExpandArgs e{tokens, parts, nullptr, terms_a, reinterpret_cast<const __bf16 *>(w + d.at), scales, dx_base, dx,
-                       p->ld_base, p->ld_out, p->inp, rank, pitch, pitch, (int32_t)d.splits_out, term_ranks};
+                       p->ld_base, p->ld_out, p->inp, rank, pitch, pitch, (int32_t)d.splits_out, term_ranks, false};
     if (const int rc = run_expand<__bf16>(e, d, s)) return rc;
     const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, rank <= 64 ? 1 : 2);
     if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
