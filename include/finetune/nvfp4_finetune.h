@@ -93,7 +93,7 @@ enum { NVFP4_INDEX_I32 = 0, NVFP4_INDEX_I64 = 1 };
 
 typedef struct {
   int64_t rows;            /* tokens, 0 .. 2^21                                                                */
-  int64_t vocab;           /* logits of a row, 1 .. 2^31 - 16                                                  */
+  int64_t vocab;           /* logits of a row, 1 .. 2^29                                                       */
   int64_t ld;              /* elements from row to row of logits and dlogits, at least vocab, any alignment     */
   int64_t top;             /* entries of a list, 1 .. 1024                                                     */
   float temperature;       /* finite, > 0                                                                      */

@@ -35,23 +35,8 @@ struct DistillArgs {
 };
 
 // ---- rows in pieces of 16 bytes --------------------------------------------------------------------------------
-// A row begins anywhere (its length may be odd): pieces are cut at multiples of 16 bytes of the address, and the first and last
-// piece hold elements of this row only, one by one.
-
-template <typename T>
-struct Row {
-  static constexpr int kPer = 16 / sizeof(T);
-  char *at;                    // the first piece
-  int32_t off, end;            // this row's elements are [off, end) counted from there
-  __device__ Row(const void *base, int64_t row, int64_t ld, int32_t vocab) {
-    const char *p = static_cast<const char *>(base) + row * ld * (int64_t)sizeof(T);
-    off = (int32_t)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
-    at = const_cast<char *>(p) - off * sizeof(T);
-    end = off + vocab;         // (vocab < 2^31 - 8 by the host's check)
-  }
-  __device__ int32_t pieces() const { return (end + kPer - 1) / kPer; }
-  __device__ bool whole(int32_t v) const { return v * kPer >= off && (v + 1) * kPer <= end; }
-};
+// A row begins anywhere (its length may be odd): pieces are cut at multiples of 16 bytes of the address.  What lies before the first and
+// after the last whole piece, fewer than a piece's elements each, are the row's edges: a thread takes one of them by itself.
 
 __device__ inline float up(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
 
@@ -85,28 +70,31 @@ __device__ inline void set_element(void *p, int64_t i, float x) {
   else
     static_cast<__bf16 *>(p)[i] = (__bf16)x;
 }
-// Piece v; elements of other rows come as -inf, whose exponential is 0.
+
 template <typename T>
-__device__ inline u32x4 load_piece(const Row<T> &r, int32_t v) {
-  if (r.whole(v)) return *reinterpret_cast<const u32x4 *>(r.at + (int64_t)v * 16);
-  float x[Row<T>::kPer];
-  for (int i = 0; i < Row<T>::kPer; ++i) {
-    const int32_t e = v * Row<T>::kPer + i;
-    x[i] = e >= r.off && e < r.end ? element<T>(r.at, e) : -kInf;
+struct Row {
+  static constexpr int kPer = 16 / sizeof(T);
+  char *at;                    // the first whole piece
+  int32_t pieces;              // whole ones
+  int32_t before, after;       // elements on either edge
+  __device__ Row(const void *base, int64_t row, int64_t ld, int32_t vocab) {
+    const char *p = static_cast<const char *>(base) + row * ld * (int64_t)sizeof(T);
+    before = (int32_t)((-reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    if (before > vocab) before = vocab;
+    pieces = (vocab - before) / kPer;
+    after = vocab - before - pieces * kPer;
+    at = const_cast<char *>(p) + before * (int64_t)sizeof(T);
   }
-  return pack<T>(x);
-}
-template <typename T>
-__device__ inline void store_piece(const Row<T> &r, int32_t v, const float *x) {
-  if (r.whole(v)) {
-    *reinterpret_cast<u32x4 *>(r.at + (int64_t)v * 16) = pack<T>(x);
-    return;
+  // (a row's bytes fit 32 bits, which leaves an address one register a thread)
+  __device__ u32x4 load(int32_t v) const { return *reinterpret_cast<const u32x4 *>(at + (uint32_t)v * 16u); }
+  __device__ void store(int32_t v, const float *x) const { *reinterpret_cast<u32x4 *>(at + (uint32_t)v * 16u) = pack<T>(x); }
+  // The edge element of a thread, counted from the first whole piece; kNoEdge: it has none.
+  static constexpr int64_t kNoEdge = INT64_MIN;
+  __device__ int64_t edge(int32_t thread) const {
+    if (thread < before) return thread - before;
+    return thread >= kPer && thread - kPer < after ? (int64_t)pieces * kPer + thread - kPer : kNoEdge;
   }
-  for (int i = 0; i < Row<T>::kPer; ++i) {
-    const int32_t e = v * Row<T>::kPer + i;
-    if (e >= r.off && e < r.end) set_element<T>(r.at, e, x[i]);
-  }
-}
+};
 
 // ---- maximum and sum together ---------------------------------------------------------------------------------------
 
@@ -144,19 +132,43 @@ __device__ inline Running wave_join(Running r, float c) {
 
 // ---- the list ---------------------------------------------------------------------------------------------------------
 
+// In dynamic LDS, as long as the list is (list_bytes).
 struct List {
-  float p[kMostTop], log_p[kMostTop], z[kMostTop];     // the teacher's probability, its logarithm, the logit itself
-  int32_t index[kMostTop];                             // -1: no entry
-  int32_t any;
+  float *p, *log_p, *z;        // the teacher's probability, its logarithm, the logit itself
+  int32_t *index;              // -1: no entry
+  int32_t *table;              // 2^bits, at least twice the entries: to find words that stand twice in
+  int32_t *any, *twice;        // there is an entry; there are two of one word
+  int bits;
+  // (`which`: the first or the second)
+  __device__ explicit List(int32_t top, int which = 0) {
+    extern __shared__ float space[];
+    bits = 32 - __clz(2 * top - 1);
+    if (bits < 6) bits = 6;
+    p = space + which * (4 * top + 2 + (1 << bits));
+    log_p = p + top;
+    z = log_p + top;
+    index = reinterpret_cast<int32_t *>(z + top);
+    any = index + top;
+    twice = any + 1;
+    table = twice + 1;
+  }
 };
+size_t list_bytes(int64_t top) {
+  int64_t table = 64;
+  while (table < 2 * top) table *= 2;
+  return (size_t)(4 * top + 2 + table) * 4;
+}
 
-// By the first wave, each lane its own entries (nothing to wait for in between); z only where it is asked for.
+// By the first wave, each lane its own entries (nothing to wait for in between).  Logits and words that stand twice are asked for among
+// the words [first, last).
 template <typename T>
-__device__ inline void read_list(List &l, const DistillArgs &a, int64_t row, bool want_z) {
+__device__ inline void read_list(const List &l, const DistillArgs &a, int64_t row, int64_t first, int64_t last) {
   const int lane = threadIdx.x & 63;
   const void *logits = static_cast<const char *>(a.logits) + row * a.ld * (int64_t)sizeof(T);
+  for (int j = lane; j < 1 << l.bits; j += 64) l.table[j] = -1;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   float m = -kInf;
-  bool any = false;
+  bool any = false, twice = false;
   for (int j = lane; j < a.top; j += 64) {
     const int64_t e = row * a.top + j;
     const int64_t i = a.index_wide ? static_cast<const int64_t *>(a.index)[e] : static_cast<const int32_t *>(a.index)[e];
@@ -166,7 +178,15 @@ __device__ inline void read_list(List &l, const DistillArgs &a, int64_t row, boo
     l.log_p[j] = t;
     if (entry) m = fmaxf(m, t);
     any |= entry;
-    if (want_z) l.z[j] = entry ? element<T>(logits, i) : 0.0f;
+    if (entry && i >= first && i < last) {
+      l.z[j] = element<T>(logits, i);
+      uint32_t h = (uint32_t)i * 0x9E3779B1u >> (32 - l.bits);
+      for (;; h = (h + 1) & ((1u << l.bits) - 1)) {      // (at least half of the table stays free)
+        const int32_t there = atomicCAS(&l.table[h], -1, (int32_t)i);
+        twice |= there == (int32_t)i;
+        if (there == -1 || there == (int32_t)i) break;
+      }
+    }
   }
   m = wave_max(m);
   float s = 0.0f;
@@ -181,10 +201,10 @@ __device__ inline void read_list(List &l, const DistillArgs &a, int64_t row, boo
     l.p[j] = l.index[j] < 0 ? 0.0f : l.p[j] * inv_s;
     l.log_p[j] = (l.log_p[j] - m) * a.inv_t - log_s;
   }
-  if (__ballot(any) != 0) {
-    if (lane == 0) l.any = 1;
-  } else if (lane == 0) {
-    l.any = 0;
+  const bool some = __ballot(any) != 0, two = __ballot(twice) != 0;
+  if (lane == 0) {
+    *l.any = some;
+    *l.twice = two;
   }
 }
 // By the first wave.
@@ -195,74 +215,81 @@ __device__ inline float list_loss(const List &l, const DistillArgs &a, float lse
   return wave_sum(s);
 }
 
+// exp(z / temperature - lse)
+__device__ inline float probability(float z, float inv_t, float lse) {
+  constexpr float kLog2e = 1.44269504088896340736f;
+  return __builtin_amdgcn_exp2f(fmaf(z, inv_t, -lse) * kLog2e);
+}
+// The places of the list among the words [first, last) of a row are written again, after what stands there now: the caller has the
+// workgroup's stores and the list behind a barrier.  `probability_of` is that of the other words.
+template <typename T, int NT, typename P>
+__device__ inline void rewrite_list(const List &l, const DistillArgs &a, int64_t row, int64_t first, int64_t last, float g, P &&probability_of) {
+  if (!*l.any) return;
+  char *const d = static_cast<char *>(a.dlogits) + row * a.ld * (int64_t)sizeof(T);
+  for (int j = threadIdx.x; j < a.top; j += NT) {
+    const int32_t at = l.index[j];
+    if (at < first || at >= last) continue;
+    float p = l.p[j];
+    if (*l.twice) {
+      p = 0.0f;
+      for (int k = 0; k < a.top; ++k) p += l.index[k] == at ? l.p[k] : 0.0f;
+    }
+    set_element<T>(d, at, g * (probability_of(l.z[j]) - p));
+  }
+}
+
 // ---- whole workgroups -----------------------------------------------------------------------------------------------
 
 template <int NT>
 struct Scratch {
-  List list;
   float m[NT / 64], s[NT / 64];
 };
 
+// The waves' sums together; one barrier.
+template <int NT>
+__device__ inline Running join_waves(float *m, float *s, Running run, float c) {
+  run = wave_join(run, c);
+  if ((threadIdx.x & 63) == 0) {
+    m[threadIdx.x / 64] = run.m;
+    s[threadIdx.x / 64] = run.s;
+  }
+  __syncthreads();
+  run = {};
+  for (int i = 0; i < NT / 64; ++i) run = join(run, {m[i], s[i]}, c);
+  return run;
+}
 template <typename T, int NT>
 __device__ inline Running row_sum(Scratch<NT> &sh, const Row<T> &r, float c) {
   constexpr int kAhead = 4, kPer = Row<T>::kPer;
   Running run;
-  for (int32_t v0 = threadIdx.x; v0 < r.pieces(); v0 += NT * kAhead) {
+  for (int32_t v0 = threadIdx.x; v0 < r.pieces; v0 += NT * kAhead) {
     u32x4 w[kAhead];
-    for (int i = 0; i < kAhead; ++i)
-      if (v0 + i * NT < r.pieces()) w[i] = load_piece(r, v0 + i * NT);
+    for (int i = 0; i < kAhead; ++i) w[i] = r.load(v0 + i * NT < r.pieces ? v0 + i * NT : r.pieces - 1);
     float x[kAhead * kPer];
     for (int i = 0; i < kAhead; ++i) {
       unpack<T>(w[i], x + i * kPer);
-      if (v0 + i * NT >= r.pieces())
+      if (v0 + i * NT >= r.pieces)
         for (int k = 0; k < kPer; ++k) x[i * kPer + k] = -kInf;
     }
     add<kAhead * kPer>(run, x, c);
   }
-  run = wave_join(run, c);
-  if ((threadIdx.x & 63) == 0) {
-    sh.m[threadIdx.x / 64] = run.m;
-    sh.s[threadIdx.x / 64] = run.s;
+  if (const int64_t e = r.edge(threadIdx.x); e != Row<T>::kNoEdge) {
+    const float x = element<T>(r.at, e);
+    add<1>(run, &x, c);
   }
-  __syncthreads();
-  run = {};
-  for (int i = 0; i < NT / 64; ++i) run = join(run, {sh.m[i], sh.s[i]}, c);
-  return run;
+  return join_waves<NT>(sh.m, sh.s, run, c);
 }
 __device__ inline float lse_of(Running r, float inv_t) { return r.m * inv_t + logf(r.s); }
-
-// The gradient of pieces [first, last), then of the list's places among them.
-template <typename T, int NT>
-__device__ inline void gradient(const List &l, const DistillArgs &a, int64_t row, int32_t first, int32_t last, float lse) {
-  constexpr int kPer = Row<T>::kPer;
-  const Row<T> r(a.logits, row, a.ld, a.vocab), d(a.dlogits, row, a.ld, a.vocab);
-  const float g = a.weight ? a.weight[row] * a.inv_t : a.inv_t;
-  constexpr float kLog2e = 1.44269504088896340736f;
-  for (int32_t v = first + threadIdx.x; v < last; v += NT) {
-    float x[kPer];
-    unpack<T>(load_piece(r, v), x);
-    for (int i = 0; i < kPer; ++i) x[i] = l.any ? g * __builtin_amdgcn_exp2f((x[i] * a.inv_t - lse) * kLog2e) : 0.0f;
-    store_piece(d, v, x);
-  }
-  __syncthreads();             // the places of the list are written again, after what stands there now
-  if (!l.any) return;
-  for (int j = threadIdx.x; j < a.top; j += NT) {
-    const int32_t at = l.index[j], v = (at + r.off) / kPer;
-    if (at < 0 || v < first || v >= last) continue;
-    float p = 0.0f;
-    for (int k = 0; k < a.top; ++k) p += l.index[k] == at ? l.p[k] : 0.0f;
-    set_element<T>(d.at, at + r.off, g * (__builtin_amdgcn_exp2f((l.z[j] * a.inv_t - lse) * kLog2e) - p));
-  }
-}
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) k_distill_forward(DistillArgs a) {
   __shared__ Scratch<NT> sh;
+  const List list(a.top);
   const int64_t row = blockIdx.x;
-  if (threadIdx.x < 64) read_list<T>(sh.list, a, row, true);
+  if (threadIdx.x < 64) read_list<T>(list, a, row, 0, a.vocab);
   const float lse = lse_of(row_sum<T, NT>(sh, Row<T>(a.logits, row, a.ld, a.vocab), a.c), a.inv_t);
   if (threadIdx.x < 64) {
-    const float loss = sh.list.any ? list_loss(sh.list, a, lse) : 0.0f;
+    const float loss = *list.any ? list_loss(list, a, lse) : 0.0f;
     if (threadIdx.x == 0) {
       a.loss[row] = loss;
       if (a.lse) a.lse[row] = lse;
@@ -270,28 +297,134 @@ __global__ void __launch_bounds__(NT) k_distill_forward(DistillArgs a) {
   }
 }
 
+// `per` pieces of a row for a workgroup.
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT) k_distill_backward(DistillArgs a, int32_t pieces) {
-  __shared__ List list;
+__global__ void __launch_bounds__(NT) k_distill_backward(DistillArgs a, int32_t per) {
+  constexpr int kAhead = 4, kPer = Row<T>::kPer;
+  const List list(a.top);
   const int64_t row = blockIdx.x;
-  if (threadIdx.x < 64) read_list<T>(list, a, row, true);
+  const Row<T> r(a.logits, row, a.ld, a.vocab), d(a.dlogits, row, a.ld, a.vocab);
+  const int32_t first = (int32_t)blockIdx.y * per, last = r.pieces - first < per ? r.pieces : first + per;
+  // this workgroup's words: its pieces, and the edge that they touch
+  const bool begins = blockIdx.y == 0, ends = blockIdx.y == gridDim.y - 1;
+  const auto word_of = [&](int32_t piece) { return (int64_t)(piece < r.pieces ? piece : r.pieces) * kPer + r.before; };
+  const int64_t word0 = begins ? 0 : word_of(first), word1 = ends ? a.vocab : word_of(first + per);
+  const float lse = a.lse_in[row], g = a.weight ? a.weight[row] * a.inv_t : a.inv_t;
+  u32x4 w[kAhead];
+  const auto fetch = [&](int32_t v0) {
+    for (int i = 0; i < kAhead; ++i) w[i] = r.load(v0 + i * NT < last ? v0 + i * NT : last - 1);
+  };
+  if (first < last) fetch(first + threadIdx.x);
+  if (threadIdx.x < 64) read_list<T>(list, a, row, word0, word1);
+  __syncthreads();             // (dlogits may be the logits: the list's are read before any is written)
+  const bool any = *list.any;
+  const auto of = [&](float z) { return any ? g * probability(z, a.inv_t, lse) : 0.0f; };
+  for (int32_t v0 = first + threadIdx.x; v0 < last; v0 += NT * kAhead) {
+    float x[kAhead][kPer];
+    for (int i = 0; i < kAhead; ++i) {
+      unpack<T>(w[i], x[i]);
+      for (int k = 0; k < kPer; ++k) x[i][k] = of(x[i][k]);
+    }
+    if (v0 + NT * kAhead < last) fetch(v0 + NT * kAhead);
+    for (int i = 0; i < kAhead; ++i)
+      if (v0 + i * NT < last) d.store(v0 + i * NT, x[i]);
+  }
+  if (const int64_t e = r.edge(threadIdx.x); e != Row<T>::kNoEdge && (e < 0 ? begins : ends)) set_element<T>(d.at, e, of(element<T>(r.at, e)));
   __syncthreads();
-  const int32_t first = (int32_t)blockIdx.y * pieces, all = Row<T>(a.logits, row, a.ld, a.vocab).pieces();
-  gradient<T, NT>(list, a, row, first, all - first < pieces ? all : first + pieces, a.lse_in[row]);
+  rewrite_list<T, NT>(list, a, row, word0, word1, g, [&](float z) { return probability(z, a.inv_t, lse); });
 }
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
+  constexpr int kPer = Row<T>::kPer;
   __shared__ Scratch<NT> sh;
+  const List list(a.top);
   const int64_t row = blockIdx.x;
-  const Row<T> r(a.logits, row, a.ld, a.vocab);
-  if (threadIdx.x < 64) read_list<T>(sh.list, a, row, true);
-  const float lse = lse_of(row_sum<T, NT>(sh, r, a.c), a.inv_t);
+  const Row<T> r(a.logits, row, a.ld, a.vocab), d(a.dlogits, row, a.ld, a.vocab);
+  if (threadIdx.x < 64) read_list<T>(list, a, row, 0, a.vocab);
+  const float lse = lse_of(row_sum<T, NT>(sh, r, a.c), a.inv_t), g = a.weight ? a.weight[row] * a.inv_t : a.inv_t;
   if (threadIdx.x < 64) {
-    const float loss = sh.list.any ? list_loss(sh.list, a, lse) : 0.0f;
+    const float loss = *list.any ? list_loss(list, a, lse) : 0.0f;
     if (threadIdx.x == 0) a.loss[row] = loss;
   }
-  gradient<T, NT>(sh.list, a, row, 0, r.pieces(), lse);
+  const bool any = *list.any;
+  const auto of = [&](float z) { return any ? g * probability(z, a.inv_t, lse) : 0.0f; };
+  for (int32_t v = threadIdx.x; v < r.pieces; v += NT) {
+    float x[kPer];
+    unpack<T>(r.load(v), x);
+    for (int k = 0; k < kPer; ++k) x[k] = of(x[k]);
+    d.store(v, x);
+  }
+  if (const int64_t e = r.edge(threadIdx.x); e != Row<T>::kNoEdge) set_element<T>(d.at, e, of(element<T>(r.at, e)));
+  __syncthreads();
+  rewrite_list<T, NT>(list, a, row, 0, a.vocab, g, [&](float z) { return probability(z, a.inv_t, lse); });
+}
+
+// The same with the row in registers, NV pieces a thread.  A workgroup takes row after row: where a piece of the gradient has been
+// written, that piece of the next row is asked for, so that loads and stores are on their way together and the exponentials of one row
+// lie over the loads of the next.
+template <typename T, int NT, int NV>
+__global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows) {
+  constexpr int kPer = Row<T>::kPer;
+  __shared__ Scratch<NT> sh[2];                  // (and two lists: each is written again two barriers after it was read)
+  u32x4 w[NV];
+  float edge = 0.0f;
+  const auto fetch = [&](const Row<T> &of, int i) {              // (pieces past the last: the last once more)
+    const int32_t v = threadIdx.x + i * NT;
+    w[i] = of.load(v < of.pieces ? v : of.pieces - 1);
+  };
+  const auto fetch_edge = [&](const Row<T> &of) {
+    if (const int64_t e = of.edge(threadIdx.x); e != Row<T>::kNoEdge) edge = element<T>(of.at, e);
+  };
+  {
+    const Row<T> of(a.logits, blockIdx.x, a.ld, a.vocab);
+    if (of.pieces > 0)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) fetch(of, i);
+    fetch_edge(of);
+  }
+  if (threadIdx.x < 64) read_list<T>(List(a.top, 0), a, blockIdx.x, 0, a.vocab);
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+    const List list(a.top, turn);
+    const Row<T> r(a.logits, row, a.ld, a.vocab), d(a.dlogits, row, a.ld, a.vocab);
+    const int64_t e = r.edge(threadIdx.x);
+    Running run;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float x[kPer];
+      unpack<T>(w[i], x);
+      if ((int32_t)threadIdx.x + i * NT < r.pieces) add<kPer>(run, x, a.c);
+      __builtin_amdgcn_sched_barrier(0);         // (one piece after the other: side by side they would not fit the registers)
+    }
+    if (e != Row<T>::kNoEdge) add<1>(run, &edge, a.c);
+    run = join_waves<NT>(sh[turn].m, sh[turn].s, run, a.c);
+    const float g = a.weight ? a.weight[row] * a.inv_t : a.inv_t, inv_s = 1.0f / run.s, gs = g * inv_s;
+    const bool any = *list.any;
+    if (threadIdx.x < 64) {
+      const float loss = any ? list_loss(list, a, lse_of(run, a.inv_t)) : 0.0f;
+      if (threadIdx.x == 0) a.loss[row] = loss;
+    }
+    const int64_t next = row + gridDim.x;
+    const bool more = next < rows;
+    const Row<T> then(a.logits, more ? next : row, a.ld, a.vocab);
+    if (e != Row<T>::kNoEdge) set_element<T>(d.at, e, any ? gs * exp2_diff(edge, run.m, a.c) : 0.0f);
+    if (more) fetch_edge(then);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int32_t v = threadIdx.x + i * NT;
+      float x[kPer];
+      asm("" : "+v"(w[i]));                      // (unpacked again: the values of the sum above are not kept for it)
+      unpack<T>(w[i], x);
+      for (int k = 0; k < kPer; ++k) x[k] = any ? gs * exp2_diff(x[k], run.m, a.c) : 0.0f;
+      if (v < r.pieces) d.store(v, x);
+      if (more && then.pieces > 0) fetch(then, i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+    rewrite_list<T, NT>(list, a, row, 0, a.vocab, g, [&](float z) { return exp2_diff(z, run.m, a.c) * inv_s; });
+    if (threadIdx.x < 64 && more) read_list<T>(List(a.top, turn ^ 1), a, next, 0, a.vocab);
+  }
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
@@ -299,7 +432,7 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
 // (`more`: the call's other pointers are given)
 int check(const void *logits, const nvfp4_distill_params *p, const void *teacher, const void *index, bool more) {
   if (!p || (p->rows != 0 && (!logits || !teacher || !index || !more))) return NVFP4_ERR_NULL;
-  if (p->rows < 0 || p->rows > kMostRows || p->vocab <= 0 || p->vocab > ((int64_t)1 << 31) - 16 || p->ld < p->vocab ||
+  if (p->rows < 0 || p->rows > kMostRows || p->vocab <= 0 || p->vocab > (int64_t)1 << 29 || p->ld < p->vocab ||
       p->ld > (int64_t)1 << 40 || p->rows * p->ld > (int64_t)1 << 40 || p->top <= 0 || p->top > kMostTop)
     return NVFP4_ERR_SHAPE;
   if (!(p->temperature > 0.0f) || !(p->temperature < kInf) || p->x_dtype > NVFP4_X_F32 || p->teacher_dtype > NVFP4_X_F32 ||
@@ -326,6 +459,25 @@ DistillArgs args(const void *logits, const nvfp4_distill_params *p, const void *
   return a;
 }
 
+constexpr int kComputeUnits = 256;
+
+template <typename T, int NT, int NV>
+int run_rows(const DistillArgs &a, int64_t rows, int per_cu, hipStream_t s) {
+  const int64_t most = (int64_t)kComputeUnits * per_cu;
+  return launch(k_distill_rows<T, NT, NV>, dim3((uint32_t)(rows < most ? rows : most)), dim3(NT), 2 * list_bytes(a.top), s, a, (int32_t)rows);
+}
+template <typename T>
+int run_step(const DistillArgs &a, int64_t rows, hipStream_t s) {
+  constexpr int64_t kPer = 16 / sizeof(T);
+  const int64_t pieces = a.vocab / kPer;         // (whole ones, at most)
+  if (pieces <= 256 * 4) return run_rows<T, 256, 4>(a, rows, 8, s);
+  if (pieces <= 256 * 8) return run_rows<T, 256, 8>(a, rows, 8, s);
+  if (pieces <= 512 * 8) return run_rows<T, 512, 8>(a, rows, 4, s);
+  if (pieces <= 1024 * 8) return run_rows<T, 1024, 8>(a, rows, 2, s);
+  if (pieces <= 1024 * 16) return run_rows<T, 1024, 16>(a, rows, 1, s);
+  return launch(k_distill_step<T, 1024>, dim3((uint32_t)rows), dim3(1024), list_bytes(a.top), s, a);
+}
+
 }  // namespace
 }  // namespace nvfp4_46
 
@@ -340,7 +492,7 @@ extern "C" int nvfp4_distill_forward(const void *logits, const nvfp4_distill_par
   a.loss = loss;
   a.lse = lse;
   return launch(p->x_dtype ? k_distill_forward<float, 256> : k_distill_forward<__bf16, 256>, dim3((uint32_t)p->rows), dim3(256),
-                0, static_cast<hipStream_t>(stream), a);
+                list_bytes(p->top), static_cast<hipStream_t>(stream), a);
 }
 
 extern "C" int nvfp4_distill_backward(const void *logits, const nvfp4_distill_params *p, const void *teacher, const void *index,
@@ -354,9 +506,13 @@ extern "C" int nvfp4_distill_backward(const void *logits, const nvfp4_distill_pa
   a.lse_in = lse;
   a.weight = weight;
   a.dlogits = dlogits;
-  const int32_t per = p->x_dtype ? 4 : 8, pieces = (int32_t)((p->vocab + per - 1) / per) + 1;    // (one more where rows begin inside)
-  return launch(p->x_dtype ? k_distill_backward<float, 256> : k_distill_backward<__bf16, 256>, dim3((uint32_t)p->rows, 1),
-                dim3(256), 0, static_cast<hipStream_t>(stream), a, pieces);
+  const int64_t per = p->x_dtype ? 4 : 8, pieces = p->vocab / per > 0 ? p->vocab / per : 1;      // (whole ones, at most)
+  // few rows: several workgroups a row, of 1024 pieces at least
+  int64_t splits = 1;
+  while (splits < 256 && p->rows * splits < 512 && pieces / (2 * splits) >= 1024) splits *= 2;
+  return launch(p->x_dtype ? k_distill_backward<float, 256> : k_distill_backward<__bf16, 256>,
+                dim3((uint32_t)p->rows, (uint32_t)splits), dim3(256), list_bytes(p->top), static_cast<hipStream_t>(stream), a,
+                (int32_t)((pieces + splits - 1) / splits));
 }
 
 extern "C" int nvfp4_distill_step(const void *logits, const nvfp4_distill_params *p, const void *teacher, const void *index,
@@ -370,6 +526,6 @@ extern "C" int nvfp4_distill_step(const void *logits, const nvfp4_distill_params
   a.loss = loss;
   a.weight = weight;
   a.dlogits = dlogits;
-  return launch(p->x_dtype ? k_distill_step<float, 256> : k_distill_step<__bf16, 256>, dim3((uint32_t)p->rows), dim3(256), 0,
-                static_cast<hipStream_t>(stream), a);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return p->x_dtype ? run_step<float>(a, p->rows, s) : run_step<__bf16>(a, p->rows, s);
 }
