@@ -361,45 +361,50 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
 }
 
 // The same with the row in registers, NV pieces a thread.  A workgroup takes row after row: where a piece of the gradient has been
-// written, that piece of the next row is asked for, so that loads and stores are on their way together and the exponentials of one row
-// lie over the loads of the next.
+// written, that piece of the next row is asked for, and kLag pieces later it enters the next row's sum.  So loads and stores are on
+// their way together, and the exponentials of both passes lie over them.
 template <typename T, int NT, int NV>
 __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows) {
-  constexpr int kPer = Row<T>::kPer;
+  constexpr int kPer = Row<T>::kPer, kLag = NV / 4;
   __shared__ Scratch<NT> sh[2];                  // (and two lists: each is written again two barriers after it was read)
   u32x4 w[NV];
   float edge = 0.0f;
+  int32_t thread = threadIdx.x;
   const auto fetch = [&](const Row<T> &of, int i) {              // (pieces past the last: the last once more)
-    const int32_t v = threadIdx.x + i * NT;
-    w[i] = of.load(v < of.pieces ? v : of.pieces - 1);
+    const int32_t v = thread + i * NT;
+    if (of.pieces > 0) w[i] = of.load(v < of.pieces ? v : of.pieces - 1);
   };
   const auto fetch_edge = [&](const Row<T> &of) {
     if (const int64_t e = of.edge(threadIdx.x); e != Row<T>::kNoEdge) edge = element<T>(of.at, e);
   };
+  const auto sum = [&](const Row<T> &of, int i, Running &run) {
+    float x[kPer];
+    asm("" : "+v"(w[i]));                        // (what is unpacked here is not kept for the gradient: there would be no registers)
+    unpack<T>(w[i], x);
+    if (thread + i * NT < of.pieces) add<kPer>(run, x, a.c);
+  };
+  Running run;
   {
     const Row<T> of(a.logits, blockIdx.x, a.ld, a.vocab);
-    if (of.pieces > 0)
 #pragma unroll
-      for (int i = 0; i < NV; ++i) fetch(of, i);
+    for (int i = 0; i < NV; ++i) fetch(of, i);
     fetch_edge(of);
+    if (threadIdx.x < 64) read_list<T>(List(a.top, 0), a, blockIdx.x, 0, a.vocab);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      sum(of, i, run);
+      __builtin_amdgcn_sched_barrier(0);         // (one piece after the other: side by side they would not fit the registers)
+    }
   }
-  if (threadIdx.x < 64) read_list<T>(List(a.top, 0), a, blockIdx.x, 0, a.vocab);
   int turn = 0;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+    asm("" : "+v"(thread));                      // (the pieces' places are found again for each row, not kept)
     const List list(a.top, turn);
     const Row<T> r(a.logits, row, a.ld, a.vocab), d(a.dlogits, row, a.ld, a.vocab);
     const int64_t e = r.edge(threadIdx.x);
-    Running run;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float x[kPer];
-      unpack<T>(w[i], x);
-      if ((int32_t)threadIdx.x + i * NT < r.pieces) add<kPer>(run, x, a.c);
-      __builtin_amdgcn_sched_barrier(0);         // (one piece after the other: side by side they would not fit the registers)
-    }
     if (e != Row<T>::kNoEdge) add<1>(run, &edge, a.c);
     run = join_waves<NT>(sh[turn].m, sh[turn].s, run, a.c);
-    const float g = a.weight ? a.weight[row] * a.inv_t : a.inv_t, inv_s = 1.0f / run.s, gs = g * inv_s;
+    const float g = a.weight ? a.weight[row] * a.inv_t : a.inv_t, inv_s = 1.0f / run.s, gs = g * inv_s, most = run.m;
     const bool any = *list.any;
     if (threadIdx.x < 64) {
       const float loss = any ? list_loss(list, a, lse_of(run, a.inv_t)) : 0.0f;
@@ -408,21 +413,31 @@ __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows
     const int64_t next = row + gridDim.x;
     const bool more = next < rows;
     const Row<T> then(a.logits, more ? next : row, a.ld, a.vocab);
-    if (e != Row<T>::kNoEdge) set_element<T>(d.at, e, any ? gs * exp2_diff(edge, run.m, a.c) : 0.0f);
+    if (e != Row<T>::kNoEdge) set_element<T>(d.at, e, any ? gs * exp2_diff(edge, most, a.c) : 0.0f);
     if (more) fetch_edge(then);
+    run = {};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int32_t v = threadIdx.x + i * NT;
+      const int32_t v = thread + i * NT;
       float x[kPer];
-      asm("" : "+v"(w[i]));                      // (unpacked again: the values of the sum above are not kept for it)
+      asm("" : "+v"(w[i]));
       unpack<T>(w[i], x);
-      for (int k = 0; k < kPer; ++k) x[k] = any ? gs * exp2_diff(x[k], run.m, a.c) : 0.0f;
+      for (int k = 0; k < kPer; ++k) x[k] = any ? gs * exp2_diff(x[k], most, a.c) : 0.0f;
       if (v < r.pieces) d.store(v, x);
-      if (more && then.pieces > 0) fetch(then, i);
+      if (more) fetch(then, i);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more && i >= kLag) sum(then, i - kLag, run);
       __builtin_amdgcn_sched_barrier(0);
     }
+    if (more) {
+#pragma unroll
+      for (int i = NV - kLag; i < NV; ++i) {
+        sum(then, i, run);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     __syncthreads();
-    rewrite_list<T, NT>(list, a, row, 0, a.vocab, g, [&](float z) { return exp2_diff(z, run.m, a.c) * inv_s; });
+    rewrite_list<T, NT>(list, a, row, 0, a.vocab, g, [&](float z) { return exp2_diff(z, most, a.c) * inv_s; });
     if (threadIdx.x < 64 && more) read_list<T>(List(a.top, turn ^ 1), a, next, 0, a.vocab);
   }
 }
@@ -471,9 +486,9 @@ int run_step(const DistillArgs &a, int64_t rows, hipStream_t s) {
   constexpr int64_t kPer = 16 / sizeof(T);
   const int64_t pieces = a.vocab / kPer;         // (whole ones, at most)
   if (pieces <= 256 * 4) return run_rows<T, 256, 4>(a, rows, 8, s);
-  if (pieces <= 256 * 8) return run_rows<T, 256, 8>(a, rows, 8, s);
-  if (pieces <= 512 * 8) return run_rows<T, 512, 8>(a, rows, 4, s);
-  if (pieces <= 1024 * 8) return run_rows<T, 1024, 8>(a, rows, 2, s);
+  if (pieces <= 256 * 8) return run_rows<T, 256, 8>(a, rows, 7, s);
+  if (pieces <= 256 * 16) return run_rows<T, 256, 16>(a, rows, 4, s);
+  if (pieces <= 512 * 16) return run_rows<T, 512, 16>(a, rows, 2, s);
   if (pieces <= 1024 * 16) return run_rows<T, 1024, 16>(a, rows, 1, s);
   return launch(k_distill_step<T, 1024>, dim3((uint32_t)rows), dim3(1024), list_bytes(a.top), s, a);
 }
