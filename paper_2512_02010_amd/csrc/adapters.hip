@@ -26,7 +26,7 @@ constexpr int kTile = 32;                       // tokens of a planned tile
 constexpr int kFewTile = 16;                    // ... and of a tile that a workgroup finds for itself
 constexpr int kFewTokens = 256;                 // up to here there is no plan (find_tile)
 constexpr int kPlanThreads = 1024;
-constexpr int kOuterWidth = 512;                // columns of a workgroup of k_outer, 128 a wave
+constexpr int kOuterWidth = 128;                // columns of a workgroup of k_outer
 constexpr int kBlock = 64;                      // columns of a block of k_expand
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -693,7 +693,7 @@ struct OuterHalf {
 };
 struct OuterArgs {
   Plan plan;
-  int32_t rank, term_ranks, tiles;   // tiles of a range
+  int32_t L, rank, term_ranks, tiles;        // tiles of a range
   OuterHalf half[2];
 };
 
@@ -705,101 +705,136 @@ __device__ inline int64_t place(const Plan &p, int32_t adapter, int32_t range, i
 }
 
 // D[column][rank], summed over the tokens of a tile.  Of 32 tokens and 128 columns lane (row, group) loads columns 8 row .. 8 row + 7 of
-// tokens 8 group .. 8 group + 7, which transposes within the lane: product j has columns 8 row + j.
+// tokens 8 group .. 8 group + 7, which transposes within the lane: product j has columns 8 row + j.  The waves of a workgroup have the
+// same columns and every fourth tile of an adapter each; their sums meet in LDS, so that a workgroup leaves one sum an adapter.
 template <int RT>
-__global__ void __launch_bounds__(256) k_outer(OuterArgs a) {
+__global__ void __launch_bounds__(256, 2) k_outer(OuterArgs a) {
+  __shared__ float sums[4][2048];
   const bool second = (int32_t)blockIdx.x >= a.half[0].chunks;
   const OuterHalf f = second ? a.half[1] : a.half[0];
   const int32_t chunk = (int32_t)blockIdx.x - (second ? a.half[0].chunks : 0), range = blockIdx.y, rank0 = blockIdx.z * RT * 16;
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
-  const int64_t c0 = (int64_t)chunk * kOuterWidth + wave * 128, c = c0 + row * 8;
-  if (c0 >= f.width) return;
+  const int64_t c0 = (int64_t)chunk * kOuterWidth, c = c0 + row * 8, size = f.width * a.rank;
   const __bf16 *const from = f.x + (c < f.width ? c : f.width - 8);          // (columns past the last are not kept)
-  const int64_t size = f.width * a.rank;
   const int32_t count = *a.plan.count, first = range * a.tiles, last = first + a.tiles < count ? first + a.tiles : count;
-  f32x4 acc[RT][8] = {};
-  int32_t adapter = -1;
-  const auto flush = [&] {
-    if (adapter < 0) return;
-    const int64_t at = place(a.plan, adapter, range, a.tiles);
-    float *const to = at < 0 ? f.out + adapter * size : f.parted + at * size;
-    for (int r = 0; r < RT; ++r) {
-      const int rank = rank0 + r * 16 + row;
-      for (int v = 0; v < 4; ++v) {
-        const int64_t col = c0 + (group * 4 + v) * 8;
-        if (rank < a.rank && col < f.width) {
-          if (f.by_rank) {
-            for (int j = 0; j < 8; ++j) to[(col + j) * a.rank + rank] = acc[r][j][v];
-          } else {
-            for (int j = 0; j < 8; j += 4)
-              *reinterpret_cast<f32x4 *>(to + rank * f.width + col + j) = f32x4{acc[r][j][v], acc[r][j + 1][v], acc[r][j + 2][v], acc[r][j + 3][v]};
-          }
-        }
-      }
+  // eight columns of rank rank0 + r 16 + row, from c0 + (group 4 + wave) 8
+  const auto put = [&](float *to, int r, const float *v) {
+    const int rank = rank0 + r * 16 + row;
+    const int64_t col = c0 + (group * 4 + wave) * 8;
+    if (rank >= a.rank || col >= f.width) return;
+    if (f.by_rank) {
+      for (int j = 0; j < 8; ++j) to[(col + j) * a.rank + rank] = v[j];
+    } else {
+      for (int j = 0; j < 8; j += 4) *reinterpret_cast<f32x4 *>(to + rank * f.width + col + j) = f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
     }
-    for (int r = 0; r < RT; ++r)
-      for (int j = 0; j < 8; ++j) acc[r][j] = f32x4{};
   };
-  // tile i's columns and terms are on their way while tile i - 1 is multiplied, its tokens' numbers one tile earlier still
-  int32_t token[8];
+  if (range == 0)                                // adapters without tokens
+    for (int32_t l = 0; l < a.L; ++l)
+      if (a.plan.tile_begin[l] == a.plan.tile_begin[l + 1])
+        for (int r = 0; r < RT; ++r) {
+          const float zero[8] = {};
+          put(f.out + l * size, r, zero);
+        }
+  const auto segment_end = [&](int32_t i, int32_t adapter) {
+    const int32_t end = a.plan.tile_begin[adapter + 1];
+    return end < last ? end : last;
+  };
+  // this wave's first tile of the segments from i on, `last`: there is none
+  const auto first_from = [&](int32_t i) {
+    while (i < last) {
+      const int32_t l = a.plan.tiles[i].adapter;
+      if (l < 0) return last;                    // (they come last)
+      const int32_t end = segment_end(i, l);
+      if (i + wave < end) return i + wave;
+      i = end;
+    }
+    return last;
+  };
+  f32x4 acc[RT][8];
   u32x4 x[8];
   bf16x8 hs[RT][3];
-  const auto fetch_tokens = [&](int32_t i) {
-    if (i >= last) return;
-    for (int q = 0; q < 8; ++q) token[q] = a.plan.order[(int64_t)i * kTile + group * 8 + q];
+  const auto fetch_x = [&](int32_t i) {
+    const u32x4 *const tokens = reinterpret_cast<const u32x4 *>(a.plan.order + (int64_t)i * kTile + group * 8);
+    const u32x4 token[2] = {tokens[0], tokens[1]};
+    for (int q = 0; q < 8; ++q) {
+      const int32_t t = (int32_t)token[q / 4][q % 4];
+      x[q] = *reinterpret_cast<const u32x4 *>(from + (int64_t)(t < 0 ? 0 : t) * f.ld);
+    }
   };
-  const auto fetch = [&](int32_t i) {
-    if (i >= last) return;
-    for (int q = 0; q < 8; ++q) x[q] = *reinterpret_cast<const u32x4 *>(from + (token[q] < 0 ? 0 : token[q]) * f.ld);
+  const auto fetch_terms = [&](int32_t i) {
     for (int r = 0; r < RT; ++r)
       for (int which = 0; which < 3; ++which)
         hs[r][which] = load8(f.terms + ((i * (int64_t)3 + which) * a.term_ranks + rank0 + r * 16 + row) * kTile + group * 8);
   };
-  fetch_tokens(first);
-  fetch(first);
-  fetch_tokens(first + 1);
-  for (int32_t i = first; i < last; ++i) {
-    const Tile t = a.plan.tiles[i];
-    if (t.adapter < 0) break;                    // (they come last)
-    if (t.adapter != adapter) flush();
-    adapter = t.adapter;
-    if (t.count < kTile)                         // (the terms there are 0, but what was loaded need not be finite)
-      for (int q = 0; q < 8; ++q)
-        if (group * 8 + q >= t.count) x[q] = u32x4{};
-    bf16x8 xt[8], now[RT][3];
-    for (int j = 0; j < 8; ++j) {
-      u32x4 p;
-      for (int q = 0; q < 4; ++q) p[q] = __builtin_amdgcn_perm(x[2 * q + 1][j / 2], x[2 * q][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-      xt[j] = __builtin_bit_cast(bf16x8, p);
-    }
-    for (int r = 0; r < RT; ++r)
-      for (int which = 0; which < 3; ++which) now[r][which] = hs[r][which];
-    fetch(i + 1);
-    fetch_tokens(i + 2);
-    for (int r = 0; r < RT; ++r)
-      for (int which = 0; which < 3; ++which)
-        for (int j = 0; j < 8; ++j) acc[r][j] = multiply(xt[j], now[r][which], acc[r][j]);
+  int32_t mine = first_from(first);
+  if (mine < last) {
+    fetch_x(mine);
+    fetch_terms(mine);
   }
-  flush();
+  for (int32_t i = first; i < last;) {
+    const int32_t adapter = a.plan.tiles[i].adapter;
+    if (adapter < 0) break;
+    const int32_t end = segment_end(i, adapter);
+    for (int r = 0; r < RT; ++r)
+      for (int j = 0; j < 8; ++j) acc[r][j] = f32x4{};
+    while (mine < end) {
+      const Tile t = a.plan.tiles[mine];
+      const int32_t next = mine + 4 < end ? mine + 4 : first_from(end);
+      if (t.count < kTile)                       // (the terms there are 0, but what was loaded need not be finite)
+        for (int q = 0; q < 8; ++q)
+          if (group * 8 + q >= t.count) x[q] = u32x4{};
+      bf16x8 xt[8];
+      for (int j = 0; j < 8; ++j) {
+        u32x4 p;
+        for (int q = 0; q < 4; ++q) p[q] = __builtin_amdgcn_perm(x[2 * q + 1][j / 2], x[2 * q][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+        xt[j] = __builtin_bit_cast(bf16x8, p);
+      }
+      __builtin_amdgcn_sched_barrier(0);         // (the next tile's columns go where these were, its terms where these are)
+      if (next < last) fetch_x(next);
+      for (int r = 0; r < RT; ++r)
+        for (int which = 0; which < 3; ++which)
+          for (int j = 0; j < 8; ++j) acc[r][j] = multiply(xt[j], hs[r][which], acc[r][j]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (next < last) fetch_terms(next);
+      mine = next;
+    }
+    const int64_t at = place(a.plan, adapter, range, a.tiles);
+    float *const to = at < 0 ? f.out + adapter * size : f.parted + at * size;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      for (int j = 0; j < 8; ++j)
+        for (int v = 0; v < 4; ++v) sums[wave][(j * 4 + v) * 64 + lane] = acc[r][j][v];
+      __syncthreads();
+      float v[8];
+      for (int j = 0; j < 8; ++j) {
+        const int e = (j * 4 + wave) * 64 + lane;
+        v[j] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+      }
+      put(to, r, v);
+      __syncthreads();
+    }
+    i = end;
+  }
 }
 
 // ---- k_join -----------------------------------------------------------------------------------------------------------
 
+// Adapters whose tokens lie in several ranges.
 __global__ void __launch_bounds__(256) k_join(OuterArgs a) {
   const int32_t l = blockIdx.y, t0 = a.plan.tile_begin[l], t1 = a.plan.tile_begin[l + 1];
-  const int32_t s0 = t0 / a.tiles, s1 = t1 > t0 ? (t1 - 1) / a.tiles : s0;
-  if (t1 > t0 && s0 == s1) return;               // k_outer has written it
-  for (int k = 0; k < 2; ++k) {
-    const OuterHalf &f = a.half[k];
-    const int64_t size = f.width * a.rank;       // (a multiple of 8)
-    for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < size; e += (int64_t)gridDim.x * 1024) {
-      f32x4 s{};
-      if (t1 > t0) {
-        s = *reinterpret_cast<const f32x4 *>(f.parted + (2 * s0 + 1) * size + e);
-        for (int64_t r = s0 + 1; r <= s1; ++r) s += *reinterpret_cast<const f32x4 *>(f.parted + 2 * r * size + e);
-      }
-      *reinterpret_cast<f32x4 *>(f.out + l * size + e) = s;
+  const int32_t s0 = t0 / a.tiles, s1 = (t1 - 1) / a.tiles;
+  if (t1 <= t0 || s0 == s1) return;              // k_outer has written it
+  const OuterHalf &f = a.half[blockIdx.z];
+  const int64_t size = f.width * a.rank;         // (a multiple of 8)
+  for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < size; e += (int64_t)gridDim.x * 1024) {
+    f32x4 s = *reinterpret_cast<const f32x4 *>(f.parted + (2 * (int64_t)s0 + 1) * size + e);
+    for (int32_t r = s0 + 1; r <= s1; r += 4) {                     // (four on their way; past the last once more the last)
+      f32x4 v[4];
+      for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const f32x4 *>(f.parted + 2 * (int64_t)(r + k < s1 ? r + k : s1) * size + e);
+      for (int k = 0; k < 4; ++k)
+        if (r + k <= s1) s += v[k];
     }
+    *reinterpret_cast<f32x4 *>(f.out + l * size + e) = s;
   }
 }
 
@@ -845,8 +880,8 @@ struct Layout {
     const int64_t chunks = divide_up(p.inp, kOuterWidth) + divide_up(p.out, kOuterWidth);
     ranges = divide_up(512, chunks);
     range_tiles = divide_up(tiles, ranges);
-    if (range_tiles < 1) range_tiles = 1;
-    ranges = divide_up(tiles, range_tiles);
+    if (range_tiles < 4) range_tiles = 4;        // (a tile for each wave)
+    ranges = tiles ? divide_up(tiles, range_tiles) : 1;
     int64_t end = 0;
     const auto take = [&](int64_t n) {
       const int64_t begin = end;
@@ -1009,7 +1044,7 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
   float *const parts = reinterpret_cast<float *>(w + d.parts);
   __bf16 *const terms_a = reinterpret_cast<__bf16 *>(w + d.terms_a), *const terms_b = reinterpret_cast<__bf16 *>(w + d.terms_b);
   const int32_t rank = (int32_t)p->rank, pitch = (int32_t)Layout::pitch(*p), term_ranks = (int32_t)Layout::term_ranks(*p);
-  const OuterArgs g{d.plan(w), rank, term_ranks, (int32_t)d.range_tiles,
+  const OuterArgs g{d.plan(w), (int32_t)p->adapters, rank, term_ranks, (int32_t)d.range_tiles,
                     {{static_cast<const __bf16 *>(x), terms_a, da, reinterpret_cast<float *>(w + d.parted_a), p->ld_x, p->inp,
                       (int32_t)divide_up(p->inp, kOuterWidth), false},
                      {static_cast<const __bf16 *>(dy), terms_b, db, reinterpret_cast<float *>(w + d.parted_b), p->ld_dy, p->out,
@@ -1021,9 +1056,10 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
     const ExpandArgs e{tokens, parts, nullptr, terms_a, reinterpret_cast<const __bf16 *>(w + d.at), scales, dx_base, dx,
                        p->ld_base, p->ld_out, p->inp, rank, pitch, pitch, (int32_t)d.splits_out, term_ranks, false};
     if (const int rc = run_expand<__bf16>(e, d, s)) return rc;
-    const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, rank <= 64 ? 1 : 2);
-    if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
   }
+  const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, rank <= 64 ? 1 : 2);
+  if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
+  if (d.ranges == 1) return NVFP4_OK;
   const int64_t most = divide_up(p->rank * (p->inp > p->out ? p->inp : p->out), 1024);
-  return launch(k_join, dim3((uint32_t)(most < 256 ? most : 256), (uint32_t)p->adapters), dim3(256), 0, s, g);
+  return launch(k_join, dim3((uint32_t)(most < 256 ? most : 256), (uint32_t)p->adapters, 2), dim3(256), 0, s, g);
 }
