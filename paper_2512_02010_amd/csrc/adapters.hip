@@ -708,7 +708,7 @@ __device__ inline int64_t place(const Plan &p, int32_t adapter, int32_t range, i
 // tokens 8 group .. 8 group + 7, which transposes within the lane: product j has columns 8 row + j.  The waves of a workgroup have the
 // same columns and every fourth tile of an adapter each; their sums meet in LDS, so that a workgroup leaves one sum an adapter.
 template <int RT>
-__global__ void __launch_bounds__(256, 2) k_outer(OuterArgs a) {
+__global__ void __launch_bounds__(256, RT <= 2 ? 2 : 1) k_outer(OuterArgs a) {
   __shared__ float sums[4][2048];
   const bool second = (int32_t)blockIdx.x >= a.half[0].chunks;
   const OuterHalf f = second ? a.half[1] : a.half[0];
@@ -753,9 +753,11 @@ __global__ void __launch_bounds__(256, 2) k_outer(OuterArgs a) {
   f32x4 acc[RT][8];
   u32x4 x[8];
   bf16x8 hs[RT][3];
-  const auto fetch_x = [&](int32_t i) {
-    const u32x4 *const tokens = reinterpret_cast<const u32x4 *>(a.plan.order + (int64_t)i * kTile + group * 8);
-    const u32x4 token[2] = {tokens[0], tokens[1]};
+  u32x4 token[2];
+  const auto fetch_tokens = [&](int32_t i) {
+    for (int k = 0; k < 2; ++k) token[k] = reinterpret_cast<const u32x4 *>(a.plan.order + (int64_t)i * kTile + group * 8)[k];
+  };
+  const auto fetch_x = [&] {
     for (int q = 0; q < 8; ++q) {
       const int32_t t = (int32_t)token[q / 4][q % 4];
       x[q] = *reinterpret_cast<const u32x4 *>(from + (int64_t)(t < 0 ? 0 : t) * f.ld);
@@ -766,10 +768,19 @@ __global__ void __launch_bounds__(256, 2) k_outer(OuterArgs a) {
       for (int which = 0; which < 3; ++which)
         hs[r][which] = load8(f.terms + ((i * (int64_t)3 + which) * a.term_ranks + rank0 + r * 16 + row) * kTile + group * 8);
   };
-  int32_t mine = first_from(first);
+  // this wave's tile after `i`
+  const auto after = [&](int32_t i) {
+    const int32_t end = segment_end(i, a.plan.tiles[i].adapter);
+    return i + 4 < end ? i + 4 : first_from(end);
+  };
+  // a tile's tokens are asked for a tile before its columns and terms, those while the tile before is multiplied
+  int32_t mine = first_from(first), next = last;
   if (mine < last) {
-    fetch_x(mine);
+    fetch_tokens(mine);
+    fetch_x();
     fetch_terms(mine);
+    next = after(mine);
+    if (next < last) fetch_tokens(next);
   }
   for (int32_t i = first; i < last;) {
     const int32_t adapter = a.plan.tiles[i].adapter;
@@ -779,7 +790,6 @@ __global__ void __launch_bounds__(256, 2) k_outer(OuterArgs a) {
       for (int j = 0; j < 8; ++j) acc[r][j] = f32x4{};
     while (mine < end) {
       const Tile t = a.plan.tiles[mine];
-      const int32_t next = mine + 4 < end ? mine + 4 : first_from(end);
       if (t.count < kTile)                       // (the terms there are 0, but what was loaded need not be finite)
         for (int q = 0; q < 8; ++q)
           if (group * 8 + q >= t.count) x[q] = u32x4{};
@@ -790,13 +800,17 @@ __global__ void __launch_bounds__(256, 2) k_outer(OuterArgs a) {
         xt[j] = __builtin_bit_cast(bf16x8, p);
       }
       __builtin_amdgcn_sched_barrier(0);         // (the next tile's columns go where these were, its terms where these are)
-      if (next < last) fetch_x(next);
+      if (next < last) fetch_x();
       for (int r = 0; r < RT; ++r)
         for (int which = 0; which < 3; ++which)
           for (int j = 0; j < 8; ++j) acc[r][j] = multiply(xt[j], hs[r][which], acc[r][j]);
       __builtin_amdgcn_sched_barrier(0);
-      if (next < last) fetch_terms(next);
       mine = next;
+      if (mine < last) {
+        fetch_terms(mine);
+        next = after(mine);
+        if (next < last) fetch_tokens(next);
+      }
     }
     const int64_t at = place(a.plan, adapter, range, a.tiles);
     float *const to = at < 0 ? f.out + adapter * size : f.parted + at * size;
