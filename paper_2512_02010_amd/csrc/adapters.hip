@@ -8,9 +8,9 @@
 // keeps what has the rank for a side in registers.  Tokens are taken in tiles of one adapter each, in the order of their adapters
 // (k_plan), so that a tile's rows share the adapter's matrices in the matrix unit, wherever they stand.
 //
-//   k_plan     tokens in the order of their adapters (stable), tiles of 32; backwards also A and B transposed
-//   k_shrink   [T][width] times [rank][width] -> [T][rank]            h from x and A, dh / s from dy and B^T
-//   k_expand   base + s [T][rank] times [width][rank]                 out from h and B, dx from dh / s and A^T
+//   k_plan     tokens in the order of their adapters (stable), tiles of 32
+//   k_shrink   [T][width] times [rank][width] -> [T][rank]            h from x and A, dh / s from dy and B
+//   k_expand   base + s [T][rank] times [width][rank]                 out from h and B, dx from dh / s and A
 //   k_outer    s [T][rank] times [T][width] over an adapter's tokens  dA from dh / s and x, dB from h and dy
 //   k_join     sums what several workgroups of k_outer have of one adapter, in a fixed order
 #include <hip/hip_runtime.h>
@@ -142,7 +142,7 @@ __device__ inline __bf16 term(float v, int which) {
 
 struct ShrinkArgs {
   Tokens tokens;
-  const __bf16 *x, *w;         // [T] rows of `width`, and [L][rank][width]
+  const __bf16 *x, *w;         // [T] rows of `width`, and [L][rank][width], or ACROSS [L][width][rank]
   float *parts;                // [splits][T][pitch]
   float *h;                    // [T][rank], where one split is all and it is wanted; 0 for tokens without an adapter
   // backwards: the forward pass' h [T][rank], whose terms go to k_outer from here
@@ -157,36 +157,39 @@ struct ShrinkArgs {
 
 constexpr int kShrinkWaves = 8;
 
-// D[token][rank]: rows of x against rows of w, both adjacent in the summed index.  A wave has its own columns and keeps their part of w
+// D[token][rank]: rows of x against rows of w (ACROSS: its columns, turned in LDS once an adapter).  A wave has its own columns and keeps their part of w
 // in registers while it goes through 16 tokens at a time of the workgroup's stretch of the plan; the waves' sums meet in LDS.  A load has
 // 64 adjacent bytes of 16 rows; the columns of the next tokens are on their way while these are multiplied.
-template <bool FEW, int RT, int NF>
-__global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shrink(ShrinkArgs a) {
+template <bool FEW, bool ACROSS, int RT, int NF>
+__global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 && !(ACROSS && RT == 4) ? 4 : 2) k_shrink(ShrinkArgs a) {
   constexpr int kThreads = kShrinkWaves * 64, kBuffers = RT <= 4 ? 2 : 1;
   __shared__ TileTokens shared;
   __shared__ float part[kBuffers][kShrinkWaves][RT * 256];
+  __shared__ __align__(16) __bf16 turned[ACROSS ? kShrinkWaves : 1][ACROSS ? 32 * RT * 16 + 64 : 8];
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   int32_t first = 0, last = 1, token = 0;        // 16 tokens each
-  Tile only{};
+  int32_t adapter_here = -1, count_here = 0;     // of the only tile
   if constexpr (FEW) {
-    only = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, 16);
-    if (only.count == 0) return;
+    const Tile t = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, 16);
+    if (t.count == 0) return;
+    adapter_here = t.adapter;
+    count_here = t.count;
   } else {
     if (a.single) {                              // asked for together with the count
-      only = a.tokens.plan.tiles[blockIdx.x / 2];
+      adapter_here = a.tokens.plan.tiles[blockIdx.x / 2].adapter;
+      count_here = a.tokens.plan.tiles[blockIdx.x / 2].count;
       token = a.tokens.plan.order[(int64_t)blockIdx.x * 16 + row];
     }
     stretch(a.tokens.plan, 2, a.single, first, last);
   }
   const auto tile_of = [&](int32_t i) {          // the 16 tokens i
-    if constexpr (FEW) return only;
-    Tile t = a.single ? only : a.tokens.plan.tiles[i / 2];
-    t.count -= i % 2 * 16;
-    if (t.count > 16) t.count = 16;
-    return t;
+    if constexpr (FEW) return Tile{adapter_here, count_here};
+    const int32_t adapter = a.single ? adapter_here : a.tokens.plan.tiles[i / 2].adapter;
+    const int32_t left = (a.single ? count_here : a.tokens.plan.tiles[i / 2].count) - i % 2 * 16;
+    return Tile{adapter, left < 16 ? left : 16};
   };
   const auto token_of = [&](int32_t i, int n) -> int32_t {      // -1: there is none
-    if constexpr (FEW) return n < only.count ? shared.token[n] : -1;
+    if constexpr (FEW) return n < count_here ? shared.token[n] : -1;
     return a.tokens.plan.order[(int64_t)i * 16 + n];
   };
   const int32_t all_steps = (int32_t)((a.width + 31) / 32), step0 = ((int32_t)blockIdx.y * kShrinkWaves + wave) * a.steps;
@@ -232,8 +235,40 @@ __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 ? 4 : 2) k_shr
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const int n = r * 16 + row < a.rank ? r * 16 + row : a.rank - 1;            // (ranks past the last are not kept)
-      fetch(w[r], a.w + ((int64_t)adapter * a.rank + n) * a.width);
-      clear(w[r]);
+      if constexpr (!ACROSS) {
+        fetch(w[r], a.w + ((int64_t)adapter * a.rank + n) * a.width);
+        clear(w[r]);
+      } else {
+        // 32 columns of a step are 4 rank adjacent pieces of 16 bytes, 64 of them to a load
+        const __bf16 *const from = a.w + (int64_t)adapter * a.width * a.rank;
+        const int64_t most = (int64_t)width * a.rank / 8 - 1;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const int64_t piece = (int64_t)(step0 + f) * 4 * a.rank + r * 64 + lane;
+          w[r][f] = load8(from + (piece < most ? piece : most) * 8);
+        }
+      }
+    }
+    if constexpr (ACROSS) {                      // the other way round, a step at a time through the wave's own LDS
+      __bf16 *const turn = turned[ACROSS ? wave : 0];
+      const int pieces = 4 * a.rank;
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        for (int r = 0; r < RT; ++r)             // (8 columns are `rank` pieces; 32 bytes between them keep their banks apart)
+          if (const int piece = r * 64 + lane; piece < pieces) *reinterpret_cast<bf16x8 *>(turn + piece * 8 + piece / a.rank * 16) = w[r][f];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        int32_t line = group * (8 * a.rank + 16);
+        asm("" : "+v"(line));                    // (the places are found again for each step: kept, they would not leave registers)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const int n = r * 16 + row < a.rank ? r * 16 + row : a.rank - 1;
+          for (int k = 0; k < 8; ++k) w[r][f][k] = turn[line + k * a.rank + n];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      for (int r = 0; r < RT; ++r) clear(w[r]);
     }
     for (; i < last; ++i) {
       const Tile t = tile_of(i);
@@ -283,22 +318,27 @@ struct ExpandArgs {
   const float *parts;          // [splits][T][h_pitch]
   float *h;                    // their sum [T][rank], where it is wanted and k_shrink has not written it; or nullptr
   __bf16 *terms;               // backwards: the three terms of s h for k_outer, [tile][term][rank][token]; or nullptr
-  const __bf16 *w;             // [L][width] rows of `rank`, `pitch` apart
+  const __bf16 *w;             // [L][width][rank], or kAcross [L][rank][width]
   const float *scales;
   const void *base;
   void *out;                   // nullptr: only the terms
   int64_t ld_base, ld_out, width;
-  int32_t rank, pitch, h_pitch, splits, term_ranks;
+  int32_t rank, h_pitch, splits, term_ranks;
   bool single;                 // a workgroup for every tile
 };
 
-// Eight ranks of a row of w, from `first`; where rows are not WHOLE pieces of 16 bytes, one by one.
-template <bool WHOLE>
-__device__ inline bf16x8 load_ranks(const __bf16 *row, int first, int rank) {
-  if constexpr (WHOLE) return load8(row + first);
-  bf16x8 v{};
+// How the matrix of k_expand lies: rows of ranks that are whole pieces of 16 bytes, or not, or the other way round [rank][width].
+enum { kWhole, kRagged, kAcross };
+
+// Eight ranks of column c, from `first`.
+template <int LIES>
+__device__ inline bf16x8 load_ranks(const __bf16 *w, int32_t c, int first, int rank) {
+  const __bf16 *const from = w + (int64_t)c * rank;
+  if constexpr (LIES == kWhole) return load8(from + first);
+  bf16x8 v;
+  for (int i = 0; i < 8; ++i) v[i] = from[first + i < rank ? first + i : rank - 1];
   for (int i = 0; i < 8; ++i)
-    if (first + i < rank) v[i] = row[first + i];
+    if (first + i >= rank) v[i] = (__bf16)0.0f;
   return v;
 }
 
@@ -338,31 +378,35 @@ struct Columns {
 template <bool FEW, typename T, int F>
 constexpr int expand_waves = !FEW && sizeof(T) == 2 ? 8 : 4;
 
-template <bool FEW, bool WHOLE, typename T, int F>
+template <bool FEW, int LIES, typename T, int F>
 __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (expand_waves<FEW, T, F>) == 8 ? 4 : 3) k_expand(ExpandArgs a) {
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 2, kSpans = F ? F : 1, kProducts = F ? kTerms : kTerms - 1;
   constexpr int MT = FEW ? 1 : 2, kWaves = expand_waves<FEW, T, F>, kThreads = kWaves * 64, kRows = MT * 16;
   __shared__ TileTokens shared;
   __shared__ bf16x8 split[FEW ? 1 : 2][kRows][kTerms * kSpans * 4 + 1];      // (an odd number of pieces: a row a bank further)
+  __shared__ __align__(16) __bf16 turned[LIES == kAcross ? kWaves : 1][LIES == kAcross ? 32 * 68 : 8];
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   int32_t first = 0, last = 1, in[MT];           // in: this lane's token of each 16, -1: there is none
-  Tile only{};
+  int32_t adapter_here = -1, count_here = 0;     // of the only tile
   if constexpr (FEW) {
-    only = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, kRows);
-    if (only.count == 0) return;
+    const Tile t = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, kRows);
+    if (t.count == 0) return;
+    adapter_here = t.adapter;
+    count_here = t.count;
   } else {
     if (a.single) {                              // asked for together with the count
-      only = a.tokens.plan.tiles[blockIdx.x];
+      adapter_here = a.tokens.plan.tiles[blockIdx.x].adapter;
+      count_here = a.tokens.plan.tiles[blockIdx.x].count;
       for (int m = 0; m < MT; ++m) in[m] = a.tokens.plan.order[(int64_t)blockIdx.x * kRows + m * 16 + row];
     }
     stretch(a.tokens.plan, 1, a.single, first, last);
   }
   const auto tile_of = [&](int32_t i) {
-    if constexpr (FEW) return only;
-    return a.single ? only : a.tokens.plan.tiles[i];
+    if constexpr (FEW) return Tile{adapter_here, count_here};
+    return a.single ? Tile{adapter_here, count_here} : Tile{a.tokens.plan.tiles[i].adapter, a.tokens.plan.tiles[i].count};
   };
   const auto token_of = [&](int32_t i, int n) -> int32_t {       // -1: there is none
-    if constexpr (FEW) return n < only.count ? shared.token[n] : -1;
+    if constexpr (FEW) return n < count_here ? shared.token[n] : -1;
     return a.tokens.plan.order[(int64_t)i * kRows + n];
   };
   const T *const base = static_cast<const T *>(a.base);
@@ -422,15 +466,44 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
   };
   bf16x8 w[4][kSpans];
   const auto fetch_w = [&](int32_t adapter) {
-    const __bf16 *const of = a.w + (int64_t)adapter * a.width * a.pitch;
+    const __bf16 *const of = a.w + (int64_t)adapter * a.width * a.rank;
+    const auto column_of = [&](int p) { return c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4; };
+    if constexpr (LIES != kAcross) {
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int32_t c = c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4;
+      for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int f = 0; f < kSpans; ++f) {
+          const int piece = F ? f * 4 + group : group % pieces;
+          w[p][f] = load_ranks<LIES>(of, column_of(p) < width ? column_of(p) : width - 1, piece < pieces ? piece * 8 : 0, a.rank);
+          if (F && pieces % 4 && piece >= pieces) w[p][f] = bf16x8{};
+        }
+    } else {
+      // A load has eight ranks' 64 columns; 32 ranks at a time are turned in the wave's own LDS.
+      __bf16 *const turn = turned[LIES == kAcross ? wave : 0];
+      constexpr int kLine = 68;                  // (eight lines are 16 banks further)
+#pragma unroll
+      for (int f = 0; f < kSpans; ++f)
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int rank = f * 32 + p * 8 + lane / 8;
+          const int32_t c = c0 + lane % 8 * 8;
+          w[p][f] = load8(of + (int64_t)(rank < a.rank ? rank : a.rank - 1) * a.width + (c < width ? c : width - 8));
+          if (rank >= a.rank) w[p][f] = bf16x8{};
+        }
 #pragma unroll
       for (int f = 0; f < kSpans; ++f) {
-        const int piece = F ? f * 4 + group : group % pieces;
-        w[p][f] = load_ranks<WHOLE>(of + (int64_t)(c < width ? c : width - 1) * a.pitch, piece < pieces ? piece * 8 : 0, a.rank);
-        if (F && pieces % 4 && piece >= pieces) w[p][f] = bf16x8{};
+        for (int p = 0; p < 4; ++p)
+          for (int k = 0; k < 2; ++k)
+            reinterpret_cast<bf16x4 *>(turn + (p * 8 + lane / 8) * kLine + lane % 8 * 8)[k] = k ? bf16x4{w[p][f][4], w[p][f][5], w[p][f][6], w[p][f][7]}
+                                                                                              : bf16x4{w[p][f][0], w[p][f][1], w[p][f][2], w[p][f][3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int piece = F ? group : group % pieces;
+          for (int k = 0; k < 8; ++k) w[p][f][k] = turn[(piece * 8 + k) * kLine + column_of(p) - c0];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
   };
@@ -502,15 +575,10 @@ struct PlanArgs {
   const int32_t *which;
   Plan plan;
   int32_t T, L;
-  // backwards: A [L][rank][K] -> [L][K][pitch] and B [L][N][rank] -> [L][rank][N], in units of `columns` of K or N
-  const __bf16 *a, *b;
-  __bf16 *at, *bt;
-  int64_t K, N, units;
-  int32_t rank, pitch, columns;
 };
 
 // Stable counting sort by one workgroup, each wave its own stretch of the tokens, 64 at a time.
-__device__ inline void plan_tokens(const PlanArgs &p) {
+__global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs p) {
   extern __shared__ int32_t counts[];            // [16][groups + 1]: each wave's tokens of a group, then how many come before them
   const int32_t groups = p.L + 1, line = groups + 1;
   int32_t *const tile_begin = counts + 16 * line, *const members = tile_begin + groups + 1;
@@ -620,64 +688,6 @@ __device__ inline void plan_tokens(const PlanArgs &p) {
       for (int32_t n = left; n < kTile; ++n) p.plan.order[(int64_t)i * kTile + n] = -1;
     }
   }
-}
-
-// One unit: p.columns columns of an A, or rows of a B, through LDS.
-__device__ inline void transpose(const PlanArgs &p, int64_t unit) {
-  extern __shared__ int32_t space[];
-  __bf16 *const tile = reinterpret_cast<__bf16 *>(space);              // [columns][line]
-  const int64_t of_a = (p.K + p.columns - 1) / p.columns, of_b = (p.N + p.columns - 1) / p.columns, l = unit / (of_a + of_b);
-  const int64_t u = unit % (of_a + of_b);
-  const int line = p.pitch + 2, eights = p.columns / 8, pieces = p.pitch / 8;
-  if (u < of_a) {
-    const int64_t c = u * p.columns;
-    const int n = (int)(p.K - c < p.columns ? p.K - c : p.columns);    // (a multiple of 8)
-    const __bf16 *const from = p.a + l * p.rank * p.K + c;
-    for (int i = threadIdx.x; i < p.pitch * eights; i += kPlanThreads) {
-      const int rank = i / eights, k0 = i % eights * 8;
-      if (k0 >= n) continue;
-      const bf16x8 v = rank < p.rank ? load8(from + rank * p.K + k0) : bf16x8{};
-      for (int k = 0; k < 8; ++k) tile[(k0 + k) * line + rank] = v[k];
-    }
-    __syncthreads();
-    __bf16 *const to = p.at + (l * p.K + c) * p.pitch;
-    for (int i = threadIdx.x; i < n * pieces; i += kPlanThreads) {
-      bf16x8 v;
-      for (int k = 0; k < 8; ++k) v[k] = tile[i / pieces * line + i % pieces * 8 + k];
-      *reinterpret_cast<bf16x8 *>(to + (int64_t)i * 8) = v;
-    }
-  } else {
-    const int64_t c = (u - of_a) * p.columns;
-    const int n = (int)(p.N - c < p.columns ? p.N - c : p.columns);
-    const __bf16 *const from = p.b + (l * p.N + c) * p.rank;
-    if (p.rank % 8 == 0) {
-      for (int i = threadIdx.x; i < n * pieces; i += kPlanThreads) {
-        const bf16x8 v = load8(from + (int64_t)i * 8);
-        for (int k = 0; k < 8; ++k) tile[i / pieces * line + i % pieces * 8 + k] = v[k];
-      }
-    } else {
-      for (int i = threadIdx.x; i < n * p.rank; i += kPlanThreads) tile[i / p.rank * line + i % p.rank] = from[i];
-    }
-    __syncthreads();
-    __bf16 *const to = p.bt + l * p.rank * p.N + c;
-    for (int i = threadIdx.x; i < p.rank * eights; i += kPlanThreads) {
-      const int rank = i / eights, k0 = i % eights * 8;
-      if (k0 >= n) continue;
-      bf16x8 v;
-      for (int k = 0; k < 8; ++k) v[k] = tile[(k0 + k) * line + rank];
-      *reinterpret_cast<bf16x8 *>(to + rank * p.N + k0) = v;
-    }
-  }
-}
-
-__global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs p) {
-  if (blockIdx.x == 0)
-    plan_tokens(p);
-  else
-    for (int64_t unit = (int64_t)blockIdx.x - 1; unit < p.units; unit += (int64_t)gridDim.x - 1) {
-      transpose(p, unit);
-      __syncthreads();
-    }
 }
 
 // ---- k_outer ----------------------------------------------------------------------------------------------------------
@@ -872,13 +882,13 @@ struct Layout {
   int64_t tiles;               // at most so many planned tiles
   int64_t steps_in, steps_out, splits_in, splits_out;        // of k_shrink's sums over inp (h), over out (dh)
   int64_t ranges, range_tiles; // of k_outer
-  int64_t count, tile_begin, order, table, parts, at, bt, terms_a, terms_b, parted_a, parted_b, bytes;   // byte offsets
+  int64_t count, tile_begin, order, table, parts, terms_a, terms_b, parted_a, parted_b, bytes;   // byte offsets
 
   // Steps of 32 columns that a wave of k_shrink keeps w of in registers: as many as fit (ranks), fewer where there would not be
   // workgroups for the compute units, but not below two.  The splits of the sum follow.
-  static int64_t shrink_steps(int64_t tokens, bool few, int64_t width, int64_t rank) {
+  static int64_t shrink_steps(int64_t tokens, bool few, int64_t width, int64_t rank, bool across) {
     const int64_t all = divide_up(width, 32), groups = few ? divide_up(tokens, 4) : divide_up(tokens, 16);
-    int64_t steps = rank <= 64 ? 8 : 4;
+    int64_t steps = (rank <= 64 ? 8 : 4) / (across ? 2 : 1);
     while (steps > 2 && groups * divide_up(all, steps * kShrinkWaves) < 128) steps /= 2;
     const int64_t splits = divide_up(all, steps * kShrinkWaves);
     return divide_up(all, splits * kShrinkWaves);            // evenly
@@ -887,8 +897,8 @@ struct Layout {
   Layout(const nvfp4_adapters_params &p, bool backward) {
     few = !backward && p.tokens <= kFewTokens;
     tiles = p.tokens / kTile + (p.adapters + 1 < p.tokens ? p.adapters + 1 : p.tokens);
-    steps_in = shrink_steps(p.tokens, few, p.inp, p.rank);
-    steps_out = shrink_steps(p.tokens, few, p.out, p.rank);
+    steps_in = shrink_steps(p.tokens, few, p.inp, p.rank, false);
+    steps_out = shrink_steps(p.tokens, few, p.out, p.rank, true);
     splits_in = splits(steps_in, p.inp);
     splits_out = splits(steps_out, p.out);
     const int64_t chunks = divide_up(p.inp, kOuterWidth) + divide_up(p.out, kOuterWidth);
@@ -910,8 +920,6 @@ struct Layout {
     }
     parts = take((backward ? splits_out : splits_in) * p.tokens * pitch(p) * 4);
     if (backward) {
-      at = take(p.adapters * p.inp * pitch(p) * 2);
-      bt = take(p.adapters * p.out * p.rank * 2);
       terms_a = take(tiles * 3 * term_ranks(p) * kTile * 2);
       terms_b = take(tiles * 3 * term_ranks(p) * kTile * 2);
       parted_a = take(2 * ranges * p.rank * p.inp * 4);
@@ -927,66 +935,67 @@ struct Layout {
   }
 };
 
-// LDS words of plan_tokens
+// LDS words of k_plan
 constexpr size_t plan_words(int64_t adapters) { return 16 * (size_t)(adapters + 2) + (size_t)(adapters + 2) + (size_t)(adapters + 1); }
 
-int run_plan(const nvfp4_adapters_params &p, const Layout &d, char *w, const int32_t *which, const void *a, const void *b,
-             hipStream_t s) {
-  const int32_t pitch = (int32_t)Layout::pitch(p), columns = (pitch <= 8 ? 1024 : pitch <= 16 ? 512 : pitch <= 32 ? 256 : pitch <= 64 ? 128 : 64);
-  const PlanArgs g{which, d.plan(w), (int32_t)p.tokens, (int32_t)p.adapters, static_cast<const __bf16 *>(a), static_cast<const __bf16 *>(b),
-                   reinterpret_cast<__bf16 *>(w + d.at), reinterpret_cast<__bf16 *>(w + d.bt), p.inp, p.out,
-                   a ? p.adapters * (divide_up(p.inp, columns) + divide_up(p.out, columns)) : 0, (int32_t)p.rank, pitch, columns};
-  const size_t counts = plan_words(p.adapters) * 4, tile = a ? (size_t)columns * (pitch + 2) * 2 : 0;
-  constexpr size_t kMostLds = plan_words(kMostAdapters) * 4;
-  if (counts > 48 * 1024 &&
-      hipFuncSetAttribute(reinterpret_cast<const void *>(k_plan), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMostLds) != hipSuccess)
+int run_plan(const nvfp4_adapters_params &p, const Layout &d, char *w, const int32_t *which, hipStream_t s) {
+  const size_t bytes = plan_words(p.adapters) * 4, most = plan_words(kMostAdapters) * 4;
+  if (bytes > 48 * 1024 &&
+      hipFuncSetAttribute(reinterpret_cast<const void *>(k_plan), hipFuncAttributeMaxDynamicSharedMemorySize, (int)most) != hipSuccess)
     return NVFP4_ERR_HIP;
-  return launch(k_plan, dim3((uint32_t)(1 + (g.units < 65536 ? g.units : 65536))), dim3(kPlanThreads), counts > tile ? counts : tile, s, g);
+  return launch(k_plan, dim3(1), dim3(kPlanThreads), bytes, s, PlanArgs{which, d.plan(w), (int32_t)p.tokens, (int32_t)p.adapters});
 }
 
-template <int RT, int NF>
+template <bool ACROSS, int RT, int NF>
 int run_shrink_of(ShrinkArgs g, const Layout &d, int64_t splits, hipStream_t s) {
   g.splits = (int32_t)splits;
-  if (d.few)
-    return launch(k_shrink<true, RT, NF>, dim3((uint32_t)g.tokens.T, (uint32_t)splits), dim3(kShrinkWaves * 64), 0, s, g);
+  if (d.few)                                     // (a backward pass has a plan)
+    return launch(k_shrink<!ACROSS, ACROSS, RT, NF>, dim3((uint32_t)g.tokens.T, (uint32_t)splits), dim3(kShrinkWaves * 64), 0, s, g);
   // two workgroups a compute unit where registers allow it
   const int64_t most = divide_up(RT * NF <= 8 ? 512 : 256, splits);
   g.single = 2 * d.tiles <= most;
   const dim3 grid((uint32_t)(g.single ? 2 * d.tiles : most), (uint32_t)(splits + (g.terms_of ? 1 : 0)));
-  return launch(k_shrink<false, RT, NF>, grid, dim3(kShrinkWaves * 64), 0, s, g);
+  return launch(k_shrink<false, ACROSS, RT, NF>, grid, dim3(kShrinkWaves * 64), 0, s, g);
 }
+template <bool ACROSS, int RT>
+int run_shrink_of(const ShrinkArgs &g, const Layout &d, int64_t splits, hipStream_t s) {
+  if (g.steps <= 2) return run_shrink_of<ACROSS, RT, 2>(g, d, splits, s);
+  if constexpr (!ACROSS || RT <= 4)
+    if (g.steps <= 4) return run_shrink_of<ACROSS, RT, 4>(g, d, splits, s);
+  if constexpr (!ACROSS && RT <= 4) return run_shrink_of<ACROSS, RT, 8>(g, d, splits, s);
+  return NVFP4_ERR_UNSUPPORTED;                  // (shrink_steps gives no more)
+}
+template <bool ACROSS>
 int run_shrink(const ShrinkArgs &g, const Layout &d, int64_t splits, hipStream_t s) {
-  if (g.rank <= 16)
-    return g.steps <= 2 ? run_shrink_of<1, 2>(g, d, splits, s) : g.steps <= 4 ? run_shrink_of<1, 4>(g, d, splits, s)
-                                                                             : run_shrink_of<1, 8>(g, d, splits, s);
-  if (g.rank <= 32)
-    return g.steps <= 2 ? run_shrink_of<2, 2>(g, d, splits, s) : g.steps <= 4 ? run_shrink_of<2, 4>(g, d, splits, s)
-                                                                             : run_shrink_of<2, 8>(g, d, splits, s);
-  if (g.rank <= 64)
-    return g.steps <= 2 ? run_shrink_of<4, 2>(g, d, splits, s) : g.steps <= 4 ? run_shrink_of<4, 4>(g, d, splits, s)
-                                                                             : run_shrink_of<4, 8>(g, d, splits, s);
-  return g.steps <= 2 ? run_shrink_of<8, 2>(g, d, splits, s) : run_shrink_of<8, 4>(g, d, splits, s);
+  if (g.rank <= 16) return run_shrink_of<ACROSS, 1>(g, d, splits, s);
+  if (g.rank <= 32) return run_shrink_of<ACROSS, 2>(g, d, splits, s);
+  if (g.rank <= 64) return run_shrink_of<ACROSS, 4>(g, d, splits, s);
+  return run_shrink_of<ACROSS, 8>(g, d, splits, s);
 }
 
-template <typename T, int F>
+template <int LIES, typename T, int F>
 int run_expand_of(ExpandArgs g, const Layout &d, hipStream_t s) {
   if (d.few) {
     const dim3 grid((uint32_t)g.tokens.T, (uint32_t)divide_up(g.width, kBlock * 4));
-    return launch(g.pitch % 8 ? k_expand<true, false, T, F> : k_expand<true, true, T, F>, grid, dim3(256), 0, s, g);
+    return launch(k_expand<LIES != kAcross, LIES, T, F>, grid, dim3(256), 0, s, g);             // (a backward pass has a plan)
   }
   constexpr int kWaves = expand_waves<false, T, F>;
   const int64_t across = g.out ? divide_up(g.width, kBlock * kWaves) : 1;
   const int64_t most = divide_up(F <= 1 ? 2048 : (F == 2 ? 1024 : 512) * (sizeof(T) == 4 ? 2 : 1), across);
   g.single = d.tiles <= most;
   const dim3 grid((uint32_t)(g.single ? d.tiles : most), (uint32_t)across);
-  return launch(g.pitch % 8 ? k_expand<false, false, T, F> : k_expand<false, true, T, F>, grid, dim3(kWaves * 64), 0, s, g);
+  return launch(k_expand<false, LIES, T, F>, grid, dim3(kWaves * 64), 0, s, g);
+}
+template <int LIES, typename T>
+int run_expand(const ExpandArgs &g, const Layout &d, hipStream_t s) {
+  if (g.rank <= 16) return run_expand_of<LIES, T, 0>(g, d, s);
+  if (g.rank <= 32) return run_expand_of<LIES, T, 1>(g, d, s);
+  if (g.rank <= 64) return run_expand_of<LIES, T, 2>(g, d, s);
+  return run_expand_of<LIES, T, 4>(g, d, s);
 }
 template <typename T>
 int run_expand(const ExpandArgs &g, const Layout &d, hipStream_t s) {
-  if (g.rank <= 16) return run_expand_of<T, 0>(g, d, s);
-  if (g.rank <= 32) return run_expand_of<T, 1>(g, d, s);
-  if (g.rank <= 64) return run_expand_of<T, 2>(g, d, s);
-  return run_expand_of<T, 4>(g, d, s);
+  return g.rank % 8 ? run_expand<kRagged, T>(g, d, s) : run_expand<kWhole, T>(g, d, s);
 }
 
 }  // namespace
@@ -1015,7 +1024,7 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
   char *const w = static_cast<char *>(workspace);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (!d.few)
-    if (const int rc = run_plan(*p, d, w, which, nullptr, nullptr, s)) return rc;
+    if (const int rc = run_plan(*p, d, w, which, s)) return rc;
   const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters};
   float *const parts = reinterpret_cast<float *>(w + d.parts);
   const int32_t rank = (int32_t)p->rank, pitch = (int32_t)Layout::pitch(*p);
@@ -1030,9 +1039,9 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
   g.rank = rank;
   g.pitch = pitch;
   g.steps = (int32_t)d.steps_in;
-  if (const int rc = run_shrink(g, d, d.splits_in, s)) return rc;
+  if (const int rc = run_shrink<false>(g, d, d.splits_in, s)) return rc;
   const ExpandArgs e{tokens, parts, d.splits_in == 1 ? nullptr : h, nullptr, static_cast<const __bf16 *>(b), scales, base, out,
-                     p->ld_base, p->ld_out, p->out, rank, rank, pitch, (int32_t)d.splits_in, 0, false};
+                     p->ld_base, p->ld_out, p->out, rank, pitch, (int32_t)d.splits_in, 0, false};
   return p->out_dtype == NVFP4_OUT_F32 ? run_expand<float>(e, d, s) : run_expand<__bf16>(e, d, s);
 }
 
@@ -1053,7 +1062,7 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
   char *const w = static_cast<char *>(workspace);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool any = p->tokens != 0;
-  if (const int rc = run_plan(*p, d, w, which, any ? a : nullptr, b, s)) return rc;
+  if (const int rc = run_plan(*p, d, w, which, s)) return rc;
   const Tokens tokens{which, d.plan(w), (int32_t)p->tokens, (int32_t)p->adapters};
   float *const parts = reinterpret_cast<float *>(w + d.parts);
   __bf16 *const terms_a = reinterpret_cast<__bf16 *>(w + d.terms_a), *const terms_b = reinterpret_cast<__bf16 *>(w + d.terms_b);
@@ -1064,12 +1073,12 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
                      {static_cast<const __bf16 *>(dy), terms_b, db, reinterpret_cast<float *>(w + d.parted_b), p->ld_dy, p->out,
                       (int32_t)divide_up(p->out, kOuterWidth), true}}};
   if (any) {
-    const ShrinkArgs dh{tokens, static_cast<const __bf16 *>(dy), reinterpret_cast<const __bf16 *>(w + d.bt), parts, nullptr, h, scales,
+    const ShrinkArgs dh{tokens, static_cast<const __bf16 *>(dy), static_cast<const __bf16 *>(b), parts, nullptr, h, scales,
                         terms_b, p->ld_dy, p->out, rank, pitch, (int32_t)d.steps_out, term_ranks, 0, false};
-    if (const int rc = run_shrink(dh, d, d.splits_out, s)) return rc;
-    const ExpandArgs e{tokens, parts, nullptr, terms_a, reinterpret_cast<const __bf16 *>(w + d.at), scales, dx_base, dx,
-                       p->ld_base, p->ld_out, p->inp, rank, pitch, pitch, (int32_t)d.splits_out, term_ranks, false};
-    if (const int rc = run_expand<__bf16>(e, d, s)) return rc;
+    if (const int rc = run_shrink<true>(dh, d, d.splits_out, s)) return rc;
+    const ExpandArgs e{tokens, parts, nullptr, terms_a, static_cast<const __bf16 *>(a), scales, dx_base, dx,
+                       p->ld_base, p->ld_out, p->inp, rank, pitch, (int32_t)d.splits_out, term_ranks, false};
+    if (const int rc = run_expand<kAcross, __bf16>(e, d, s)) return rc;
   }
   const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, rank <= 64 ? 1 : 2);
   if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
