@@ -24,7 +24,8 @@ namespace {
 constexpr int kMostRank = 128, kMostAdapters = 2048;
 constexpr int kTile = 32;                       // tokens of a planned tile
 constexpr int kFewTile = 16;                    // ... and of a tile that a workgroup finds for itself
-constexpr int kFewTokens = 256;                 // up to here there is no plan (find_tile)
+constexpr int kFewTokens = 192;                 // forwards, up to here there is no plan (find_tile)
+constexpr int kWholeTokens = 512;               // backwards, up to here an adapter's gradients are one workgroup's sums
 constexpr int kPlanThreads = 1024;
 constexpr int kOuterWidth = 128;                // columns of a workgroup of k_outer
 constexpr int kBlock = 64;                      // columns of a block of k_expand
@@ -704,6 +705,7 @@ struct OuterHalf {
 struct OuterArgs {
   Plan plan;
   int32_t L, rank, term_ranks, tiles;        // tiles of a range
+  bool whole;                  // ranges have whole adapters, those that begin among their tiles
   OuterHalf half[2];
 };
 
@@ -726,7 +728,13 @@ __global__ void __launch_bounds__(256, RT <= 2 ? 2 : 1) k_outer(OuterArgs a) {
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   const int64_t c0 = (int64_t)chunk * kOuterWidth, c = c0 + row * 8, size = f.width * a.rank;
   const __bf16 *const from = f.x + (c < f.width ? c : f.width - 8);          // (columns past the last are not kept)
-  const int32_t count = *a.plan.count, first = range * a.tiles, last = first + a.tiles < count ? first + a.tiles : count;
+  const int32_t count = *a.plan.count;
+  const auto boundary = [&](int32_t i) {
+    if (i >= count) return count;
+    const int32_t l = a.plan.tiles[i].adapter;
+    return !a.whole || l < 0 || a.plan.tile_begin[l] == i ? i : a.plan.tile_begin[l + 1];
+  };
+  const int32_t first = boundary(range * a.tiles), last = boundary((range + 1) * a.tiles);
   // eight columns of rank rank0 + r 16 + row, from c0 + (group 4 + wave) 8
   const auto put = [&](float *to, int r, const float *v) {
     const int rank = rank0 + r * 16 + row;
@@ -822,7 +830,7 @@ __global__ void __launch_bounds__(256, RT <= 2 ? 2 : 1) k_outer(OuterArgs a) {
         if (next < last) fetch_tokens(next);
       }
     }
-    const int64_t at = place(a.plan, adapter, range, a.tiles);
+    const int64_t at = a.whole ? -1 : place(a.plan, adapter, range, a.tiles);
     float *const to = at < 0 ? f.out + adapter * size : f.parted + at * size;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -878,7 +886,7 @@ int64_t divide_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // How a call's work is dealt out, and what it needs of the workspace: all of it follows from the sizes.
 struct Layout {
-  bool few;
+  bool few, whole;
   int64_t tiles;               // at most so many planned tiles
   int64_t steps_in, steps_out, splits_in, splits_out;        // of k_shrink's sums over inp (h), over out (dh)
   int64_t ranges, range_tiles; // of k_outer
@@ -896,6 +904,7 @@ struct Layout {
   static int64_t splits(int64_t steps, int64_t width) { return divide_up(divide_up(width, 32), steps * kShrinkWaves); }
   Layout(const nvfp4_adapters_params &p, bool backward) {
     few = !backward && p.tokens <= kFewTokens;
+    whole = p.tokens <= kWholeTokens;
     tiles = p.tokens / kTile + (p.adapters + 1 < p.tokens ? p.adapters + 1 : p.tokens);
     steps_in = shrink_steps(p.tokens, few, p.inp, p.rank, false);
     steps_out = shrink_steps(p.tokens, few, p.out, p.rank, true);
@@ -922,8 +931,8 @@ struct Layout {
     if (backward) {
       terms_a = take(tiles * 3 * term_ranks(p) * kTile * 2);
       terms_b = take(tiles * 3 * term_ranks(p) * kTile * 2);
-      parted_a = take(2 * ranges * p.rank * p.inp * 4);
-      parted_b = take(2 * ranges * p.rank * p.out * 4);
+      parted_a = take(whole ? 0 : 2 * ranges * p.rank * p.inp * 4);
+      parted_b = take(whole ? 0 : 2 * ranges * p.rank * p.out * 4);
     }
     bytes = end;
   }
@@ -1067,7 +1076,7 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
   float *const parts = reinterpret_cast<float *>(w + d.parts);
   __bf16 *const terms_a = reinterpret_cast<__bf16 *>(w + d.terms_a), *const terms_b = reinterpret_cast<__bf16 *>(w + d.terms_b);
   const int32_t rank = (int32_t)p->rank, pitch = (int32_t)Layout::pitch(*p), term_ranks = (int32_t)Layout::term_ranks(*p);
-  const OuterArgs g{d.plan(w), (int32_t)p->adapters, rank, term_ranks, (int32_t)d.range_tiles,
+  const OuterArgs g{d.plan(w), (int32_t)p->adapters, rank, term_ranks, (int32_t)d.range_tiles, d.whole,
                     {{static_cast<const __bf16 *>(x), terms_a, da, reinterpret_cast<float *>(w + d.parted_a), p->ld_x, p->inp,
                       (int32_t)divide_up(p->inp, kOuterWidth), false},
                      {static_cast<const __bf16 *>(dy), terms_b, db, reinterpret_cast<float *>(w + d.parted_b), p->ld_dy, p->out,
@@ -1082,7 +1091,7 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
   }
   const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, rank <= 64 ? 1 : 2);
   if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
-  if (d.ranges == 1) return NVFP4_OK;
+  if (d.whole || d.ranges == 1) return NVFP4_OK;
   const int64_t most = divide_up(p->rank * (p->inp > p->out ? p->inp : p->out), 1024);
   return launch(k_join, dim3((uint32_t)(most < 256 ? most : 256), (uint32_t)p->adapters, 2), dim3(256), 0, s, g);
 }
