@@ -87,7 +87,13 @@ struct Row {
   }
   // (a row's bytes fit 32 bits, which leaves an address one register a thread)
   __device__ u32x4 load(int32_t v) const { return *reinterpret_cast<const u32x4 *>(at + (uint32_t)v * 16u); }
-  __device__ void store(int32_t v, const float *x) const { *reinterpret_cast<u32x4 *>(at + (uint32_t)v * 16u) = pack<T>(x); }
+  template <bool PAST>
+  __device__ void store(int32_t v, const float *x) const {
+    if constexpr (PAST)
+      __builtin_nontemporal_store(pack<T>(x), reinterpret_cast<u32x4 *>(at + (uint32_t)v * 16u));
+    else
+      *reinterpret_cast<u32x4 *>(at + (uint32_t)v * 16u) = pack<T>(x);
+  }
   // The edge element of a thread, counted from the first whole piece; kNoEdge: it has none.
   static constexpr int64_t kNoEdge = INT64_MIN;
   __device__ int64_t edge(int32_t thread) const {
@@ -298,7 +304,7 @@ __global__ void __launch_bounds__(NT) k_distill_forward(DistillArgs a) {
 }
 
 // `per` pieces of a row for a workgroup.
-template <typename T, int NT>
+template <typename T, int NT, bool PAST>
 __global__ void __launch_bounds__(NT) k_distill_backward(DistillArgs a, int32_t per) {
   constexpr int kAhead = 4, kPer = Row<T>::kPer;
   const List list(a.top);
@@ -327,14 +333,14 @@ __global__ void __launch_bounds__(NT) k_distill_backward(DistillArgs a, int32_t 
     }
     if (v0 + NT * kAhead < last) fetch(v0 + NT * kAhead);
     for (int i = 0; i < kAhead; ++i)
-      if (v0 + i * NT < last) d.store(v0 + i * NT, x[i]);
+      if (v0 + i * NT < last) d.template store<PAST>(v0 + i * NT, x[i]);
   }
   if (const int64_t e = r.edge(threadIdx.x); e != Row<T>::kNoEdge && (e < 0 ? begins : ends)) set_element<T>(d.at, e, of(element<T>(r.at, e)));
   __syncthreads();
   rewrite_list<T, NT>(list, a, row, word0, word1, g, [&](float z) { return probability(z, a.inv_t, lse); });
 }
 
-template <typename T, int NT>
+template <typename T, int NT, bool PAST>
 __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
   constexpr int kPer = Row<T>::kPer;
   __shared__ Scratch<NT> sh;
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
     float x[kPer];
     unpack<T>(r.load(v), x);
     for (int k = 0; k < kPer; ++k) x[k] = of(x[k]);
-    d.store(v, x);
+    d.template store<PAST>(v, x);
   }
   if (const int64_t e = r.edge(threadIdx.x); e != Row<T>::kNoEdge) set_element<T>(d.at, e, of(element<T>(r.at, e)));
   __syncthreads();
@@ -363,7 +369,7 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
 // The same with the row in registers, NV pieces a thread.  A workgroup takes row after row: where a piece of the gradient has been
 // written, that piece of the next row is asked for, and kLag pieces later it enters the next row's sum.  So loads and stores are on
 // their way together, and the exponentials of both passes lie over them.
-template <typename T, int NT, int NV>
+template <typename T, int NT, int NV, bool PAST>
 __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows) {
   constexpr int kPer = Row<T>::kPer, kLag = NV / 4;
   __shared__ Scratch<NT> sh[2];                  // (and two lists: each is written again two barriers after it was read)
@@ -423,7 +429,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows
       asm("" : "+v"(w[i]));
       unpack<T>(w[i], x);
       for (int k = 0; k < kPer; ++k) x[k] = any ? gs * exp2_diff(x[k], most, a.c) : 0.0f;
-      if (v < r.pieces) d.store(v, x);
+      if (v < r.pieces) d.template store<PAST>(v, x);
       if (more) fetch(then, i);
       __builtin_amdgcn_sched_barrier(0);
       if (more && i >= kLag) sum(then, i - kLag, run);
@@ -476,22 +482,36 @@ DistillArgs args(const void *logits, const nvfp4_distill_params *p, const void *
 
 constexpr int kComputeUnits = 256;
 
-template <typename T, int NT, int NV>
+template <typename T, int NT, int NV, bool PAST>
 int run_rows(const DistillArgs &a, int64_t rows, int per_cu, hipStream_t s) {
   const int64_t most = (int64_t)kComputeUnits * per_cu;
-  return launch(k_distill_rows<T, NT, NV>, dim3((uint32_t)(rows < most ? rows : most)), dim3(NT), 2 * list_bytes(a.top), s, a, (int32_t)rows);
+  return launch(k_distill_rows<T, NT, NV, PAST>, dim3((uint32_t)(rows < most ? rows : most)), dim3(NT), 2 * list_bytes(a.top), s, a,
+                (int32_t)rows);
 }
-template <typename T>
+template <typename T, bool PAST>
 int run_step(const DistillArgs &a, int64_t rows, hipStream_t s) {
-  constexpr int64_t kPer = 16 / sizeof(T);
-  const int64_t pieces = a.vocab / kPer;         // (whole ones, at most)
-  if (pieces <= 256 * 4) return run_rows<T, 256, 4>(a, rows, 8, s);
-  if (pieces <= 256 * 8) return run_rows<T, 256, 8>(a, rows, 7, s);
-  if (pieces <= 256 * 16) return run_rows<T, 256, 16>(a, rows, 4, s);
-  if (pieces <= 512 * 16) return run_rows<T, 512, 16>(a, rows, 2, s);
-  if (pieces <= 1024 * 16) return run_rows<T, 1024, 16>(a, rows, 1, s);
-  return launch(k_distill_step<T, 1024>, dim3((uint32_t)rows), dim3(1024), list_bytes(a.top), s, a);
+  const int64_t pieces = a.vocab / (int64_t)(16 / sizeof(T));        // (whole ones, at most)
+  if (pieces <= 256 * 4) return run_rows<T, 256, 4, PAST>(a, rows, 8, s);
+  if (pieces <= 256 * 8) return run_rows<T, 256, 8, PAST>(a, rows, 7, s);
+  if (pieces <= 256 * 16) return run_rows<T, 256, 16, PAST>(a, rows, 4, s);
+  if (pieces <= 512 * 16) return run_rows<T, 512, 16, PAST>(a, rows, 2, s);
+  if (pieces <= 1024 * 16) return run_rows<T, 1024, 16, PAST>(a, rows, 1, s);
+  return launch(k_distill_step<T, 1024, PAST>, dim3((uint32_t)rows), dim3(1024), list_bytes(a.top), s, a);
 }
+template <typename T, bool PAST>
+int run_backward(const DistillArgs &a, int64_t rows, hipStream_t s) {
+  const int64_t per = 16 / sizeof(T), pieces = a.vocab / per > 0 ? a.vocab / per : 1;      // (whole ones, at most)
+  // few rows: several workgroups a row, of 1024 pieces at least
+  int64_t splits = 1;
+  while (splits < 256 && rows * splits < 512 && pieces / (2 * splits) >= 1024) splits *= 2;
+  return launch(k_distill_backward<T, 256, PAST>, dim3((uint32_t)rows, (uint32_t)splits), dim3(256), list_bytes(a.top), s, a,
+                (int32_t)((pieces + splits - 1) / splits));
+}
+
+// A gradient that the device's last cache (256 MB) can hardly hold for its reader is written past the caches, which leaves them to the
+// logits.  Gradient and step in us, through / past: 8192 x 16001 BF16 (262 MB) 124 / 100 and 155 / 138, 4096 x 65536 (537 MB) 227 / 215 and
+// 242 / 236, 4096 x 50021 fp32 365 / 349 and 374 / 362; but 1024 x 32768 fp32 (134 MB) 45 / 56, a step of 255 x 50021 fp32 (51 MB) 22 / 25.
+bool past_caches(const nvfp4_distill_params *p) { return p->rows * p->vocab * (p->x_dtype ? 4 : 2) > (int64_t)192 << 20; }
 
 }  // namespace
 }  // namespace nvfp4_46
@@ -521,13 +541,9 @@ extern "C" int nvfp4_distill_backward(const void *logits, const nvfp4_distill_pa
   a.lse_in = lse;
   a.weight = weight;
   a.dlogits = dlogits;
-  const int64_t per = p->x_dtype ? 4 : 8, pieces = p->vocab / per > 0 ? p->vocab / per : 1;      // (whole ones, at most)
-  // few rows: several workgroups a row, of 1024 pieces at least
-  int64_t splits = 1;
-  while (splits < 256 && p->rows * splits < 512 && pieces / (2 * splits) >= 1024) splits *= 2;
-  return launch(p->x_dtype ? k_distill_backward<float, 256> : k_distill_backward<__bf16, 256>,
-                dim3((uint32_t)p->rows, (uint32_t)splits), dim3(256), list_bytes(p->top), static_cast<hipStream_t>(stream), a,
-                (int32_t)((pieces + splits - 1) / splits));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (past_caches(p)) return p->x_dtype ? run_backward<float, true>(a, p->rows, s) : run_backward<__bf16, true>(a, p->rows, s);
+  return p->x_dtype ? run_backward<float, false>(a, p->rows, s) : run_backward<__bf16, false>(a, p->rows, s);
 }
 
 extern "C" int nvfp4_distill_step(const void *logits, const nvfp4_distill_params *p, const void *teacher, const void *index,
@@ -542,5 +558,6 @@ extern "C" int nvfp4_distill_step(const void *logits, const nvfp4_distill_params
   a.weight = weight;
   a.dlogits = dlogits;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  return p->x_dtype ? run_step<float>(a, p->rows, s) : run_step<__bf16>(a, p->rows, s);
+  if (past_caches(p)) return p->x_dtype ? run_step<float, true>(a, p->rows, s) : run_step<__bf16, true>(a, p->rows, s);
+  return p->x_dtype ? run_step<float, false>(a, p->rows, s) : run_step<__bf16, false>(a, p->rows, s);
 }
