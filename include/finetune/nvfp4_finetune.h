@@ -57,7 +57,7 @@ size_t nvfp4_adapters_workspace_bytes(const nvfp4_adapters_params *p, int backwa
  *   which      in   [tokens] int32
  *   scales     in   [adapters] fp32
  *   h          out  [tokens][rank] fp32, dense, for the backward pass; or NULL
- *   out        out  [tokens][out]; may be base itself (with the same stride), no other input
+ *   out        out  [tokens][out]; may be base itself (with the same stride, else ERR_SHAPE), no other input
  *   workspace  scratch, 16-byte aligned; holds nothing between calls.  Calls whose work may overlap need one each.
  * Errors: NULL pointer -> ERR_NULL; sizes or strides out of range -> ERR_SHAPE; a buffer that is not 16-byte aligned (which, scales
  * and h: 4 bytes) or a stride that is no multiple of 8 -> ERR_ALIGN; out_dtype, or workspace too small -> ERR_PARAM.  */
@@ -69,7 +69,7 @@ int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params *p, const 
  *   dy       in   [tokens][out] BF16
  *   x        in   [tokens][inp] BF16, and h [tokens][rank] as the forward pass left it
  *   dx_base  in   [tokens][inp] BF16: the gradient through the shared projection, or NULL for 0
- *   dx       out  [tokens][inp] BF16; may be dx_base itself (with the same stride); NULL if it is not wanted
+ *   dx       out  [tokens][inp] BF16; may be dx_base itself (with the same stride, else ERR_SHAPE); NULL if it is not wanted
  *   da, db   out  [adapters][rank][inp] and [adapters][out][rank] fp32, dense; 0 for an adapter without tokens
  * Errors: as above.                                                                                             */
 int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_params *p, const void *x, const float *h, const void *a,

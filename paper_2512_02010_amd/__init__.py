@@ -8,11 +8,11 @@ back to a CPU implementation.
 """
 from . import workloads  # noqa: F401
 
-__all__ = ["workloads", "binding", "build", "finetune"]
+__all__ = ["workloads", "binding", "build", "finetune", "recover"]
 
 
 def __getattr__(name):
-    if name in ("binding", "build", "finetune"):
+    if name in ("binding", "build", "finetune", "recover"):
         import importlib
         return importlib.import_module(f"{__name__}.{name}")
     raise AttributeError(name)

@@ -13,6 +13,10 @@
 //   k_expand   base + s [T][rank] times [width][rank]                 out from h and B, dx from dh / s and A
 //   k_outer    s [T][rank] times [T][width] over an adapter's tokens  dA from dh / s and x, dB from h and dy
 //   k_join     sums what several workgroups of k_outer have of one adapter, in a fixed order
+//
+// Forwards that is two launches up to kFewTokens tokens and three beyond, backwards four and five.  Whole calls, among others:
+// 16384 tokens, 4096 x 4096, rank 16, four adapters 116 us (405 MB: 3.5 TB/s, a copy 5.1), of which plan 9, shrink 39, expand 69; backwards 8192
+// tokens, 8192 x 8192, rank 32, eight adapters 205 us (563 MB): plan 8, shrink 37, expand 79, outer 78, join 6.  One token 8.5 us: two launches.
 #include <hip/hip_runtime.h>
 
 #include "finetune/nvfp4_finetune.h"
@@ -21,11 +25,15 @@
 namespace nvfp4_46 {
 namespace {
 
-constexpr int kMostRank = 128, kMostAdapters = 2048;
+constexpr int kMostRank = 128, kMostAdapters = 2048;          // (by the instances of the kernels, by the LDS of k_plan)
 constexpr int kTile = 32;                       // tokens of a planned tile
 constexpr int kFewTile = 16;                    // ... and of a tile that a workgroup finds for itself
-constexpr int kFewTokens = 192;                 // forwards, up to here there is no plan (find_tile)
-constexpr int kWholeTokens = 512;               // backwards, up to here an adapter's gradients are one workgroup's sums
+// Forwards, up to here there is no plan (find_tile).  Without / with one, 4096 x 4096, rank 16, 16 adapters: 96 tokens 8.7 / 15.2 us, 192
+// 10.5 / 15.8, 256 17.4 / 15.6; 8192 x 8192, rank 64, 32 adapters: 128 tokens 28.0 / 29.0, 256 43 / 29.
+constexpr int kFewTokens = 192;
+// Backwards, up to here an adapter's gradients are one workgroup's sums and k_join is not needed.  4096 x 4096, rank 16: 256 tokens of
+// one adapter 20.6 us so, 22.7 with k_join, 512 tokens of 16 adapters 32.0 / 35.4, 512 of one 23.3 / 23.5.
+constexpr int kWholeTokens = 512;
 constexpr int kPlanThreads = 1024;
 constexpr int kOuterWidth = 128;                // columns of a workgroup of k_outer
 constexpr int kBlock = 64;                      // columns of a block of k_expand
@@ -71,30 +79,15 @@ __device__ inline int32_t adapter_of(const int32_t *which, int32_t t, int32_t L)
 // ---- tiles ----------------------------------------------------------------------------------------------------------
 
 struct TileTokens {
-  int32_t token[kTile];
+  int32_t token[kFewTile];
   uint64_t same[kFewTokens / 64];               // tokens of this workgroup's adapter, a bit each
 };
 
-// The tile of `index` in `shared`, as (count, adapter); count 0: there is none.  All threads of the workgroup call it.  With a plan
-// the index is that of a tile (rows == 16: of half a tile).  Without, it is a token's: the token leads a tile if a multiple of 16 of
-// the tokens before it have its adapter, and the next of them go with it.
-template <bool FEW, int NT>
-__device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t index, int rows) {
-  Tile t{-1, 0};
-  if constexpr (!FEW) {
-    // (the three are asked for together; past the last tile they hold anything)
-    const int halves = kTile / rows, tile = index / halves;
-    const int32_t tiles = *k.plan.count, token = (int)threadIdx.x < rows ? k.plan.order[(int64_t)index * rows + threadIdx.x] : 0;
-    t = k.plan.tiles[tile];
-    if (tile >= tiles) return {-1, 0};
-    t.count -= index % halves * rows;
-    if (t.count <= 0) return {-1, 0};
-    if (t.count > rows) t.count = rows;
-    if ((int)threadIdx.x < rows) shared.token[threadIdx.x] = token;
-    __syncthreads();
-    return t;
-  }
-  t.adapter = adapter_of(k.which, index, k.L);
+// Without a plan: the tile that the token `index` leads, its tokens in `shared`; count 0: it leads none.  All threads of the workgroup
+// call it.  A token leads a tile if a multiple of 16 of the tokens before it have its adapter, and the next of them go with it.
+template <int NT>
+__device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t index) {
+  Tile t{adapter_of(k.which, index, k.L), 0};
   for (int32_t i = threadIdx.x; i < kFewTokens; i += NT) {          // (whole waves: NT and kFewTokens are multiples of 64)
     const bool same = i < k.T && adapter_of(k.which, i, k.L) == t.adapter;
     const uint64_t mask = __ballot(same);
@@ -107,7 +100,7 @@ __device__ inline Tile find_tile(const Tokens &k, TileTokens &shared, int32_t in
     return n;
   };
   const int32_t mine = before(index);
-  if (mine % kFewTile) return {-1, 0};
+  if (mine % kFewTile) return t;
   int32_t all = 0;
   for (int w = 0; w < kFewTokens / 64; ++w) all += __popcll(shared.same[w]);
   t.count = all - mine < kFewTile ? all - mine : kFewTile;
@@ -158,9 +151,11 @@ struct ShrinkArgs {
 
 constexpr int kShrinkWaves = 8;
 
-// D[token][rank]: rows of x against rows of w (ACROSS: its columns, turned in LDS once an adapter).  A wave has its own columns and keeps their part of w
-// in registers while it goes through 16 tokens at a time of the workgroup's stretch of the plan; the waves' sums meet in LDS.  A load has
-// 64 adjacent bytes of 16 rows; the columns of the next tokens are on their way while these are multiplied.
+// D[token][rank]: rows of x against rows of w (ACROSS: its columns, turned in LDS once an adapter).  A wave has its own columns and keeps
+// their part of w in registers while it goes through 16 tokens at a time of the workgroup's stretch of the plan; the waves' sums meet in
+// LDS.  A load has 64 adjacent bytes of 16 rows; the columns of the next tokens are on their way while these are multiplied.
+// Bound by the loads of x.  16384 x 4096 (134 MB) by itself: 29 us at rank 16, 33 at 32, 39 at 64, 53 at 128; the loads alone 22.5 to 25.  With
+// w read again for every tile, through the L2, it was 35 to 44 at rank 16 and 52 at 64.
 template <bool FEW, bool ACROSS, int RT, int NF>
 __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 && !(ACROSS && RT == 4) ? 4 : 2) k_shrink(ShrinkArgs a) {
   constexpr int kThreads = kShrinkWaves * 64, kBuffers = RT <= 4 ? 2 : 1;
@@ -171,7 +166,7 @@ __global__ void __launch_bounds__(kShrinkWaves * 64, RT * NF <= 8 && !(ACROSS &&
   int32_t first = 0, last = 1, token = 0;        // 16 tokens each
   int32_t adapter_here = -1, count_here = 0;     // of the only tile
   if constexpr (FEW) {
-    const Tile t = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, 16);
+    const Tile t = find_tile<kThreads>(a.tokens, shared, blockIdx.x);
     if (t.count == 0) return;
     adapter_here = t.adapter;
     count_here = t.count;
@@ -371,10 +366,12 @@ struct Columns {
 };
 
 // D[column][token]: rows of w against s h, which enters as terms (term).  Row 4 a + b of product p of a block is column
-// 32 (p / 2) + 8 a + 4 (p % 2) + b, so that a lane ends up with twice 8 adjacent columns of its token, 64 bytes in four lanes.  The summed index of a product is four pieces of
-// eight ranks: F > 0: 32 ranks of one term, F times.  F == 0, rank <= 16: the one or two pieces of every term side by side.
+// 32 (p / 2) + 8 a + 4 (p % 2) + b, so that a lane ends up with twice 8 adjacent columns of its token, 64 bytes in four lanes.  The
+// summed index of a product is four pieces of eight ranks: F > 0: 32 ranks of one term, F times.  F == 0, rank <= 16: the one or two pieces
+// of every term side by side.
 // A wave has a block of columns of its own and keeps their part of w in registers while it goes through the workgroup's stretch of the
 // plan; per tile the workgroup sums the parts of s h and splits them once, into LDS, while the tile's columns of base are on their way.
+// Bound by base and out.  16384 x 4096 BF16 (268 MB) by itself: 65 us up to rank 32, 76 at 64, 101 at 128; a copy of as much 57.
 // Eight waves a workgroup, two workgroups a compute unit, where 128 registers are enough for it; else four waves and three.
 template <bool FEW, typename T, int F>
 constexpr int expand_waves = !FEW && sizeof(T) == 2 ? 8 : 4;
@@ -390,7 +387,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
   int32_t first = 0, last = 1, in[MT];           // in: this lane's token of each 16, -1: there is none
   int32_t adapter_here = -1, count_here = 0;     // of the only tile
   if constexpr (FEW) {
-    const Tile t = find_tile<true, kThreads>(a.tokens, shared, blockIdx.x, kRows);
+    const Tile t = find_tile<kThreads>(a.tokens, shared, blockIdx.x);
     if (t.count == 0) return;
     adapter_here = t.adapter;
     count_here = t.count;
@@ -578,7 +575,8 @@ struct PlanArgs {
   int32_t T, L;
 };
 
-// Stable counting sort by one workgroup, each wave its own stretch of the tokens, 64 at a time.
+// Stable counting sort by one workgroup, each wave its own stretch of the tokens, 64 at a time, or 256 where they have one adapter.
+// Bound by the instructions of its sixteen waves: 5 us for 2048 tokens, 9 for 16384 in segments (17 at 64 at a time).
 __global__ void __launch_bounds__(kPlanThreads) k_plan(PlanArgs p) {
   extern __shared__ int32_t counts[];            // [16][groups + 1]: each wave's tokens of a group, then how many come before them
   const int32_t groups = p.L + 1, line = groups + 1;
@@ -892,8 +890,9 @@ struct Layout {
   int64_t ranges, range_tiles; // of k_outer
   int64_t count, tile_begin, order, table, parts, terms_a, terms_b, parted_a, parted_b, bytes;   // byte offsets
 
-  // Steps of 32 columns that a wave of k_shrink keeps w of in registers: as many as fit (ranks), fewer where there would not be
-  // workgroups for the compute units, but not below two.  The splits of the sum follow.
+  // Steps of 32 columns that a wave of k_shrink keeps w of in registers: as many as fit (ranks; ACROSS needs more of them to turn w),
+  // fewer where there would not be workgroups for half of the compute units, but not below two.  The splits of the sum follow: each
+  // is one more part for k_expand to add up.
   static int64_t shrink_steps(int64_t tokens, bool few, int64_t width, int64_t rank, bool across) {
     const int64_t all = divide_up(width, 32), groups = few ? divide_up(tokens, 4) : divide_up(tokens, 16);
     int64_t steps = (rank <= 64 ? 8 : 4) / (across ? 2 : 1);
@@ -1022,7 +1021,7 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
   if (!p || !a || !b || !scales || !workspace) return NVFP4_ERR_NULL;
   if (p->tokens != 0 && (!x || !which || !out)) return NVFP4_ERR_NULL;
   if (!sizes_fit(*p) || !stride_fits(p->ld_x, p->inp, p->tokens) || (base && !stride_fits(p->ld_base, p->out, p->tokens)) ||
-      !stride_fits(p->ld_out, p->out, p->tokens))
+      !stride_fits(p->ld_out, p->out, p->tokens) || (base == out && p->ld_base != p->ld_out))
     return NVFP4_ERR_SHAPE;
   if (!at(x, 16) || !at(base, 16) || !at(a, 16) || !at(b, 16) || !at(out, 16) || !at(workspace, 16) || !at(which, 4) ||
       !at(scales, 4) || !at(h, 4) || p->ld_x % 8 || (base && p->ld_base % 8) || p->ld_out % 8)
@@ -1060,7 +1059,8 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
   if (!p || !a || !b || !scales || !da || !db || !workspace) return NVFP4_ERR_NULL;
   if (p->tokens != 0 && (!dy || !x || !h || !which)) return NVFP4_ERR_NULL;
   if (!sizes_fit(*p) || !stride_fits(p->ld_x, p->inp, p->tokens) || !stride_fits(p->ld_dy, p->out, p->tokens) ||
-      (dx && dx_base && !stride_fits(p->ld_base, p->inp, p->tokens)) || (dx && !stride_fits(p->ld_out, p->inp, p->tokens)))
+      (dx && dx_base && !stride_fits(p->ld_base, p->inp, p->tokens)) || (dx && !stride_fits(p->ld_out, p->inp, p->tokens)) ||
+      (dx && dx_base == dx && p->ld_base != p->ld_out))
     return NVFP4_ERR_SHAPE;
   if (!at(dy, 16) || !at(x, 16) || !at(a, 16) || !at(b, 16) || !at(dx_base, 16) || !at(dx, 16) || !at(da, 16) || !at(db, 16) ||
       !at(workspace, 16) || !at(h, 4) || !at(which, 4) || !at(scales, 4) || p->ld_x % 8 || p->ld_dy % 8 ||

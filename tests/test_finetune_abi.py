@@ -42,14 +42,14 @@ def _adapters(**kw):
 
 
 def _forward(p, room=1 << 30, **kw):
-    v = dict(x=P, base=P, a=P, b=P, which=P, scales=P, h=None, out=P, workspace=P)
+    v = dict(x=P, base=P, a=P, b=P, which=P, scales=P, h=None, out=2 * P, workspace=P)
     v.update(kw)
     return F.lib().nvfp4_adapters_forward(v["x"], C.byref(p) if p else None, v["base"], v["a"], v["b"], v["which"], v["scales"], v["h"],
                                           v["out"], v["workspace"], room, None)
 
 
 def _backward(p, room=1 << 30, **kw):
-    v = dict(dy=P, x=P, h=P, a=P, b=P, which=P, scales=P, dx_base=P, dx=P, da=P, db=P, workspace=P)
+    v = dict(dy=P, x=P, h=P, a=P, b=P, which=P, scales=P, dx_base=P, dx=2 * P, da=P, db=P, workspace=P)
     v.update(kw)
     return F.lib().nvfp4_adapters_backward(v["dy"], C.byref(p) if p else None, v["x"], v["h"], v["a"], v["b"], v["which"], v["scales"],
                                            v["dx_base"], v["dx"], v["da"], v["db"], v["workspace"], room, None)
@@ -78,6 +78,8 @@ def test_refusals_of_the_adapters():
     assert _backward(_adapters(ld_base=64, ld_out=64, ld_dy=16)) == 2
     assert _backward(_adapters(ld_base=64, ld_out=64, ld_dy=36)) == 3
     assert _forward(_adapters(out_dtype=2)) == 4
+    # in place, but with another stride
+    assert _forward(_adapters(ld_out=40), base=P, out=P) == 2 and _backward(_adapters(ld_base=64, ld_out=72), dx_base=P, dx=P) == 2
     assert _forward(_adapters(), h=P + 2) == 3 and _forward(_adapters(), base=P + 4) == 3
     assert _backward(_adapters(**back), dx=P + 4) == 3 and _backward(_adapters(**back), dx_base=P + 4) == 3
     for p in (None, _adapters(rank=0), _adapters(inp=12), _adapters(tokens=-1)):
