@@ -76,6 +76,9 @@ __device__ inline void set_element(void *p, int64_t i, float x) {
     static_cast<__bf16 *>(p)[i] = (__bf16)x;
 }
 
+// What goes past the caches (past_caches).
+enum { kThrough, kLoads, kBoth };
+
 template <typename T>
 struct Row {
   static constexpr int kPer = 16 / sizeof(T);
@@ -91,10 +94,15 @@ struct Row {
     at = const_cast<char *>(p) + before * (int64_t)sizeof(T);
   }
   // (a row's bytes fit 32 bits, which leaves an address one register a thread)
-  __device__ u32x4 load(int32_t v) const { return *reinterpret_cast<const u32x4 *>(at + (uint32_t)v * 16u); }
-  template <bool PAST>
+  template <int PAST = kThrough>
+  __device__ u32x4 load(int32_t v) const {
+    const u32x4 *const p = reinterpret_cast<const u32x4 *>(at + (uint32_t)v * 16u);
+    if constexpr (PAST >= kLoads) return __builtin_nontemporal_load(p);
+    return *p;
+  }
+  template <int PAST>
   __device__ void store(int32_t v, const float *x) const {
-    if constexpr (PAST)
+    if constexpr (PAST >= kBoth)
       __builtin_nontemporal_store(pack<T>(x), reinterpret_cast<u32x4 *>(at + (uint32_t)v * 16u));
     else
       *reinterpret_cast<u32x4 *>(at + (uint32_t)v * 16u) = pack<T>(x);
@@ -310,7 +318,7 @@ __global__ void __launch_bounds__(NT) k_distill_forward(DistillArgs a) {
 
 // `per` pieces of a row for a workgroup.  The next pieces are asked for before these are written; the first before the list is read, which
 // takes two turns to memory (2047 x 50021 BF16: 97 us, one piece at a time and after the list 113).
-template <typename T, int NT, bool PAST>
+template <typename T, int NT, int PAST>
 __global__ void __launch_bounds__(NT) k_distill_backward(DistillArgs a, int32_t per) {
   constexpr int kAhead = 4, kPer = Row<T>::kPer;
   const List list(a.top);
@@ -324,7 +332,7 @@ __global__ void __launch_bounds__(NT) k_distill_backward(DistillArgs a, int32_t 
   const float lse = a.lse_in[row], g = a.weight ? a.weight[row] * a.inv_t : a.inv_t;
   u32x4 w[kAhead];
   const auto fetch = [&](int32_t v0) {
-    for (int i = 0; i < kAhead; ++i) w[i] = r.load(v0 + i * NT < last ? v0 + i * NT : last - 1);
+    for (int i = 0; i < kAhead; ++i) w[i] = r.template load<PAST>(v0 + i * NT < last ? v0 + i * NT : last - 1);
   };
   if (first < last) fetch(first + threadIdx.x);
   if (threadIdx.x < 64) read_list<T>(list, a, row, word0, word1);
@@ -348,7 +356,7 @@ __global__ void __launch_bounds__(NT) k_distill_backward(DistillArgs a, int32_t 
 
 // Sum and gradient of a row too long for registers (k_distill_rows), which is read twice: 2048 x 151936 BF16 289 us (4.3 TB/s of the bytes
 // that it would take once).
-template <typename T, int NT, bool PAST>
+template <typename T, int NT, int PAST>
 __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
   constexpr int kPer = Row<T>::kPer;
   __shared__ Scratch<NT> sh;
@@ -365,7 +373,7 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
   const auto of = [&](float z) { return any ? g * probability(z, a.inv_t, lse) : 0.0f; };
   for (int32_t v = threadIdx.x; v < r.pieces; v += NT) {
     float x[kPer];
-    unpack<T>(r.load(v), x);
+    unpack<T>(r.template load<PAST>(v), x);
     for (int k = 0; k < kPer; ++k) x[k] = of(x[k]);
     d.template store<PAST>(v, x);
   }
@@ -378,7 +386,7 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
 // written, that piece of the next row is asked for, and kLag pieces later it enters the next row's sum.  So loads and stores are on
 // their way together, and the exponentials of both passes lie over them.  4096 x 131072 BF16: read twice 656 us, in registers 533, with
 // the next row's sum between the stores 477.
-template <typename T, int NT, int NV, bool PAST>
+template <typename T, int NT, int NV, int PAST>
 __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows) {
   constexpr int kPer = Row<T>::kPer, kLag = NV / 4;
   __shared__ Scratch<NT> sh[2];                  // (and two lists: each is written again two barriers after it was read)
@@ -387,7 +395,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows
   int32_t thread = threadIdx.x;
   const auto fetch = [&](const Row<T> &of, int i) {              // (pieces past the last: the last once more)
     const int32_t v = thread + i * NT;
-    if (of.pieces > 0) w[i] = of.load(v < of.pieces ? v : of.pieces - 1);
+    if (of.pieces > 0) w[i] = of.template load<PAST>(v < of.pieces ? v : of.pieces - 1);
   };
   const auto fetch_edge = [&](const Row<T> &of) {
     if (const int64_t e = of.edge(threadIdx.x); e != Row<T>::kNoEdge) edge = element<T>(of.at, e);
@@ -491,13 +499,13 @@ DistillArgs args(const void *logits, const nvfp4_distill_params *p, const void *
 
 constexpr int kComputeUnits = 256;            // of an MI355X: where there are others, only how rows are dealt out is less even
 
-template <typename T, int NT, int NV, bool PAST>
+template <typename T, int NT, int NV, int PAST>
 int run_rows(const DistillArgs &a, int64_t rows, int per_cu, hipStream_t s) {
   const int64_t most = (int64_t)kComputeUnits * per_cu;
   return launch(k_distill_rows<T, NT, NV, PAST>, dim3((uint32_t)(rows < most ? rows : most)), dim3(NT), 2 * list_bytes(a.top), s, a,
                 (int32_t)rows);
 }
-template <typename T, bool PAST>
+template <typename T, int PAST>
 int run_step(const DistillArgs &a, int64_t rows, hipStream_t s) {
   // As many workgroups a compute unit as its registers hold: 16 to 32 waves.  (Of 4097 to 8192 pieces 1024 threads with eight each would leave
   // room for one only.)
@@ -509,7 +517,7 @@ int run_step(const DistillArgs &a, int64_t rows, hipStream_t s) {
   if (pieces <= 1024 * 16) return run_rows<T, 1024, 16, PAST>(a, rows, 1, s);
   return launch(k_distill_step<T, 1024, PAST>, dim3((uint32_t)rows), dim3(1024), list_bytes(a.top), s, a);
 }
-template <typename T, bool PAST>
+template <typename T, int PAST>
 int run_backward(const DistillArgs &a, int64_t rows, hipStream_t s) {
   const int64_t per = 16 / sizeof(T), pieces = a.vocab / per > 0 ? a.vocab / per : 1;      // (whole ones, at most)
   // few rows: several workgroups a row, of 1024 pieces at least
@@ -519,10 +527,25 @@ int run_backward(const DistillArgs &a, int64_t rows, hipStream_t s) {
                 (int32_t)((pieces + splits - 1) / splits));
 }
 
-// A gradient that the device's last cache (256 MB) can hardly hold for its reader is written past the caches, which leaves them to the
-// logits.  Gradient and step in us, through / past: 8192 x 16001 BF16 (262 MB) 124 / 100 and 155 / 138, 4096 x 65536 (537 MB) 227 / 215 and
-// 242 / 236, 4096 x 50021 fp32 365 / 349 and 374 / 362; but 1024 x 32768 fp32 (134 MB) 45 / 56, a step of 255 x 50021 fp32 (51 MB) 22 / 25.
-bool past_caches(const nvfp4_distill_params *p) { return p->rows * p->vocab * (p->x_dtype ? 4 : 2) > (int64_t)192 << 20; }
+// Logits are read here for the last time: where they and the gradient do not fit the device's last cache (256 MB) together, they are loaded past
+// the caches, which leaves them to the gradient's reader; where it can hardly hold the gradient alone, that is stored past them
+// too.  In us, with several batches in turn, all through / loads past: gradients of 512 x 16384 fp32 (34 MB) 13 / 15, 512 x 32768 (67 MB) 25 / 25,
+// 1024 x 32768 (134 MB) 59 / 46, 2048 x 32768 BF16 (134 MB) 59 / 49; a step 60 / 55 and 67 / 60.  Loads past / both: 4096 x 65536 BF16 (537 MB)
+// 227 / 215, a step 242 / 236; but 1024 x 32768 fp32 46 / 55.
+int past_caches(const nvfp4_distill_params *p) {
+  const int64_t megabytes = p->rows * p->vocab * (p->x_dtype ? 4 : 2) >> 20;
+  return megabytes > 192 ? kBoth : megabytes > 96 ? kLoads : kThrough;
+}
+
+template <typename T>
+int run_step(int past, const DistillArgs &a, int64_t rows, hipStream_t s) {
+  return past == kBoth ? run_step<T, kBoth>(a, rows, s) : past == kLoads ? run_step<T, kLoads>(a, rows, s) : run_step<T, kThrough>(a, rows, s);
+}
+template <typename T>
+int run_backward(int past, const DistillArgs &a, int64_t rows, hipStream_t s) {
+  return past == kBoth ? run_backward<T, kBoth>(a, rows, s) : past == kLoads ? run_backward<T, kLoads>(a, rows, s)
+                                                                            : run_backward<T, kThrough>(a, rows, s);
+}
 
 }  // namespace
 }  // namespace nvfp4_46
@@ -553,8 +576,7 @@ extern "C" int nvfp4_distill_backward(const void *logits, const nvfp4_distill_pa
   a.weight = weight;
   a.dlogits = dlogits;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (past_caches(p)) return p->x_dtype ? run_backward<float, true>(a, p->rows, s) : run_backward<__bf16, true>(a, p->rows, s);
-  return p->x_dtype ? run_backward<float, false>(a, p->rows, s) : run_backward<__bf16, false>(a, p->rows, s);
+  return p->x_dtype ? run_backward<float>(past_caches(p), a, p->rows, s) : run_backward<__bf16>(past_caches(p), a, p->rows, s);
 }
 
 extern "C" int nvfp4_distill_step(const void *logits, const nvfp4_distill_params *p, const void *teacher, const void *index,
@@ -569,6 +591,5 @@ extern "C" int nvfp4_distill_step(const void *logits, const nvfp4_distill_params
   a.weight = weight;
   a.dlogits = dlogits;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (past_caches(p)) return p->x_dtype ? run_step<float, true>(a, p->rows, s) : run_step<__bf16, true>(a, p->rows, s);
-  return p->x_dtype ? run_step<float, false>(a, p->rows, s) : run_step<__bf16, false>(a, p->rows, s);
+  return p->x_dtype ? run_step<float>(past_caches(p), a, p->rows, s) : run_step<__bf16>(past_caches(p), a, p->rows, s);
 }

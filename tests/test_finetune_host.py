@@ -66,7 +66,7 @@ def test_registers_of_the_streaming_kernels():
     shrink = {k: v for k, v in adapters.items() if "k_shrink" in k}
     outer = {k: v for k, v in adapters.items() if "k_outer" in k}
     rows = {k: v for k, v in distill.items() if "k_distill_rows" in k}
-    assert len(shrink) >= 20 and len(outer) == 3 and len(rows) == 20
+    assert len(shrink) >= 20 and len(outer) == 3 and len(rows) == 30
     for name, v in {**shrink, **outer, **distill}.items():
         assert v["ScratchSize"] == 0, (name, v)
     for name, v in shrink.items():
