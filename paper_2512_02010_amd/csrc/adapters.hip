@@ -877,7 +877,7 @@ bool sizes_fit(const nvfp4_adapters_params &p) {
          p.inp % 8 == 0 && p.out % 8 == 0 && p.adapters > 0 && p.adapters <= kMostAdapters && p.rank > 0 && p.rank <= kMostRank;
 }
 bool stride_fits(int64_t ld, int64_t width, int64_t rows) {
-  return ld >= width && ld <= (int64_t)1 << 40 && rows * ld <= (int64_t)1 << 40;
+  return ld >= width && ld <= ((int64_t)1 << 40) / (rows > 0 ? rows : 1);
 }
 bool at(const void *ptr, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(ptr) % bytes == 0; }
 int64_t divide_up(int64_t a, int64_t b) { return (a + b - 1) / b; }

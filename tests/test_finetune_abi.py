@@ -78,6 +78,8 @@ def test_refusals_of_the_adapters():
     assert _backward(_adapters(ld_base=64, ld_out=64, ld_dy=16)) == 2
     assert _backward(_adapters(ld_base=64, ld_out=64, ld_dy=36)) == 3
     assert _forward(_adapters(out_dtype=2)) == 4
+    # rows times stride past 64 bits
+    assert _forward(_adapters(tokens=(1 << 24) - 1, ld_x=1 << 40)) == 2 and _forward(_adapters(tokens=(1 << 24) - 1, ld_out=1 << 40)) == 2
     # in place, but with another stride
     assert _forward(_adapters(ld_out=40), base=P, out=P) == 2 and _backward(_adapters(ld_base=64, ld_out=72), dx_base=P, dx=P) == 2
     assert _forward(_adapters(), h=P + 2) == 3 and _forward(_adapters(), base=P + 4) == 3

@@ -291,6 +291,24 @@ def test_refusals_of_device_tensors():
         assert e.value.status == status
 
 
+@pytest.mark.parametrize("T", [5, 300])
+def test_offsets_past_32_bits(T):
+    """Rows so far apart that elements, and then bytes, are no 32-bit numbers any more."""
+    s = _inputs(T, 64, 48, 8, 3)
+    want = F.nvfp4_adapters_forward(s["x"], s["base"], s["a"], s["b"], s["which"], s["scales"], want_h=True)
+    back = F.nvfp4_adapters_backward(s["dy"], s["x"], want[1], s["a"], s["b"], s["which"], s["scales"], s["dx_base"])
+    ld = ((1 << 32) // (T - 1) + 8) // 8 * 8
+    room = torch.empty((T - 1) * ld + 256, dtype=torch.bfloat16, device="cuda")
+    far = {k: room.as_strided((T, s[k].shape[1]), (ld, 1), at) for k, at in (("x", 0), ("base", 64), ("dy", 128), ("dx_base", 192))}
+    for k, v in far.items():
+        v.copy_(s[k])
+    out, h = F.nvfp4_adapters_forward(far["x"], far["base"], s["a"], s["b"], s["which"], s["scales"], want_h=True, out=far["base"])
+    assert torch.equal(out, want[0]) and torch.equal(h, want[1])
+    got = F.nvfp4_adapters_backward(far["dy"], far["x"], h, s["a"], s["b"], s["which"], s["scales"], far["dx_base"], out=far["dx_base"])
+    for u, v in zip(got, back):
+        assert torch.equal(u, v)
+
+
 def test_replayed_from_a_graph():
     """Captured once and replayed: nothing is asked of the host, and nothing is left from one replay to the next."""
     s = _inputs(1100, 256, 512, 16, 3)

@@ -229,6 +229,26 @@ def test_rows_that_begin_anywhere(V, dtype):
     del want
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_offsets_past_32_bits(dtype):
+    """Rows so far apart that elements, and then bytes, are no 32-bit numbers any more."""
+    s = _inputs(4, 5003, 20, dtype)
+    want = _check(s)
+    ld = (1 << 32) // 3 + 11
+    room = torch.empty(3 * ld + 5003, dtype=dtype, device="cuda")
+    far = room.as_strided((4, 5003), (ld, 1))
+    far.copy_(s["logits"])
+    loss, lse = F.nvfp4_distill_forward(far, s["teacher"], s["index"])
+    for got, was in ((loss, want[0]), (lse, want[1])):
+        assert bool(((got - was).abs() <= 2.0 ** -17 * (1 + was.abs())).all())                # (rows begin elsewhere: other sums)
+    d = F.nvfp4_distill_backward(far, s["teacher"], s["index"], lse, s["weight"], out=far)
+    assert bool(((d - want[2]).abs() <= 2.0 ** -7 * want[2].abs() + 1e-30).all())
+    far.copy_(s["logits"])
+    loss, d = F.nvfp4_distill_step(far, s["teacher"], s["index"], s["weight"], out=far)
+    assert bool(((loss - want[3]).abs() <= 2.0 ** -17 * (1 + want[3].abs())).all())
+    assert bool(((d - want[4]).abs() <= 2.0 ** -7 * want[4].abs() + 1e-30).all())
+
+
 def test_no_rows():
     s = {k: v[:0] for k, v in _inputs(4, 100, 5).items()}
     loss, lse = F.nvfp4_distill_forward(s["logits"], s["teacher"], s["index"])
