@@ -1089,8 +1089,12 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
                        p->ld_base, p->ld_out, p->inp, rank, pitch, (int32_t)d.splits_out, term_ranks, false};
     if (const int rc = run_expand<kAcross, __bf16>(e, d, s)) return rc;
   }
-  const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, rank <= 64 ? 1 : 2);
-  if (const int rc = launch(rank <= 16 ? k_outer<1> : rank <= 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
+  // A workgroup has up to 64 ranks, which read x and dy once; where its sums go to the output at once, up to 32, since the gradients are
+  // much of the bytes then and more workgroups write them.  32 / 64, 4096 x 4096, rank 64: one token 26.9 / 28.8 us, 512 of one adapter
+  // 33.8 / 36.7, of 64 adapters 118 / 147; beyond, 8192 tokens of 8 adapters 186 / 178, at 8192 x 8192 322 / 295.
+  const int ranks = rank <= 16 ? 16 : rank <= 32 || d.whole ? 32 : 64;
+  const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, (uint32_t)divide_up(rank, ranks));
+  if (const int rc = launch(ranks == 16 ? k_outer<1> : ranks == 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
   if (d.whole || d.ranges == 1) return NVFP4_OK;
   const int64_t most = divide_up(p->rank * (p->inp > p->out ? p->inp : p->out), 1024);
   return launch(k_join, dim3((uint32_t)(most < 256 ? most : 256), (uint32_t)p->adapters, 2), dim3(256), 0, s, g);
