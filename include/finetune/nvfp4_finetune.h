@@ -96,7 +96,7 @@ typedef struct {
   int64_t vocab;           /* logits of a row, 1 .. 2^29                                                       */
   int64_t ld;              /* elements from row to row of logits and dlogits, at least vocab, any alignment     */
   int64_t top;             /* entries of a list, 1 .. 1024                                                     */
-  float temperature;       /* finite, > 0                                                                      */
+  float temperature;       /* finite, at least 2^-126 (fp32's least normal number)                         */
   uint32_t x_dtype;        /* NVFP4_X_BF16 or NVFP4_X_F32: of logits and dlogits                               */
   uint32_t teacher_dtype;  /* the same, of teacher                                                             */
   uint32_t index_dtype;    /* NVFP4_INDEX_I32 or NVFP4_INDEX_I64                                               */

@@ -22,6 +22,7 @@ namespace {
 constexpr int kMostTop = 1024;
 constexpr int64_t kMostRows = 1 << 21;        // (a workgroup of 1024 each: a grid has fewer than 2^32 threads)
 constexpr float kInf = __builtin_inff();
+constexpr float kLeastTemperature = 0x1p-126f;      // (a little below half of it, log2(e) / temperature is infinite)
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -473,7 +474,7 @@ int check(const void *logits, const nvfp4_distill_params *p, const void *teacher
   if (p->rows < 0 || p->rows > kMostRows || p->vocab <= 0 || p->vocab > (int64_t)1 << 29 || p->ld < p->vocab ||
       p->ld > (int64_t)1 << 40 || p->rows * p->ld > (int64_t)1 << 40 || p->top <= 0 || p->top > kMostTop)
     return NVFP4_ERR_SHAPE;
-  if (!(p->temperature > 0.0f) || !(p->temperature < kInf) || p->x_dtype > NVFP4_X_F32 || p->teacher_dtype > NVFP4_X_F32 ||
+  if (!(p->temperature >= kLeastTemperature) || !(p->temperature < kInf) || p->x_dtype > NVFP4_X_F32 || p->teacher_dtype > NVFP4_X_F32 ||
       p->index_dtype > NVFP4_INDEX_I64)
     return NVFP4_ERR_PARAM;
   return NVFP4_OK;
