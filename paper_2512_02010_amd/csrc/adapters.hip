@@ -1018,9 +1018,11 @@ extern "C" size_t nvfp4_adapters_workspace_bytes(const nvfp4_adapters_params *p,
 extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params *p, const void *base, const void *a, const void *b,
                                       const int32_t *which, const float *scales, float *h, void *out, void *workspace,
                                       size_t workspace_bytes, void *stream) {
-  if (!p || !a || !b || !scales || !workspace) return NVFP4_ERR_NULL;
+  if (!p) return NVFP4_ERR_NULL;
+  if (!sizes_fit(*p)) return NVFP4_ERR_SHAPE;    // (first: what has no element, a workspace among it, may well have no address)
+  if (!a || !b || !scales || !workspace) return NVFP4_ERR_NULL;
   if (p->tokens != 0 && (!x || !which || !out)) return NVFP4_ERR_NULL;
-  if (!sizes_fit(*p) || !stride_fits(p->ld_x, p->inp, p->tokens) || (base && !stride_fits(p->ld_base, p->out, p->tokens)) ||
+  if (!stride_fits(p->ld_x, p->inp, p->tokens) || (base && !stride_fits(p->ld_base, p->out, p->tokens)) ||
       !stride_fits(p->ld_out, p->out, p->tokens) || (base == out && p->ld_base != p->ld_out))
     return NVFP4_ERR_SHAPE;
   if (!at(x, 16) || !at(base, 16) || !at(a, 16) || !at(b, 16) || !at(out, 16) || !at(workspace, 16) || !at(which, 4) ||
@@ -1056,9 +1058,11 @@ extern "C" int nvfp4_adapters_forward(const void *x, const nvfp4_adapters_params
 extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_params *p, const void *x, const float *h, const void *a,
                                        const void *b, const int32_t *which, const float *scales, const void *dx_base, void *dx,
                                        float *da, float *db, void *workspace, size_t workspace_bytes, void *stream) {
-  if (!p || !a || !b || !scales || !da || !db || !workspace) return NVFP4_ERR_NULL;
+  if (!p) return NVFP4_ERR_NULL;
+  if (!sizes_fit(*p)) return NVFP4_ERR_SHAPE;
+  if (!a || !b || !scales || !da || !db || !workspace) return NVFP4_ERR_NULL;
   if (p->tokens != 0 && (!dy || !x || !h || !which)) return NVFP4_ERR_NULL;
-  if (!sizes_fit(*p) || !stride_fits(p->ld_x, p->inp, p->tokens) || !stride_fits(p->ld_dy, p->out, p->tokens) ||
+  if (!stride_fits(p->ld_x, p->inp, p->tokens) || !stride_fits(p->ld_dy, p->out, p->tokens) ||
       (dx && dx_base && !stride_fits(p->ld_base, p->inp, p->tokens)) || (dx && !stride_fits(p->ld_out, p->inp, p->tokens)) ||
       (dx && dx_base == dx && p->ld_base != p->ld_out))
     return NVFP4_ERR_SHAPE;

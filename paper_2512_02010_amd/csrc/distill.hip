@@ -468,12 +468,13 @@ __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows
 
 // ---- host -----------------------------------------------------------------------------------------------------------
 
-// (`more`: the call's other pointers are given)
+// (`more`: the call's other pointers are given.  Sizes come first: what has no element may well have no address.)
 int check(const void *logits, const nvfp4_distill_params *p, const void *teacher, const void *index, bool more) {
-  if (!p || (p->rows != 0 && (!logits || !teacher || !index || !more))) return NVFP4_ERR_NULL;
+  if (!p) return NVFP4_ERR_NULL;
   if (p->rows < 0 || p->rows > kMostRows || p->vocab <= 0 || p->vocab > (int64_t)1 << 29 || p->ld < p->vocab ||
       p->ld > (int64_t)1 << 40 || p->rows * p->ld > (int64_t)1 << 40 || p->top <= 0 || p->top > kMostTop)
     return NVFP4_ERR_SHAPE;
+  if (p->rows != 0 && (!logits || !teacher || !index || !more)) return NVFP4_ERR_NULL;
   if (!(p->temperature >= kLeastTemperature) || !(p->temperature < kInf) || p->x_dtype > NVFP4_X_F32 || p->teacher_dtype > NVFP4_X_F32 ||
       p->index_dtype > NVFP4_INDEX_I64)
     return NVFP4_ERR_PARAM;

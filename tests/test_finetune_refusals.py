@@ -5,7 +5,7 @@ import pytest
 
 from paper_2512_02010_amd import finetune as F
 
-from .test_finetune_abi import P, _distill, _distill_calls
+from .test_finetune_abi import _adapters, _backward, _distill, _distill_calls, _forward
 
 
 @pytest.mark.parametrize("temperature", [2.0 ** -127, 4.2e-39, 2.9e-39, 1e-39, 2.0 ** -149])
@@ -16,3 +16,15 @@ def test_temperatures_that_are_no_normal_numbers(temperature):
     for call, _ in _distill_calls():
         assert call(_distill(temperature=temperature)) == 4
         assert call(_distill(rows=0, temperature=2.0 ** -126)) == 0
+
+
+def test_sizes_are_named_before_missing_pointers():
+    """A tensor without elements has no address, nor has the workspace of a call whose sizes are refused: the status is the sizes'."""
+    for call, more in ((_forward, {}), (_backward, dict(ld_base=64, ld_out=64))):
+        for bad in (dict(inp=60, ld_x=60), dict(rank=0), dict(rank=129), dict(adapters=0), dict(adapters=2049), dict(out=0), dict(tokens=1 << 24)):
+            assert call(_adapters(**{**more, **bad}), a=None, b=None, scales=None, workspace=None, room=0) == 2, bad
+        assert call(_adapters(**more), workspace=None) == 1 and call(_adapters(**more), a=None) == 1
+    for call, names in _distill_calls():
+        for bad in (dict(vocab=0, ld=0), dict(top=0), dict(top=1025), dict(rows=-1)):
+            assert call(_distill(**bad), **dict.fromkeys(names)) == 2, bad
+        assert call(_distill(), **dict.fromkeys(names)) == 1
