@@ -549,7 +549,11 @@ void *rows_of(PyObject *o, const char *what, const at::Tensor &like, int64_t row
   *ld = rows > 1 ? t.stride(0) : cols;
   return t.data_ptr();
 }
-// The caller's workspace, or one of `need` bytes that lives as long as this.
+// A lent workspace is memory that the kernels of x's device write to.
+void check_workspace(PyObject *o, const at::Tensor &like) {
+  if (o != Py_None && tensor(o, "workspace").device() != like.device()) misfit("workspace", "on the device of the others");
+}
+// The caller's workspace (checked before), or one of `need` bytes that lives as long as this.
 struct Scratch {
   void *p;
   size_t bytes;
@@ -599,6 +603,7 @@ PyObject *adapters_forward(PyObject *const *v, Py_ssize_t n) {
   const void *const base = v[1] == Py_None ? nullptr : rows_of(v[1], "base", x, p.tokens, p.out, type, &p.ld_base);
   const int want_h = PyObject_IsTrue(v[6]);
   if (want_h < 0) return nullptr;
+  check_workspace(v[8], x);
   const OnStream on(v[10], x);
   Owned out = v[7] == Py_None ? Owned(new_tensor({p.tokens, p.out}, type, v[0], v[9])) : Owned(Py_NewRef(v[7]));
   void *const po = rows_of(out.o, "out", x, p.tokens, p.out, type, &p.ld_out);
@@ -628,6 +633,7 @@ PyObject *adapters_backward(PyObject *const *v, Py_ssize_t n) {
   const int want_dx = PyObject_IsTrue(v[8]);
   if (want_dx < 0) return nullptr;
   const void *const base = v[7] == Py_None ? nullptr : rows_of(v[7], "dx_base", x, p.tokens, p.inp, at::kBFloat16, &p.ld_base);
+  check_workspace(v[10], x);
   const OnStream on(v[12], x);
   Owned dx = !want_dx ? Owned(Py_NewRef(Py_None))
              : v[9] == Py_None ? Owned(new_tensor({p.tokens, p.inp}, at::kBFloat16, v[1], v[11])) : Owned(Py_NewRef(v[9]));

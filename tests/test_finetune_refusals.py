@@ -2,6 +2,8 @@
 import ctypes as C
 
 import pytest
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
 
 from paper_2512_02010_amd import finetune as F
 
@@ -28,3 +30,19 @@ def test_sizes_are_named_before_missing_pointers():
         for bad in (dict(vocab=0, ld=0), dict(top=0), dict(top=1025), dict(rows=-1)):
             assert call(_distill(**bad), **dict.fromkeys(names)) == 2, bad
         assert call(_distill(), **dict.fromkeys(names)) == 1
+
+
+@pytest.mark.filterwarnings("ignore:Accessing the data pointer of FakeTensor")
+def test_a_workspace_of_another_device():
+    """Refused as every other operand of another device is.  (Tensors without memory stand for those of two devices.)"""
+    with FakeTensorMode():
+        def zeros(*shape, dtype=torch.bfloat16, device="cuda:0"):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+        x, base, a, b = zeros(4, 64), zeros(4, 32), zeros(2, 8, 64), zeros(2, 32, 8)
+        which, scales, h = zeros(4, dtype=torch.int32), zeros(2, dtype=torch.float32), zeros(4, 8, dtype=torch.float32)
+        workspace = zeros(1 << 20, dtype=torch.uint8, device="cuda:1")
+    with pytest.raises(AssertionError, match="workspace must be on the device of the others"):
+        F.nvfp4_adapters_forward(x, base, a, b, which, scales, workspace=workspace)
+    with pytest.raises(AssertionError, match="workspace must be on the device of the others"):
+        F.nvfp4_adapters_backward(base, x, h, a, b, which, scales, workspace=workspace)
