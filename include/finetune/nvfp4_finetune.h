@@ -86,7 +86,10 @@ int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_params *p, cons
  *
  * An entry whose index lies outside [0, vocab), or whose teacher logit is -inf, is none.  A row without entries is not learnt from: its
  * loss and its gradient are 0, whatever its logits hold.  Entries with the same index add up.  Logits may be -inf (masked
- * words); at an entry with p_j > 0 that makes the loss infinite.  Neither loss nor gradient is multiplied by temperature^2:
+ * words); at an entry with p_j > 0 that makes the loss infinite, and a row with entries that holds nothing but -inf has no distribution:
+ * loss and gradient are NaN.  lse is fp32, and what its rounding leaves (2^-24 |lse|, or all of it where lse is beyond fp32) enters the
+ * backward pass' probabilities; loss and step go by differences from the row's largest logit and do without it, so that a row
+ * of the type's lowest value alone has its loss and its gradient there.  Neither loss nor gradient is multiplied by temperature^2:
  * `weight` is the place for it.
  */
 enum { NVFP4_INDEX_I32 = 0, NVFP4_INDEX_I64 = 1 };

@@ -227,11 +227,13 @@ __device__ inline void read_list(const List &l, const DistillArgs &a, int64_t ro
     *l.twice = two;
   }
 }
-// By the first wave.
-__device__ inline float list_loss(const List &l, const DistillArgs &a, float lse) {
+// By the first wave.  y - lse is (z - m) / temperature - log s, from the row's maximum m and sum s: m / temperature need not be a number
+// of fp32 (a row of nothing but the type's lowest value, at a temperature below 1), nor z - m, but half of it is.
+__device__ inline float list_loss(const List &l, const DistillArgs &a, Running row) {
+  const float log_s = logf(row.s), half_m = 0.5f * row.m, twice_inv_t = 2.0f * a.inv_t;
   float s = 0.0f;
   for (int j = threadIdx.x & 63; j < a.top; j += 64)
-    if (l.index[j] >= 0 && l.p[j] != 0.0f) s += l.p[j] * (l.log_p[j] - (l.z[j] * a.inv_t - lse));
+    if (l.index[j] >= 0 && l.p[j] != 0.0f) s += l.p[j] * (l.log_p[j] - ((0.5f * l.z[j] - half_m) * twice_inv_t - log_s));
   return wave_sum(s);
 }
 
@@ -299,7 +301,6 @@ __device__ inline Running row_sum(Scratch<NT> &sh, const Row<T> &r, float c) {
   }
   return join_waves<NT>(sh.m, sh.s, run, c);
 }
-__device__ inline float lse_of(Running r, float inv_t) { return r.m * inv_t + logf(r.s); }
 
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) k_distill_forward(DistillArgs a) {
@@ -307,12 +308,12 @@ __global__ void __launch_bounds__(NT) k_distill_forward(DistillArgs a) {
   const List list(a.top);
   const int64_t row = blockIdx.x;
   if (threadIdx.x < 64) read_list<T>(list, a, row, 0, a.vocab);
-  const float lse = lse_of(row_sum<T, NT>(sh, Row<T>(a.logits, row, a.ld, a.vocab), a.c), a.inv_t);
+  const Running run = row_sum<T, NT>(sh, Row<T>(a.logits, row, a.ld, a.vocab), a.c);
   if (threadIdx.x < 64) {
-    const float loss = *list.any ? list_loss(list, a, lse) : 0.0f;
+    const float loss = *list.any ? list_loss(list, a, run) : 0.0f;
     if (threadIdx.x == 0) {
       a.loss[row] = loss;
-      if (a.lse) a.lse[row] = lse;
+      if (a.lse) a.lse[row] = run.m * a.inv_t + logf(run.s);
     }
   }
 }
@@ -365,13 +366,14 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
   const int64_t row = blockIdx.x;
   const Row<T> r(a.logits, row, a.ld, a.vocab), d(a.dlogits, row, a.ld, a.vocab);
   if (threadIdx.x < 64) read_list<T>(list, a, row, 0, a.vocab);
-  const float lse = lse_of(row_sum<T, NT>(sh, r, a.c), a.inv_t), g = a.weight ? a.weight[row] * a.inv_t : a.inv_t;
+  const Running run = row_sum<T, NT>(sh, r, a.c);
+  const float g = a.weight ? a.weight[row] * a.inv_t : a.inv_t, inv_s = 1.0f / run.s, gs = g * inv_s, most = run.m;
   if (threadIdx.x < 64) {
-    const float loss = *list.any ? list_loss(list, a, lse) : 0.0f;
+    const float loss = *list.any ? list_loss(list, a, run) : 0.0f;
     if (threadIdx.x == 0) a.loss[row] = loss;
   }
   const bool any = *list.any;
-  const auto of = [&](float z) { return any ? g * probability(z, a.inv_t, lse) : 0.0f; };
+  const auto of = [&](float z) { return any ? gs * exp2_diff(z, most, a.c) : 0.0f; };
   for (int32_t v = threadIdx.x; v < r.pieces; v += NT) {
     float x[kPer];
     unpack<T>(r.template load<PAST>(v), x);
@@ -380,7 +382,7 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
   }
   if (const int64_t e = r.edge(threadIdx.x); e != Row<T>::kNoEdge) set_element<T>(d.at, e, of(element<T>(r.at, e)));
   __syncthreads();
-  rewrite_list<T, NT>(list, a, row, 0, a.vocab, g, [&](float z) { return probability(z, a.inv_t, lse); });
+  rewrite_list<T, NT>(list, a, row, 0, a.vocab, g, [&](float z) { return exp2_diff(z, most, a.c) * inv_s; });
 }
 
 // The same with the row in registers, NV pieces a thread.  A workgroup takes row after row: where a piece of the gradient has been
@@ -431,7 +433,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows
     const float g = a.weight ? a.weight[row] * a.inv_t : a.inv_t, inv_s = 1.0f / run.s, gs = g * inv_s, most = run.m;
     const bool any = *list.any;
     if (threadIdx.x < 64) {
-      const float loss = any ? list_loss(list, a, lse_of(run, a.inv_t)) : 0.0f;
+      const float loss = any ? list_loss(list, a, run) : 0.0f;
       if (threadIdx.x == 0) a.loss[row] = loss;
     }
     const int64_t next = row + gridDim.x;
