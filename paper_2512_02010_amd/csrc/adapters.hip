@@ -326,18 +326,6 @@ struct ExpandArgs {
 // How the matrix of k_expand lies: rows of ranks that are whole pieces of 16 bytes, or not, or the other way round [rank][width].
 enum { kWhole, kRagged, kAcross };
 
-// Eight ranks of column c, from `first`.
-template <int LIES>
-__device__ inline bf16x8 load_ranks(const __bf16 *w, int32_t c, int first, int rank) {
-  const __bf16 *const from = w + (int64_t)c * rank;
-  if constexpr (LIES == kWhole) return load8(from + first);
-  bf16x8 v;
-  for (int i = 0; i < 8; ++i) v[i] = from[first + i < rank ? first + i : rank - 1];
-  for (int i = 0; i < 8; ++i)
-    if (first + i >= rank) v[i] = (__bf16)0.0f;
-  return v;
-}
-
 // Eight columns of a row as they are in memory, and as fp32.
 template <typename T>
 struct Columns {
@@ -372,17 +360,25 @@ struct Columns {
 // A wave has a block of columns of its own and keeps their part of w in registers while it goes through the workgroup's stretch of the
 // plan; per tile the workgroup sums the parts of s h and splits them once, into LDS, while the tile's columns of base are on their way.
 // Bound by base and out.  16384 x 4096 BF16 (268 MB) by itself: 65 us up to rank 32, 76 at 64, 101 at 128; a copy of as much 57.
-// Eight waves a workgroup, two workgroups a compute unit, where 128 registers are enough for it; else four waves and three.
+// Planned, BF16: eight waves a workgroup, two workgroups a compute unit, where 128 registers are enough (up to 32 ranks), or one, where 168 are
+// not (beyond 64); four waves, and three workgroups, in between: 33 to 64 ranks in 128 registers left up to 148 bytes a thread to scratch memory.
+// fp32 four waves, and three or two.  Whole calls with spills / without, 4096 x 4096, rank 64: 4096 tokens 72.4 / 68.5 us, backwards 128 / 120; 16384
+// tokens 146.7 / 147.7, backwards 276 / 270.
+// Ranks that are no multiple of 8 (kRagged) go through LDS too; element by element from memory they took registers, and spilled.  So / through
+// LDS: 16384 tokens, rank 12 138 / 116 us, rank 100 250 / 205, 128 tokens of 8 adapters, rank 100 64 / 29.
 template <bool FEW, typename T, int F>
-constexpr int expand_waves = !FEW && sizeof(T) == 2 ? 8 : 4;
+constexpr int expand_waves = !FEW && sizeof(T) == 2 && F != 2 ? 8 : 4;
 
 template <bool FEW, int LIES, typename T, int F>
 __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (expand_waves<FEW, T, F>) == 8 ? 4 : 3) k_expand(ExpandArgs a) {
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 2, kSpans = F ? F : 1, kProducts = F ? kTerms : kTerms - 1;
   constexpr int MT = FEW ? 1 : 2, kWaves = expand_waves<FEW, T, F>, kThreads = kWaves * 64, kRows = MT * 16;
   __shared__ TileTokens shared;
-  __shared__ bf16x8 split[FEW ? 1 : 2][kRows][kTerms * kSpans * 4 + 1];      // (an odd number of pieces: a row a bank further)
-  __shared__ __align__(16) __bf16 turned[LIES == kAcross ? kWaves : 1][LIES == kAcross ? 32 * 68 : 8];
+  // An odd number of pieces, a row a bank further; of many pieces, which would leave LDS for one workgroup, an even one, the places in a row
+  // exchanged instead.
+  __shared__ bf16x8 split[FEW ? 1 : 2][kRows][kTerms * kSpans * 4 + (F == 4 ? 0 : 1)];
+  const auto place = [](int n, int piece) { return F == 4 ? piece ^ (n & 15) : piece; };
+  __shared__ __align__(16) __bf16 turned[LIES == kWhole ? 1 : kWaves][LIES == kAcross ? 32 * 68 : LIES == kRagged ? 32 * (F ? F * 32 : 16) : 8];
   const int lane = threadIdx.x & 63, wave = wave_of(threadIdx.x), row = lane & 15, group = lane / 16;
   int32_t first = 0, last = 1, in[MT];           // in: this lane's token of each 16, -1: there is none
   int32_t adapter_here = -1, count_here = 0;     // of the only tile
@@ -440,7 +436,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
       for (int which = 0; which < kTerms; ++which) {
         bf16x4 q;
         for (int k = 0; k < 4; ++k) q[k] = term(v[k], which);
-        reinterpret_cast<bf16x4 *>(&split[buffer][n][which * kSpans * 4])[from / 4] = q;
+        reinterpret_cast<bf16x4 *>(&split[buffer][n][place(n, which * kSpans * 4 + from / 8)])[from / 4 % 2] = q;
       }
       if (a.terms && mine && from < a.term_ranks) {
         __bf16 *const to = a.terms + ((int64_t)i * 3 * a.term_ranks + from) * kTile + n;
@@ -466,15 +462,48 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
   const auto fetch_w = [&](int32_t adapter) {
     const __bf16 *const of = a.w + (int64_t)adapter * a.width * a.rank;
     const auto column_of = [&](int p) { return c0 + p / 2 * 32 + row / 4 * 8 + p % 2 * 4 + row % 4; };
-    if constexpr (LIES != kAcross) {
+    if constexpr (LIES == kWhole) {
 #pragma unroll
       for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int f = 0; f < kSpans; ++f) {
           const int piece = F ? f * 4 + group : group % pieces;
-          w[p][f] = load_ranks<LIES>(of, column_of(p) < width ? column_of(p) : width - 1, piece < pieces ? piece * 8 : 0, a.rank);
+          w[p][f] = load8(of + (int64_t)(column_of(p) < width ? column_of(p) : width - 1) * a.rank + (piece < pieces ? piece * 8 : 0));
           if (F && pieces % 4 && piece >= pieces) w[p][f] = bf16x8{};
         }
+    } else if constexpr (LIES == kRagged) {
+      // 32 columns are 4 rank adjacent pieces of 16 bytes, 64 of them to a load; the wave's own LDS gives them back by columns and ranks.
+      constexpr int kLoads = F ? 2 * F : 1;
+      __bf16 *const turn = turned[LIES == kRagged ? wave : 0];
+      const __bf16 *const from = of + (int64_t)c0 * a.rank;
+      const int32_t most = (width - c0) * a.rank / 8 - 1;              // (of 64 columns, or of fewer where the matrix ends)
+      int32_t lane0 = lane;
+      asm("" : "+v"(lane0));                     // (the places are found again for each adapter and piece: kept, they would not leave registers)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int32_t piece = half * 4 * a.rank + i * 64 + lane0;
+          w[half * 2 + i / kSpans][i % kSpans] = load8(from + (piece < most ? piece : most) * 8);
+        }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+          if (i * 64 + lane0 < 4 * a.rank) *reinterpret_cast<bf16x8 *>(turn + (i * 64 + lane0) * 8) = w[half * 2 + i / kSpans][i % kSpans];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int p = half * 2; p < half * 2 + 2; ++p)
+#pragma unroll
+          for (int f = 0; f < kSpans; ++f) {
+            int32_t rank = (F ? f * 4 + group : group % pieces) * 8, line = (column_of(p) - c0 - half * 32) * a.rank;
+            asm("" : "+v"(rank), "+v"(line));
+            for (int k = 0; k < 8; ++k) w[p][f][k] = rank + k < a.rank ? turn[line + rank + k] : (__bf16)0.0f;
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
       // A load has eight ranks' 64 columns; 32 ranks at a time are turned in the wave's own LDS.
       __bf16 *const turn = turned[LIES == kAcross ? wave : 0];
@@ -528,7 +557,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
             for (int n = 0; n < kProducts; ++n) {
               bf16x8 h;
               if (F) {
-                h = split[buffer][m * 16 + row][n * kSpans * 4 + f * 4 + group];
+                h = split[buffer][m * 16 + row][place(row, n * kSpans * 4 + f * 4 + group)];
               } else {
                 const int q = n * 4 + group, which = q / pieces;
                 h = which < kTerms ? split[buffer][m * 16 + row][which * 4 + q % pieces] : bf16x8{};
@@ -989,7 +1018,8 @@ int run_expand_of(ExpandArgs g, const Layout &d, hipStream_t s) {
   }
   constexpr int kWaves = expand_waves<false, T, F>;
   const int64_t across = g.out ? divide_up(g.width, kBlock * kWaves) : 1;
-  const int64_t most = divide_up(F <= 1 ? 2048 : (F == 2 ? 1024 : 512) * (sizeof(T) == 4 ? 2 : 1), across);
+  // (two to four turns of the workgroups that a card holds at once; BF16, 33 to 64 ranks, 16384 tokens: two 147.7 us, two and two thirds 162.6)
+  const int64_t most = divide_up(F <= 1 ? 2048 : (F == 2 ? (sizeof(T) == 2 ? 768 : 1024) : 512) * (kWaves == 4 ? 2 : 1), across);
   g.single = d.tiles <= most;
   const dim3 grid((uint32_t)(g.single ? d.tiles : most), (uint32_t)across);
   return launch(k_expand<false, LIES, T, F>, grid, dim3(kWaves * 64), 0, s, g);
