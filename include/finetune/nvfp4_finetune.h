@@ -32,7 +32,8 @@ extern "C" {
  *
  *   dh_t = s_l B_l^T dy_t,  dx_t = dx_base_t + A_l^T dh_t,  dA_l = sum_t dh_t x_t^T,  dB_l = s_l sum_t dy_t h_t^T
  *
- * Every sum is taken in fp32.  h and dh enter the matrix units as sums of three BF16 terms, which have their 24 bits.
+ * Every sum is taken in fp32.  h and dh enter the matrix units as sums of three BF16 terms, which have their 24 bits (and their sign, so
+ * that an infinity among A, B, x or dy comes out as one where it meets a number of 2^-110 at least).
  */
 typedef struct {
   int64_t tokens;         /* rows of x, 0 .. 2^24 - 1                                                           */

@@ -121,16 +121,21 @@ __device__ inline bf16x8 load8(const __bf16 *p) { return *reinterpret_cast<const
 __device__ inline int wave_of(uint32_t thread) { return __builtin_amdgcn_readfirstlane(thread / 64); }
 __device__ inline f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// v as a sum of three BF16 terms, which leave 2^-24 of it, where the result is BF16 too: its rounding hides no more than that where the ranks' terms, or the
-// base, cancel.  (Two terms, 2^-16: 16384 x 4096, rank 16 114.5 us, three 115.9; rank 64 147.2 / 150.1.)  Of an infinity or NaN the first term is all there is.
+// The BF16 next to v on the side of 0 (never v itself); 0 of 0.
+__device__ inline float below(float v) {
+  const uint32_t bits = __float_as_uint(v);
+  return bits << 1 ? __uint_as_float((bits - 1) & 0xffff0000u) : v;
+}
+// v as a sum of three BF16 terms, eight of its 24 bits each, exactly; where the result is BF16 too, whose rounding hides what a third term adds only where
+// neither the ranks' products nor the base cancel.  (Two terms, 2^-16 of v left: 16384 x 4096, rank 16 115 us, three 116; rank 64 147 / 149.)
+// All terms have v's sign and none is 0 unless v is, so that an infinity that meets them in a product comes out as if it met v: with terms rounded to
+// nearest inf times the second, 0 or of the other sign, made a NaN of it.  (Below 2^-110 BF16 has no numbers for all three.)  Of an infinity, or NaN,
+// the first term is all there is, and the others must not be 0.
 __device__ inline __bf16 term(float v, int which) {
-  __bf16 hi = (__bf16)v;
-  if (__builtin_isinf((float)hi) && __builtin_isfinite(v))          // rounded up past the largest BF16
-    hi = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(v) >> 16));
-  if (which == 0) return hi;
-  const float rest = __builtin_isfinite((float)hi) ? v - (float)hi : 0.0f;
-  const __bf16 mid = (__bf16)rest;
-  return which == 1 ? mid : (__bf16)(rest - (float)mid);
+  const bool finite = __builtin_isfinite(v);
+  if (which == 0) return (__bf16)(finite ? below(v) : v);
+  const float rest = finite ? v - below(v) : __builtin_copysignf(1.0f, v), mid = below(rest);
+  return (__bf16)(which == 1 ? mid : rest - mid);
 }
 
 // ---- k_shrink ---------------------------------------------------------------------------------------------------------
@@ -357,7 +362,7 @@ struct Columns {
 // D[column][token]: rows of w against s h, which enters as terms (term).  Row 4 a + b of product p of a block is column
 // 32 (p / 2) + 8 a + 4 (p % 2) + b, so that a lane ends up with twice 8 adjacent columns of its token, 64 bytes in four lanes.  The
 // summed index of a product is four pieces of eight ranks: F > 0: 32 ranks of one term, F times.  F == 0, rank <= 16: the one or two pieces
-// of every term side by side.
+// of every term side by side, the third by halves, which fill the four that there are (0 must not meet w, as an infinity would be NaN).
 // A wave has a block of columns of its own and keeps their part of w in registers while it goes through the workgroup's stretch of the
 // plan; per tile the workgroup sums the parts of s h and splits them once, into LDS, while the tile's columns of base are on their way.
 // Bound by base and out.  16384 x 4096 BF16 (268 MB) by itself: 65 us up to rank 32, 76 at 64, 101 at 128; a copy of as much 57.
@@ -437,6 +442,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
       for (int which = 0; which < kTerms; ++which) {
         bf16x4 q;
         for (int k = 0; k < 4; ++k) q[k] = term(v[k], which);
+        if (!F && which == 2) q *= (__bf16)0.5f;                      // (the products have it twice)
         reinterpret_cast<bf16x4 *>(&split[buffer][n][place(n, which * kSpans * 4 + from / 8)])[from / 4 % 2] = q;
       }
       if (a.terms && mine && from < a.term_ranks) {
@@ -470,7 +476,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
         for (int f = 0; f < kSpans; ++f) {
           const int piece = F ? f * 4 + group : group % pieces;
           w[p][f] = load8(of + (int64_t)(column_of(p) < width ? column_of(p) : width - 1) * a.rank + (piece < pieces ? piece * 8 : 0));
-          if (F && pieces % 4 && piece >= pieces) w[p][f] = bf16x8{};
+          if (F && piece >= pieces) w[p][f] = bf16x8{};
         }
     } else if constexpr (LIES == kRagged) {
       // 32 columns are 4 rank adjacent pieces of 16 bytes, 64 of them to a load; the wave's own LDS gives them back by columns and ranks.
@@ -561,8 +567,8 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
               if (F) {
                 h = split[buffer][m * 16 + row][place(row, n * kSpans * 4 + f * 4 + group)];
               } else {
-                const int q = n * 4 + group, which = q / pieces;
-                h = which < kTerms ? split[buffer][m * 16 + row][which * 4 + q % pieces] : bf16x8{};
+                const int q = n * 4 + group, which = q / pieces < 2 ? q / pieces : 2;
+                h = split[buffer][m * 16 + row][which * 4 + q % pieces];
               }
 #pragma unroll
               for (int p = 0; p < 4; ++p) acc[m][p] = multiply(w[p][f], h, acc[m][p]);
