@@ -87,9 +87,10 @@ int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_params *p, cons
  * An entry whose index lies outside [0, vocab), or whose teacher logit is -inf, is none.  A row without entries is not learnt from: its
  * loss and its gradient are 0, whatever its logits hold.  Entries with the same index add up.  Logits may be -inf (masked
  * words); at an entry with p_j > 0 that makes the loss infinite, and a row with entries that holds nothing but -inf has no distribution:
- * loss and gradient are NaN.  lse is fp32, and what its rounding leaves (2^-24 |lse|, or all of it where lse is beyond fp32) enters the
- * backward pass' probabilities; loss and step go by differences from the row's largest logit and do without it, so that a row
- * of the type's lowest value alone has its loss and its gradient there.  Neither loss nor gradient is multiplied by temperature^2:
+ * loss and gradient are NaN, as they are (and lse is) with NaN or +inf among the logits.
+ * lse is fp32, and what its rounding leaves (2^-24 |lse|, or all of it where lse is beyond fp32) enters the backward pass'
+ * probabilities; loss and step go by differences from the row's largest logit and do without it, so that a row of the type's lowest value
+ * alone has its loss and its gradient there.  Neither loss nor gradient is multiplied by temperature^2:
  * `weight` is the place for it.
  */
 enum { NVFP4_INDEX_I32 = 0, NVFP4_INDEX_I64 = 1 };
@@ -99,7 +100,7 @@ typedef struct {
   int64_t vocab;           /* logits of a row, 1 .. 2^29                                                       */
   int64_t ld;              /* elements from row to row of logits and dlogits, at least vocab, any alignment     */
   int64_t top;             /* entries of a list, 1 .. 1024                                                     */
-  float temperature;       /* finite, at least 2^-126 (fp32's least normal number)                         */
+  float temperature;       /* finite, at least 2^-126 (fp32's least normal number)                          */
   uint32_t x_dtype;        /* NVFP4_X_BF16 or NVFP4_X_F32: of logits and dlogits                               */
   uint32_t teacher_dtype;  /* the same, of teacher                                                             */
   uint32_t index_dtype;    /* NVFP4_INDEX_I32 or NVFP4_INDEX_I64                                               */

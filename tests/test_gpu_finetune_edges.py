@@ -50,6 +50,20 @@ def test_rows_of_nothing(V):
         assert bool(t[0].isnan().all()) and not bool(t[1].any()) and bool(t[2:].isfinite().all())
 
 
+@pytest.mark.parametrize("value", [INF, float("nan")])
+@pytest.mark.parametrize("V", [1000, 131072, 270000])
+def test_rows_with_a_word_that_is_no_number(V, value):
+    """All results of such a row are NaN, and nothing of the others'."""
+    s = _inputs(4, V, 20, torch.float32, pad=False)
+    s["logits"][1, V // 2] = value
+    args = (s["logits"], s["teacher"], s["index"])
+    loss, lse = F.nvfp4_distill_forward(*args)
+    step_loss, d = F.nvfp4_distill_step(*args, s["weight"])
+    back = F.nvfp4_distill_backward(*args, lse, s["weight"])
+    for t in (loss, lse, step_loss, d, back):
+        assert bool(t[1].isnan().all()) and bool(t[[0, 2, 3]].isfinite().all())
+
+
 BITS = [(5, 1), (90, 8), (190, 16), (70, 40), (150, 100), (300, 1), (700, 12), (1000, 16), (900, 32), (800, 33), (600, 64), (700, 128)]
 
 
