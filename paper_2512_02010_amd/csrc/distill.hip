@@ -532,10 +532,11 @@ int run_backward(const DistillArgs &a, int64_t rows, hipStream_t s) {
 }
 
 // Logits are read here for the last time: where they and the gradient do not fit the device's last cache (256 MB) together, they are loaded past
-// the caches, which leaves them to the gradient's reader; where it can hardly hold the gradient alone, that is stored past them
-// too.  In us, with several batches in turn, all through / loads past: gradients of 512 x 16384 fp32 (34 MB) 13 / 15, 512 x 32768 (67 MB) 25 / 25,
-// 1024 x 32768 (134 MB) 59 / 46, 2048 x 32768 BF16 (134 MB) 59 / 49; a step 60 / 55 and 67 / 60.  Loads past / both: 4096 x 65536 BF16 (537 MB)
-// 227 / 215, a step 242 / 236; but 1024 x 32768 fp32 46 / 55.
+// the caches, which leaves them to the gradient's reader; where it can hardly hold the gradient alone, that is stored past them too.  In us, all
+// through / loads past / both, gradients of BF16 (50021 words) with several batches in turn: 80 MB 43 / 36 / 42, 128 MB 66 / 64 / 64, 192 MB
+// 93 / 95 / 91, 260 MB 123 / 127 / 121, 540 MB 247 / 261 / 248; of fp32 (32768 words): 39 / 33 / 36, 59 / 58 / 54, 87 / 86 / 79, 119 / 120 / 109,
+// 234 / 241 / 217; steps the same way.  With one batch again and again, of which the cache still has a part: BF16 30 / 35 / 40, 48 / 51 / 62, 88 / 70 / 89,
+// 121 / 94 / 120, 247 / 263 / 246.  So storing past begins to pay between 120 MB, where nothing is in the cache, and 300 MB, where as much is as there can be.
 int past_caches(const nvfp4_distill_params *p) {
   const int64_t megabytes = p->rows * p->vocab * (p->x_dtype ? 4 : 2) >> 20;
   return megabytes > 192 ? kBoth : megabytes > 96 ? kLoads : kThrough;
