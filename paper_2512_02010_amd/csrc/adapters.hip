@@ -15,8 +15,8 @@
 //   k_join     sums what several workgroups of k_outer have of one adapter, in a fixed order
 //
 // Forwards that is two launches up to kFewTokens tokens and three beyond, backwards four and five.  Whole calls, among others:
-// 16384 tokens, 4096 x 4096, rank 16, four adapters 116 us (405 MB: 3.5 TB/s, a copy 5.1), of which plan 9, shrink 39, expand 69; backwards 8192
-// tokens, 8192 x 8192, rank 32, eight adapters 205 us (563 MB): plan 8, shrink 37, expand 79, outer 78, join 6.  One token 8.5 us: two launches.
+// 16384 tokens, 4096 x 4096, rank 16, four adapters 117 us (405 MB: 3.5 TB/s, a copy 5.1), of which plan 9, shrink 39, expand 71; backwards 8192
+// tokens, 8192 x 8192, rank 32, eight adapters 205 us (563 MB): plan 9, shrink 40, expand 80, outer 75, join 6.  One token 8.5 us: two launches.
 #include <hip/hip_runtime.h>
 
 #include "finetune/nvfp4_finetune.h"
@@ -28,11 +28,12 @@ namespace {
 constexpr int kMostRank = 128, kMostAdapters = 2048;          // (by the instances of the kernels, by the LDS of k_plan)
 constexpr int kTile = 32;                       // tokens of a planned tile
 constexpr int kFewTile = 16;                    // ... and of a tile that a workgroup finds for itself
-// Forwards, up to here there is no plan (find_tile).  Without / with one, 4096 x 4096, rank 16, 16 adapters: 96 tokens 8.7 / 15.2 us, 192
-// 10.5 / 15.8, 256 17.4 / 15.6; 8192 x 8192, rank 64, 32 adapters: 128 tokens 28.0 / 29.0, 256 43 / 29.
+// Forwards, up to here there is no plan (find_tile).  Without / with one, several batches and their adapters in turn, 4096 x 4096, rank 16, 16
+// adapters: 96 tokens 9.7 / 15.7 us, 192 12.1 / 16.5, 256 17.9 / 16.6; where every token reads much of an adapter, earlier: 8192 x 8192, rank 64, 32
+// adapters: 128 tokens 41 / 32, 256 47 / 31 (28 and 29 at 128 tokens of one batch again and again, whose adapters stay in the caches).
 constexpr int kFewTokens = 192;
 // Backwards, up to here an adapter's gradients are one workgroup's sums and k_join is not needed.  4096 x 4096, rank 16: 256 tokens of
-// one adapter 20.6 us so, 22.7 with k_join, 512 tokens of 16 adapters 32.0 / 35.4, 512 of one 23.3 / 23.5.
+// one adapter 21.7 us so, 23.2 with k_join, 512 tokens of 16 adapters 30.4 / 34.1, 512 of one 24.6 / 24.7.
 constexpr int kWholeTokens = 512;
 constexpr int kPlanThreads = 1024;
 constexpr int kOuterWidth = 128;                // columns of a workgroup of k_outer
@@ -365,7 +366,7 @@ struct Columns {
 // of every term side by side, the third by halves, which fill the four that there are (0 must not meet w, as an infinity would be NaN).
 // A wave has a block of columns of its own and keeps their part of w in registers while it goes through the workgroup's stretch of the
 // plan; per tile the workgroup sums the parts of s h and splits them once, into LDS, while the tile's columns of base are on their way.
-// Bound by base and out.  16384 x 4096 BF16 (268 MB) by itself: 65 us up to rank 32, 76 at 64, 101 at 128; a copy of as much 57.
+// Bound by base and out.  16384 x 4096 BF16 (268 MB), within the call: 70 us at rank 16, 73 at 32, 94 at 64, 138 at 128; a copy of as much 57.
 // Planned, BF16: eight waves a workgroup, two workgroups a compute unit, where 128 registers are enough (up to 32 ranks), or one, where 168 are
 // not (beyond 64); four waves, and three workgroups, in between: 33 to 64 ranks in 128 registers left up to 148 bytes a thread to scratch memory.
 // fp32 four waves, and three or two.  Whole calls with spills / without, 4096 x 4096, rank 64: 4096 tokens 72.4 / 68.5 us, backwards 128 / 120; 16384
@@ -1132,8 +1133,8 @@ extern "C" int nvfp4_adapters_backward(const void *dy, const nvfp4_adapters_para
     if (const int rc = run_expand<kAcross, __bf16>(e, d, s)) return rc;
   }
   // A workgroup has up to 64 ranks, which read x and dy once; where its sums go to the output at once, up to 32, since the gradients are
-  // much of the bytes then and more workgroups write them.  32 / 64, 4096 x 4096, rank 64: one token 26.9 / 28.8 us, 512 of one adapter
-  // 33.8 / 36.7, of 64 adapters 118 / 147; beyond, 8192 tokens of 8 adapters 186 / 178, at 8192 x 8192 322 / 295.
+  // much of the bytes then and more workgroups write them.  32 / 64, 4096 x 4096, rank 64: one token 26.1 / 29.1 us, 512 of one adapter
+  // 31.6 / 35.0, of 64 adapters 119 / 146; beyond, 8192 tokens of 8 adapters 180 / 173, at 8192 x 8192 328 / 300.
   const int ranks = rank <= 16 ? 16 : rank <= 32 || d.whole ? 32 : 64;
   const dim3 grid((uint32_t)(g.half[0].chunks + g.half[1].chunks), (uint32_t)d.ranges, (uint32_t)divide_up(rank, ranks));
   if (const int rc = launch(ranks == 16 ? k_outer<1> : ranks == 32 ? k_outer<2> : k_outer<4>, grid, dim3(256), 0, s, g)) return rc;
