@@ -128,7 +128,7 @@ __device__ inline float below(float v) {
   return bits << 1 ? __uint_as_float((bits - 1) & 0xffff0000u) : v;
 }
 // v as a sum of three BF16 terms, eight of its 24 bits each, exactly; where the result is BF16 too, whose rounding hides what a third term adds only where
-// neither the ranks' products nor the base cancel.  (Two terms, 2^-16 of v left: 16384 x 4096, rank 16 115 us, three 116; rank 64 147 / 149.)
+// neither the ranks' products nor the base cancel.  (Two terms, 2^-16 of v left: 16384 x 4096, rank 16 115 us, three 116; rank 64 146 / 149; 4096 tokens, rank 128 89 / 93.)
 // All terms have v's sign and none is 0 unless v is, so that an infinity that meets them in a product comes out as if it met v: with terms rounded to
 // nearest inf times the second, 0 or of the other sign, made a NaN of it.  (Below 2^-110 BF16 has no numbers for all three.)  Of an infinity, or NaN,
 // the first term is all there is, and the others must not be 0.
@@ -412,7 +412,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
   };
   const T *const base = static_cast<const T *>(a.base);
   T *const out = static_cast<T *>(a.out);
-  const int pieces = (a.rank + 7) / 8;
+  const int pieces = (a.rank + 7) / 8, two = pieces - 1;            // (F == 0: one piece or two, so that `two` divides by shifts)
   const int32_t width = (int32_t)a.width, c0 = ((int32_t)blockIdx.y * kWaves + wave) * kBlock;
   const bool idle = c0 >= width || !out;         // a wave past the last column only helps with h
   const auto column = [&](int half) { return c0 + half * 32 + group * 8; };
@@ -475,7 +475,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
       for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int f = 0; f < kSpans; ++f) {
-          const int piece = F ? f * 4 + group : group % pieces;
+          const int piece = F ? f * 4 + group : group & two;
           w[p][f] = load8(of + (int64_t)(column_of(p) < width ? column_of(p) : width - 1) * a.rank + (piece < pieces ? piece * 8 : 0));
           if (F && piece >= pieces) w[p][f] = bf16x8{};
         }
@@ -504,7 +504,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
         for (int p = half * 2; p < half * 2 + 2; ++p)
 #pragma unroll
           for (int f = 0; f < kSpans; ++f) {
-            int32_t rank = (F ? f * 4 + group : group % pieces) * 8, line = (column_of(p) - c0 - half * 32) * a.rank;
+            int32_t rank = (F ? f * 4 + group : group & two) * 8, line = (column_of(p) - c0 - half * 32) * a.rank;
             asm("" : "+v"(rank), "+v"(line));
             for (int k = 0; k < 8; ++k) w[p][f][k] = rank + k < a.rank ? turn[line + rank + k] : (__bf16)0.0f;
             __builtin_amdgcn_sched_barrier(0);
@@ -534,7 +534,7 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const int piece = F ? group : group % pieces;
+          const int piece = F ? group : group & two;
           for (int k = 0; k < 8; ++k) w[p][f][k] = turn[(piece * 8 + k) * kLine + column_of(p) - c0];
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -568,8 +568,8 @@ __global__ void __launch_bounds__((expand_waves<FEW, T, F>)*64, F == 4 ? 2 : (ex
               if (F) {
                 h = split[buffer][m * 16 + row][place(row, n * kSpans * 4 + f * 4 + group)];
               } else {
-                const int q = n * 4 + group, which = q / pieces < 2 ? q / pieces : 2;
-                h = split[buffer][m * 16 + row][which * 4 + q % pieces];
+                const int q = n * 4 + group, which = q >> two < 2 ? q >> two : 2;
+                h = split[buffer][m * 16 + row][which * 4 + (q & two)];
               }
 #pragma unroll
               for (int p = 0; p < 4; ++p) acc[m][p] = multiply(w[p][f], h, acc[m][p]);
