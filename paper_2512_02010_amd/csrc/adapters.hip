@@ -127,8 +127,9 @@ __device__ inline float below(float v) {
   const uint32_t bits = __float_as_uint(v);
   return bits << 1 ? __uint_as_float((bits - 1) & 0xffff0000u) : v;
 }
-// v as a sum of three BF16 terms, eight of its 24 bits each, exactly; where the result is BF16 too, whose rounding hides what a third term adds only where
-// neither the ranks' products nor the base cancel.  (Two terms, 2^-16 of v left: 16384 x 4096, rank 16 115 us, three 116; rank 64 146 / 149; 4096 tokens, rank 128 89 / 93.)
+// v as a sum of three BF16 terms, eight of its 24 bits each, exactly; where the result is BF16 too, whose rounding hides what a third term adds
+// only where neither the ranks' products nor the base cancel.  (Two terms, 2^-16 of v left, / three: 16384 x 4096, rank 16 115 / 116 us, rank 64
+// 146 / 149; 4096 tokens, rank 128 89 / 93.)
 // All terms have v's sign and none is 0 unless v is, so that an infinity that meets them in a product comes out as if it met v: with terms rounded to
 // nearest inf times the second, 0 or of the other sign, made a NaN of it.  (Below 2^-110 BF16 has no numbers for all three.)  Of an infinity, or NaN,
 // the first term is all there is, and the others must not be 0.

@@ -7,7 +7,7 @@
 // probabilities and the loss are fp32; only the gradient is rounded to the logits' type, once.
 //
 // Whole calls, among others (a copy of as many bytes: 5.1 TB/s): loss of 4096 x 50021 BF16 76 us (5.4 TB/s, read only); gradient of 2047 x 50021
-// BF16 93 us (4.4), of 1024 x 32768 fp32 44 to 58 (4.6 to 6, by what the caches hold); step of 4096 x 131072 BF16 462 us (4.6), of 255 x 50021
+// BF16 93 us (4.4), of 1024 x 32768 fp32 44 to 58 (4.6 to 6, by what the caches hold); step of 4096 x 131072 BF16 460 us (4.7), of 255 x 50021
 // fp32 22 us (4.7).  A row or a few: 5 to 7 us a call, the launch's own; a step of one row of 131072, which one workgroup takes, 19.
 #include <hip/hip_runtime.h>
 
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(NT) k_distill_step(DistillArgs a) {
 // The same with the row in registers, NV pieces a thread.  A workgroup takes row after row: where a piece of the gradient has been
 // written, that piece of the next row is asked for, and kLag pieces later it enters the next row's sum.  So loads and stores are on
 // their way together, and the exponentials of both passes lie over them.  4096 x 131072 BF16: read twice 656 us, in registers 533, with
-// the next row's sum between the stores 477 (and past the caches 462).
+// the next row's sum between the stores 477 (and past the caches 460).
 template <typename T, int NT, int NV, int PAST>
 __global__ void __launch_bounds__(NT) k_distill_rows(DistillArgs a, int32_t rows) {
   constexpr int kPer = Row<T>::kPer, kLag = NV / 4;
