@@ -19,7 +19,7 @@ UNITS += [(PKG / "csrc" / "nvfp4_46.hip", {"NVFP4_46_PART": part}, f"nvfp4_46.pa
 UNITS += [(PKG / "csrc" / "gemm.hip", {"NVFP4_46_GEMM_PART": part}, f"gemm.part{part}")
           for part in (6, 0)]
 UNITS.append((PKG / "csrc" / "nvfp4_46.hip", {"NVFP4_46_PART": 0}, "nvfp4_46.part0"))
-UNITS += [(PKG / "csrc" / f"{name}.hip", {}, name) for name in ("adapters", "distill")]
+UNITS += [(PKG / "csrc" / f"{name}.hip", {}, name) for name in ("adapters", "distill", "weight_product", "experts")]
 SO = PKG / "libnvfp4_46.so"
 PYTHON_SO = PKG / "nvfp4_46_python.so"
 

@@ -1,0 +1,485 @@
+// Tokens to their experts, and back (include/finetune/nvfp4_finetune.h).
+//
+//   xs[place[t][j]] = x_t,  y_t = base_t + sum_j w[t][j] ys[place[t][j]],
+//   dys[place[t][j]] = w[t][j] dy_t,  dw[t][j] = <dy_t, ys[place[t][j]]>
+//
+// All of it is bound by the bytes of the rows.  Every kernel goes by tokens: a token's row is read once and written to all its places
+// (or is summed from them, in the order of j), so nothing is added atomically and a row of 16 bytes or more per lane is whole lines of memory
+// wherever it stands.
+//
+//   k_sort_count, k_sort    pairs in the order of their experts (stable)
+//   k_spread                x to its places
+//   k_combine               weighted sums of places
+//   k_combine_backward      both gradients, ys read once
+#include <hip/hip_runtime.h>
+
+#include "finetune/nvfp4_finetune.h"
+#include "launch.hpp"
+
+namespace nvfp4_46 {
+namespace {
+
+constexpr int64_t kMostTokens = (1 << 24) - 1, kMostWidth = 1 << 22, kMostTop = 64, kMostExperts = 1024, kMostPairs = (int64_t)1 << 30;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int64_t kSortOne = 4096;              // pairs that one workgroup sorts by itself
+constexpr int64_t kSortBlocks = 128;            // ... and of more pairs at most so many workgroups
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// ---- eight adjacent columns ---------------------------------------------------------------------------------------------
+
+template <typename T>
+struct Piece;
+template <>
+struct Piece<__bf16> {
+  bf16x8 v;
+  __device__ void load(const __bf16 *p) { v = *reinterpret_cast<const bf16x8 *>(p); }
+  __device__ void store(__bf16 *p) const { *reinterpret_cast<bf16x8 *>(p) = v; }
+  __device__ f32x8 wide() const { return __builtin_convertvector(v, f32x8); }
+  __device__ void round(f32x8 f) { v = __builtin_convertvector(f, bf16x8); }
+};
+template <>
+struct Piece<float> {
+  f32x4 lo, hi;
+  __device__ void load(const float *p) {
+    lo = *reinterpret_cast<const f32x4 *>(p);
+    hi = *reinterpret_cast<const f32x4 *>(p + 4);
+  }
+  __device__ void store(float *p) const {
+    *reinterpret_cast<f32x4 *>(p) = lo;
+    *reinterpret_cast<f32x4 *>(p + 4) = hi;
+  }
+  __device__ f32x8 wide() const { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+  __device__ void round(f32x8 f) {
+    lo = __builtin_shufflevector(f, f, 0, 1, 2, 3);
+    hi = __builtin_shufflevector(f, f, 4, 5, 6, 7);
+  }
+};
+// (the same type: as it is, every bit of a NaN too)
+template <typename T>
+__device__ inline void convert(Piece<T> &to, const Piece<T> &from) { to = from; }
+__device__ inline void convert(Piece<float> &to, const Piece<__bf16> &from) { to.round(from.wide()); }
+__device__ inline void convert(Piece<__bf16> &to, const Piece<float> &from) { to.round(from.wide()); }
+
+// ---- sort ---------------------------------------------------------------------------------------------------------------
+
+struct SortArgs {
+  const void *ids;
+  int32_t *counts;             // [workgroups][experts + 1], where there is more than one
+  int32_t *place, *token, *begin;
+  int32_t pairs, top, experts;
+  int32_t per;                 // pairs of a workgroup
+  bool wide;                   // ids are 64 bits
+};
+
+// The group of a pair: its expert, `experts` for none.
+__device__ inline int32_t group_of(const SortArgs &a, int32_t pair) {
+  if (a.wide) {
+    const int64_t id = static_cast<const int64_t *>(a.ids)[pair];
+    return id >= 0 && id < a.experts ? (int32_t)id : a.experts;
+  }
+  const int32_t id = static_cast<const int32_t *>(a.ids)[pair];
+  return id >= 0 && id < a.experts ? id : a.experts;
+}
+
+// How many pairs of its stretch every group has, of each workgroup.
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs a) {
+  __shared__ int32_t count[kMostExperts + 1];
+  const int32_t groups = a.experts + 1, first = (int32_t)blockIdx.x * a.per;
+  const int32_t last = a.pairs - first < a.per ? a.pairs : first + a.per;
+  for (int32_t g = threadIdx.x; g < groups; g += kSortThreads) count[g] = 0;
+  __syncthreads();
+  for (int32_t i = first + (int32_t)threadIdx.x; i < last; i += kSortThreads) atomicAdd(&count[group_of(a, i)], 1);
+  __syncthreads();
+  for (int32_t g = threadIdx.x; g < groups; g += kSortThreads) a.counts[(int64_t)blockIdx.x * groups + g] = count[g];
+}
+
+// Stable counting sort.  A wave has an adjacent part of its workgroup's stretch, 64 pairs at a time: how many of each group (pass 0), then, from where
+// the group's first pair of the wave goes, every pair's place (pass 1).
+__global__ void __launch_bounds__(kSortThreads) k_sort(SortArgs a) {
+  extern __shared__ int32_t counts[];            // [16][line]: each wave's pairs of a group, then where the next of them goes
+  const int32_t groups = a.experts + 1, line = groups + 1;
+  int32_t *const prior = counts + kSortWaves * line, *const total = prior + groups;      // pairs of earlier workgroups, of all
+  __shared__ int32_t sums[kSortWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  int32_t *const mine = counts + wave * line;
+  for (int32_t i = threadIdx.x; i < kSortWaves * line + 2 * groups; i += kSortThreads) counts[i] = 0;
+  __syncthreads();
+  const int32_t first = (int32_t)blockIdx.x * a.per, stop = a.pairs - first < a.per ? a.pairs : first + a.per;
+  const int32_t slice = a.per / kSortWaves, begin = first + wave * slice;
+  const int32_t end = stop - begin < slice ? stop : begin + slice;        // (of a wave past the stretch: before its begin)
+  // the lanes with this lane's group
+  const auto alike = [&](int32_t l) {
+    uint64_t m = ~(uint64_t)0;
+    for (int32_t bit = 1; bit <= groups; bit <<= 1) {
+      const uint64_t set = __ballot((l & bit) != 0);
+      m &= l & bit ? set : ~set;
+    }
+    return m;
+  };
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int32_t i0 = begin; i0 < end; i0 += 64) {
+      const int32_t i = i0 + lane, l = i < end ? group_of(a, i) : groups;       // (past the end: a group of its own, which nobody reads)
+      const uint64_t m = alike(l);
+      const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1));
+      // A wave's LDS instructions run in their order, so the lanes have all read before the first of each group adds; the fences keep
+      // the compiler to it.
+      if (pass == 1) {
+        const int32_t at = mine[l] + before;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (i < end) {
+          const bool is = l < a.experts;
+          a.place[i] = is ? at : ~at;
+          a.token[at] = is ? (int32_t)((uint32_t)i / (uint32_t)a.top) : -1;
+        }
+      }
+      if (before == 0) __hip_atomic_fetch_add(mine + l, __popcll(m), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    if (pass == 1) break;
+    if (gridDim.x > 1) {
+      // (as many threads to a group as there are; whole numbers, whose sums do not depend on their order)
+      const int32_t parts = groups < kSortThreads ? kSortThreads / groups : 1;
+      for (int32_t i = threadIdx.x; i < parts * groups; i += kSortThreads) {
+        const int32_t g = i % groups;
+        int32_t before = 0, all = 0;
+        for (int32_t b = i / groups; b < (int32_t)gridDim.x; b += parts) {
+          const int32_t n = a.counts[(int64_t)b * groups + g];
+          all += n;
+          before += b < (int32_t)blockIdx.x ? n : 0;
+        }
+        atomicAdd(prior + g, before);
+        atomicAdd(total + g, all);
+      }
+    }
+    __syncthreads();
+    // the groups one after the other, in each the workgroups', in each the waves' pairs: a thread has adjacent groups
+    const int32_t per = (groups + kSortThreads - 1) / kSortThreads, g0 = (int32_t)threadIdx.x * per;
+    int32_t here = 0;
+    for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
+      int32_t n = 0;
+      for (int w = 0; w < kSortWaves; ++w) {
+        const int32_t of = counts[w * line + g];
+        counts[w * line + g] = n;
+        n += of;
+      }
+      if (gridDim.x == 1) total[g] = n;
+      here += total[g];
+    }
+    int32_t upto = here;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int32_t other = __shfl_up(upto, d);
+      if (lane >= d) upto += other;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int32_t at = upto - here;
+    for (int w = 0; w < wave; ++w) at += sums[w];
+    for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
+      for (int w = 0; w < kSortWaves; ++w) counts[w * line + g] += at + prior[g];
+      if (blockIdx.x == 0) a.begin[g] = at;      // (of the group without an expert: the end of the last expert's)
+      at += total[g];
+    }
+    __syncthreads();
+  }
+}
+
+// ---- spread -------------------------------------------------------------------------------------------------------------
+
+struct RowArgs {
+  const void *token_rows;      // x, base, dy
+  void *token_out;             // y
+  const void *slot_rows;       // ys
+  void *slot_out;              // xs, dys
+  const int32_t *place;
+  const float *weights;
+  float *dweights;
+  int64_t ld_token, ld_base, ld_slot, ld_dslot;
+  int32_t tokens, top, pieces; // pieces of eight columns to a row
+  int32_t slots;
+  int32_t lanes;               // to a token: 64 / lanes tokens share a wave where rows are short
+};
+
+constexpr int kRowThreads = 256;
+
+// Where a lane works: its token and its first piece; the next ones are `lanes` further on.
+struct Spot {
+  int32_t token, piece;
+};
+template <int U>
+__device__ inline Spot spot_of(const RowArgs &a) {
+  const int32_t in = (int32_t)threadIdx.x & (a.lanes - 1), of = (int32_t)threadIdx.x / a.lanes;
+  return {(int32_t)blockIdx.x * (kRowThreads / a.lanes) + of, (int32_t)blockIdx.y * (a.lanes * U) + in};
+}
+
+template <typename TI, typename TO, int U>
+__global__ void __launch_bounds__(kRowThreads) k_spread(RowArgs a) {
+  const Spot at = spot_of<U>(a);
+  if (at.token >= a.tokens) return;
+  const TI *const x = static_cast<const TI *>(a.token_rows) + (int64_t)at.token * a.ld_token;
+  Piece<TO> v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int32_t piece = at.piece + u * a.lanes;
+    Piece<TI> in;
+    if (piece < a.pieces) {
+      in.load(x + (int64_t)piece * 8);
+      convert(v[u], in);
+    }
+  }
+  const int32_t *const place = a.place + (int64_t)at.token * a.top;
+  for (int32_t j = 0; j < a.top; ++j) {
+    const int32_t p = place[j], slot = p < 0 ? ~p : p;
+    if (slot >= a.slots) continue;
+    TO *const to = static_cast<TO *>(a.slot_out) + (int64_t)slot * a.ld_slot;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t piece = at.piece + u * a.lanes;
+      if (piece >= a.pieces) continue;
+      Piece<TO> out = v[u];
+      if (p < 0) out.round(f32x8{});
+      out.store(to + (int64_t)piece * 8);
+    }
+  }
+}
+
+// ---- combine ------------------------------------------------------------------------------------------------------------
+
+template <typename TS, typename TT, int U>
+__global__ void __launch_bounds__(kRowThreads) k_combine(RowArgs a) {
+  const Spot at = spot_of<U>(a);
+  if (at.token >= a.tokens) return;
+  f32x8 sum[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int32_t piece = at.piece + u * a.lanes;
+    sum[u] = f32x8{};
+    if (a.token_rows && piece < a.pieces) {
+      Piece<TT> base;
+      base.load(static_cast<const TT *>(a.token_rows) + (int64_t)at.token * a.ld_base + (int64_t)piece * 8);
+      sum[u] = base.wide();
+    }
+  }
+  const int32_t *const place = a.place + (int64_t)at.token * a.top;
+  for (int32_t j = 0; j < a.top; ++j) {
+    const int32_t p = place[j];
+    if (p < 0 || p >= a.slots) continue;
+    const float w = a.weights ? a.weights[(int64_t)at.token * a.top + j] : 1.0f;
+    const TS *const from = static_cast<const TS *>(a.slot_rows) + (int64_t)p * a.ld_slot;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t piece = at.piece + u * a.lanes;
+      if (piece >= a.pieces) continue;
+      Piece<TS> in;
+      in.load(from + (int64_t)piece * 8);
+      sum[u] += w * in.wide();
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int32_t piece = at.piece + u * a.lanes;
+    if (piece >= a.pieces) continue;
+    Piece<TT> out;
+    out.round(sum[u]);
+    out.store(static_cast<TT *>(a.token_out) + (int64_t)at.token * a.ld_token + (int64_t)piece * 8);
+  }
+}
+
+// A workgroup has a token.  (ys may be dys: an element is read before the same lane writes it.)
+template <typename TS, typename TT>
+__global__ void __launch_bounds__(kRowThreads) k_combine_backward(RowArgs a) {
+  __shared__ float part[kRowThreads / 64];
+  const int32_t token = (int32_t)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const TT *const dy = static_cast<const TT *>(a.token_rows) + (int64_t)token * a.ld_token;
+  for (int32_t j = 0; j < a.top; ++j) {
+    const int32_t p = a.place[(int64_t)token * a.top + j], slot = p < 0 ? ~p : p;
+    const bool is = p >= 0 && p < a.slots;
+    const float w = is ? a.weights[(int64_t)token * a.top + j] : 0.0f;
+    const TS *const ys = static_cast<const TS *>(a.slot_rows) + (int64_t)slot * a.ld_slot;
+    TS *const dys = static_cast<TS *>(a.slot_out) + (int64_t)slot * a.ld_dslot;
+    float dot = 0.0f;
+    for (int32_t piece = threadIdx.x; slot < a.slots && piece < a.pieces; piece += kRowThreads) {
+      Piece<TS> out;
+      out.round(f32x8{});
+      if (is) {
+        Piece<TT> d;
+        d.load(dy + (int64_t)piece * 8);
+        Piece<TS> y;
+        y.load(ys + (int64_t)piece * 8);
+        const f32x8 dv = d.wide(), yv = y.wide();
+        for (int i = 0; i < 8; ++i) dot += dv[i] * yv[i];
+        out.round(w * dv);
+      }
+      out.store(dys + (int64_t)piece * 8);
+    }
+    for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+    if (lane == 0) part[wave] = dot;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      float all = 0.0f;
+      for (int i = 0; i < kRowThreads / 64; ++i) all += part[i];
+      a.dweights[(int64_t)token * a.top + j] = is ? all : 0.0f;
+    }
+    __syncthreads();
+  }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+
+int64_t divide_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool at(const void *ptr, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(ptr) % bytes == 0; }
+bool pairs_fit(const nvfp4_experts_params &p) {
+  return p.tokens >= 0 && p.tokens <= kMostTokens && p.top > 0 && p.top <= kMostTop && p.tokens * p.top <= kMostPairs;
+}
+bool sort_fits(const nvfp4_experts_params &p) { return pairs_fit(p) && p.experts > 0 && p.experts <= kMostExperts; }
+bool width_fits(const nvfp4_experts_params &p) { return pairs_fit(p) && p.width > 0 && p.width <= kMostWidth && p.width % 8 == 0; }
+bool stride_fits(int64_t ld, int64_t width, int64_t rows) {
+  return ld >= width && ld <= ((int64_t)1 << 40) / (rows > 0 ? rows : 1);
+}
+bool types_fit(const nvfp4_experts_params &p) { return p.token_dtype <= NVFP4_X_F32 && p.slot_dtype <= NVFP4_X_F32; }
+
+int64_t sort_blocks(const nvfp4_experts_params &p) {
+  const int64_t pairs = p.tokens * p.top;
+  if (pairs <= kSortOne) return 1;
+  const int64_t blocks = divide_up(pairs, kSortThreads);
+  return blocks < kSortBlocks ? blocks : kSortBlocks;
+}
+int64_t sort_bytes(const nvfp4_experts_params &p) {
+  const int64_t blocks = sort_blocks(p);
+  return blocks == 1 ? 16 : divide_up(blocks * (p.experts + 1) * 4, 16) * 16;
+}
+constexpr size_t sort_lds(int64_t experts) { return (kSortWaves * (experts + 2) + 2 * (experts + 1)) * 4; }
+
+// Tokens across, columns down: lanes to a token, and the grid for U pieces a lane.
+template <int U>
+dim3 row_grid(RowArgs &a) {
+  int32_t lanes = 1;
+  while (lanes < 64 && lanes < a.pieces) lanes *= 2;
+  a.lanes = lanes;
+  return dim3((uint32_t)divide_up(a.tokens, kRowThreads / lanes), (uint32_t)divide_up(a.pieces, lanes * U));
+}
+
+// kernel<types of slots and tokens> for the types of a call
+template <typename F>
+int by_types(const nvfp4_experts_params &p, F f) {
+  const bool s = p.slot_dtype == NVFP4_X_F32, t = p.token_dtype == NVFP4_X_F32;
+  return s ? t ? f(float{}, float{}) : f(float{}, __bf16{}) : t ? f(__bf16{}, float{}) : f(__bf16{}, __bf16{});
+}
+
+RowArgs row_args(const nvfp4_experts_params &p, const int32_t *place) {
+  RowArgs a{};
+  a.place = place;
+  a.ld_token = p.ld_token;
+  a.ld_base = p.ld_base;
+  a.ld_slot = p.ld_slot;
+  a.ld_dslot = p.ld_dslot;
+  a.tokens = (int32_t)p.tokens;
+  a.top = (int32_t)p.top;
+  a.pieces = (int32_t)(p.width / 8);
+  a.slots = (int32_t)(p.tokens * p.top);
+  return a;
+}
+
+}  // namespace
+}  // namespace nvfp4_46
+
+using namespace nvfp4_46;
+
+extern "C" size_t nvfp4_experts_workspace_bytes(const nvfp4_experts_params *p) {
+  return p && sort_fits(*p) ? (size_t)sort_bytes(*p) : 0;
+}
+
+extern "C" int nvfp4_experts_sort(const void *ids, const nvfp4_experts_params *p, int32_t *place, int32_t *token, int32_t *begin,
+                                  void *workspace, size_t workspace_bytes, void *stream) {
+  if (!p) return NVFP4_ERR_NULL;
+  if (!sort_fits(*p)) return NVFP4_ERR_SHAPE;
+  if (!begin || !workspace || (p->tokens != 0 && (!ids || !place || !token))) return NVFP4_ERR_NULL;
+  if (p->index_dtype > NVFP4_INDEX_I64) return NVFP4_ERR_PARAM;
+  if (!at(ids, p->index_dtype == NVFP4_INDEX_I64 ? 8 : 4) || !at(place, 4) || !at(token, 4) || !at(begin, 4) || !at(workspace, 16))
+    return NVFP4_ERR_ALIGN;
+  if (workspace_bytes < (size_t)sort_bytes(*p)) return NVFP4_ERR_PARAM;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t pairs = p->tokens * p->top, blocks = sort_blocks(*p);
+  // (whole steps of 64 pairs for each wave)
+  const int64_t per = pairs ? divide_up(divide_up(pairs, blocks), kSortThreads) * kSortThreads : kSortThreads;
+  const int64_t used = pairs ? divide_up(pairs, per) : 1;
+  const SortArgs a{ids, static_cast<int32_t *>(workspace), place, token, begin, (int32_t)pairs, (int32_t)p->top,
+                   (int32_t)p->experts, (int32_t)per, p->index_dtype == NVFP4_INDEX_I64};
+  if (used > 1)
+    if (const int rc = launch(k_sort_count, dim3((uint32_t)used), dim3(kSortThreads), 0, s, a)) return rc;
+  const size_t bytes = sort_lds(p->experts);
+  // (the limit belongs to the kernel and not to the call, so it is always the same)
+  if (bytes > 48 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k_sort), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)sort_lds(kMostExperts)) != hipSuccess)
+    return NVFP4_ERR_HIP;
+  return launch(k_sort, dim3((uint32_t)used), dim3(kSortThreads), bytes, s, a);
+}
+
+extern "C" int nvfp4_experts_spread(const void *x, const nvfp4_experts_params *p, const int32_t *place, void *xs, void *stream) {
+  if (!p) return NVFP4_ERR_NULL;
+  if (!width_fits(*p)) return NVFP4_ERR_SHAPE;
+  if (p->tokens != 0 && (!x || !place || !xs)) return NVFP4_ERR_NULL;
+  if (!stride_fits(p->ld_token, p->width, p->tokens) || !stride_fits(p->ld_slot, p->width, p->tokens * p->top)) return NVFP4_ERR_SHAPE;
+  if (!at(x, 16) || !at(xs, 16) || !at(place, 4) || p->ld_token % 8 || p->ld_slot % 8) return NVFP4_ERR_ALIGN;
+  if (!types_fit(*p)) return NVFP4_ERR_PARAM;
+  if (p->tokens == 0) return NVFP4_OK;
+  RowArgs a = row_args(*p, place);
+  a.token_rows = x;
+  a.slot_out = xs;
+  return by_types(*p, [&](auto slot, auto token) {
+    const dim3 grid = row_grid<2>(a);
+    return launch(k_spread<decltype(token), decltype(slot), 2>, grid, dim3(kRowThreads), 0, static_cast<hipStream_t>(stream), a);
+  });
+}
+
+extern "C" int nvfp4_experts_combine(const void *ys, const nvfp4_experts_params *p, const int32_t *place, const float *weights,
+                                     const void *base, void *y, void *stream) {
+  if (!p) return NVFP4_ERR_NULL;
+  if (!width_fits(*p)) return NVFP4_ERR_SHAPE;
+  if (p->tokens != 0 && (!ys || !place || !y)) return NVFP4_ERR_NULL;
+  if (!stride_fits(p->ld_token, p->width, p->tokens) || !stride_fits(p->ld_slot, p->width, p->tokens * p->top) ||
+      (base && !stride_fits(p->ld_base, p->width, p->tokens)) || (base && base == y && p->ld_base != p->ld_token))
+    return NVFP4_ERR_SHAPE;
+  if (!at(ys, 16) || !at(y, 16) || !at(base, 16) || !at(place, 4) || !at(weights, 4) || p->ld_token % 8 || p->ld_slot % 8 ||
+      (base && p->ld_base % 8))
+    return NVFP4_ERR_ALIGN;
+  if (!types_fit(*p)) return NVFP4_ERR_PARAM;
+  if (p->tokens == 0) return NVFP4_OK;
+  RowArgs a = row_args(*p, place);
+  a.token_rows = base;
+  a.token_out = y;
+  a.slot_rows = ys;
+  a.weights = weights;
+  return by_types(*p, [&](auto slot, auto token) {
+    const dim3 grid = row_grid<2>(a);
+    return launch(k_combine<decltype(slot), decltype(token), 2>, grid, dim3(kRowThreads), 0, static_cast<hipStream_t>(stream), a);
+  });
+}
+
+extern "C" int nvfp4_experts_combine_backward(const void *dy, const nvfp4_experts_params *p, const void *ys, const int32_t *place,
+                                              const float *weights, void *dys, float *dweights, void *stream) {
+  if (!p) return NVFP4_ERR_NULL;
+  if (!width_fits(*p)) return NVFP4_ERR_SHAPE;
+  if (p->tokens != 0 && (!dy || !ys || !place || !weights || !dys || !dweights)) return NVFP4_ERR_NULL;
+  if (!stride_fits(p->ld_token, p->width, p->tokens) || !stride_fits(p->ld_slot, p->width, p->tokens * p->top) ||
+      !stride_fits(p->ld_dslot, p->width, p->tokens * p->top) || (ys && ys == dys && p->ld_slot != p->ld_dslot))
+    return NVFP4_ERR_SHAPE;
+  if (!at(dy, 16) || !at(ys, 16) || !at(dys, 16) || !at(place, 4) || !at(weights, 4) || !at(dweights, 4) || p->ld_token % 8 ||
+      p->ld_slot % 8 || p->ld_dslot % 8)
+    return NVFP4_ERR_ALIGN;
+  if (!types_fit(*p)) return NVFP4_ERR_PARAM;
+  if (p->tokens == 0) return NVFP4_OK;
+  RowArgs a = row_args(*p, place);
+  a.token_rows = dy;
+  a.slot_rows = ys;
+  a.slot_out = dys;
+  a.weights = weights;
+  a.dweights = dweights;
+  return by_types(*p, [&](auto slot, auto token) {
+    return launch(k_combine_backward<decltype(slot), decltype(token)>, dim3((uint32_t)a.tokens), dim3(kRowThreads), 0,
+                  static_cast<hipStream_t>(stream), a);
+  });
+}

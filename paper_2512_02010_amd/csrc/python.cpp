@@ -51,6 +51,13 @@ struct FinetuneEntryPoints {
   decltype(&nvfp4_distill_forward) distill_forward;
   decltype(&nvfp4_distill_backward) distill_backward;
   decltype(&nvfp4_distill_step) distill_step;
+  decltype(&nvfp4_weight_product) weight_product;
+  decltype(&nvfp4_experts_product) experts_product;
+  decltype(&nvfp4_experts_workspace_bytes) experts_workspace_bytes;
+  decltype(&nvfp4_experts_sort) experts_sort;
+  decltype(&nvfp4_experts_spread) experts_spread;
+  decltype(&nvfp4_experts_combine) experts_combine;
+  decltype(&nvfp4_experts_combine_backward) experts_combine_backward;
 };
 FinetuneEntryPoints finetune;
 PyObject *error_class;     // Nvfp4Error(status, name of the entry point)
@@ -648,6 +655,8 @@ PyObject *adapters_backward(PyObject *const *v, Py_ssize_t n) {
   return PyTuple_Pack(3, dx.o, da.o, db.o);
 }
 
+bool known(at::ScalarType s) { return s == at::kFloat || s == at::kBFloat16; }
+
 // What the three distillation calls have in common: logits, teacher, index, temperature
 struct Distill {
   nvfp4_distill_params p{};
@@ -656,7 +665,6 @@ struct Distill {
   explicit Distill(PyObject *const *v) : x(tensor(v[0], "logits")) {
     const at::Tensor &t = tensor(v[1], "teacher"), &i = tensor(v[2], "index");
     if (x.dim() != 2 || t.dim() != 2) fail(PyExc_AssertionError, "logits and teacher must be matrices");
-    const auto known = [](at::ScalarType s) { return s == at::kFloat || s == at::kBFloat16; };
     if (!known(x.scalar_type()) || !known(t.scalar_type())) fail(PyExc_AssertionError, "logits and teacher must be BF16 or fp32");
     if (i.scalar_type() != at::kInt && i.scalar_type() != at::kLong) fail(PyExc_AssertionError, "index must be int32 or int64");
     p.rows = x.size(0), p.vocab = x.size(1), p.top = t.size(1);
@@ -728,6 +736,179 @@ PyObject *distill_step(PyObject *const *v, Py_ssize_t n) {
   return PyTuple_Pack(2, loss.o, out.o);
 }
 
+// ---- experts.py: products with activations as they are, tokens to their experts and back.
+
+// A given tensor, or a new one of this shape.
+Owned out_or_new(PyObject *given, at::IntArrayRef shape, at::ScalarType type, PyObject *like, PyObject *allocate) {
+  return given == Py_None ? Owned(new_tensor(shape, type, like, allocate)) : Owned(Py_NewRef(given));
+}
+// The type of an output: that of a given tensor, else `fallback`.
+at::ScalarType type_of(PyObject *given, at::ScalarType fallback, const char *what) {
+  const at::ScalarType type = given == Py_None ? fallback : tensor(given, what).scalar_type();
+  if (!known(type)) misfit(what, "BF16 or fp32");
+  return type;
+}
+at::ScalarType out_type(PyObject *code) {
+  const uint64_t w = word(code);
+  if (w > NVFP4_OUT_F32) fail(PyExc_AssertionError, "out_dtype must be OUT_BF16 or OUT_F32");
+  return w == NVFP4_OUT_F32 ? at::kFloat : at::kBFloat16;
+}
+
+// What the two products have in common: x, codes, scales, alpha, out_dtype, flags.
+struct Product {
+  nvfp4_product_params p{};
+  const at::Tensor &x;
+  const void *px, *codes, *scales;
+  const float *alpha;
+  at::ScalarType type;
+  Product(PyObject *x_, PyObject *c, PyObject *s, PyObject *a, PyObject *out_dtype, PyObject *flags, PyObject *given, bool many)
+      : x(tensor(x_, "x")) {
+    const at::Tensor &t = tensor(c, "codes");
+    if (x.dim() != 2 || t.dim() != (many ? 3 : 2)) fail(PyExc_AssertionError, "x must be a matrix, codes one, or one for each expert");
+    if (!known(x.scalar_type())) misfit("x", "BF16 or fp32");
+    p.rows = x.size(0), p.inp = x.size(1), p.out = t.size(many ? 1 : 0), p.experts = many ? t.size(0) : 1;
+    p.x_dtype = x.scalar_type() == at::kFloat ? NVFP4_X_F32 : NVFP4_X_BF16;
+    p.flags = (uint32_t)word(flags);
+    type = given == Py_None ? out_type(out_dtype) : type_of(given, at::kFloat, "out");
+    p.out_dtype = type == at::kFloat ? NVFP4_OUT_F32 : NVFP4_OUT_BF16;
+    px = rows_of(x_, "x", x, p.rows, p.inp, x.scalar_type(), &p.ld_x);
+    const int64_t lines = p.flags & NVFP4_GEMM_B_TILE_SCALES ? p.out / 16 : p.out;
+    codes = many ? dense(c, "codes", x, {p.experts, p.out, p.inp / 2}, at::kByte) : dense(c, "codes", x, {p.out, p.inp / 2}, at::kByte);
+    scales = many ? dense(s, "scales", x, {p.experts, lines, p.inp / 16}, at::kByte) : dense(s, "scales", x, {lines, p.inp / 16}, at::kByte);
+    alpha = static_cast<const float *>(dense(a, "alpha", x, {p.experts}, at::kFloat));
+  }
+  void *rows_out(PyObject *o) { return rows_of(o, "out", x, p.slots, p.out, type, &p.ld_out); }
+};
+
+// x, codes, scales, alpha, out_dtype, flags, out or None, allocate, stream
+PyObject *weight_product(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 9);
+  Product d(v[0], v[1], v[2], v[3], v[4], v[5], v[6], false);
+  d.p.slots = d.p.rows;
+  const OnStream on(v[8], d.x);
+  Owned out = out_or_new(v[6], {d.p.slots, d.p.out}, d.type, v[0], v[7]);
+  void *const po = d.rows_out(out.o);
+  run("nvfp4_weight_product", [&] { return finetune.weight_product(d.px, &d.p, d.codes, d.scales, d.alpha, po, on.handle()); });
+  return out.release();
+}
+
+// x, token or None, begin, codes, scales, alpha, out_dtype, flags, out or None, allocate, stream
+PyObject *experts_product(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 11);
+  Product d(v[0], v[3], v[4], v[5], v[6], v[7], v[8], true);
+  d.p.slots = d.p.rows;
+  const int32_t *token = nullptr;
+  if (v[1] != Py_None) {
+    const at::Tensor &t = tensor(v[1], "token");
+    if (t.dim() != 1) misfit("token", "a vector");
+    d.p.slots = t.size(0);
+    token = static_cast<const int32_t *>(dense(v[1], "token", d.x, {d.p.slots}, at::kInt));
+  }
+  const auto *const begin = static_cast<const int32_t *>(dense(v[2], "begin", d.x, {d.p.experts + 1}, at::kInt));
+  const OnStream on(v[10], d.x);
+  Owned out = out_or_new(v[8], {d.p.slots, d.p.out}, d.type, v[0], v[9]);
+  void *const po = d.rows_out(out.o);
+  run("nvfp4_experts_product",
+      [&] { return finetune.experts_product(d.px, &d.p, token, begin, d.codes, d.scales, d.alpha, po, on.handle()); });
+  return out.release();
+}
+
+// ids, experts, workspace or None, allocate, stream -> place, token, begin
+PyObject *experts_sort(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 5);
+  const at::Tensor &ids = tensor(v[0], "ids");
+  if (ids.dim() != 2) misfit("ids", "a matrix");
+  if (ids.scalar_type() != at::kInt && ids.scalar_type() != at::kLong) misfit("ids", "int32 or int64");
+  nvfp4_experts_params p{};
+  p.tokens = ids.size(0), p.top = ids.size(1), p.experts = (int64_t)word(v[1]);
+  p.index_dtype = ids.scalar_type() == at::kLong ? NVFP4_INDEX_I64 : NVFP4_INDEX_I32;
+  const void *const pi = dense(v[0], "ids", ids, {p.tokens, p.top}, ids.scalar_type());
+  check_workspace(v[2], ids);
+  const int64_t need = (int64_t)finetune.experts_workspace_bytes(&p);
+  if (need == 0) run("nvfp4_experts_sort", [] { return (int)NVFP4_ERR_SHAPE; });          // (before anything of these sizes is made)
+  const OnStream on(v[4], ids);
+  Owned place(new_tensor({p.tokens, p.top}, at::kInt, v[0], v[3])), token(new_tensor({p.tokens * p.top}, at::kInt, v[0], v[3])),
+      begin(new_tensor({p.experts + 1}, at::kInt, v[0], v[3]));
+  auto *const pp = static_cast<int32_t *>(pointer(place.o)), *const pt = static_cast<int32_t *>(pointer(token.o)),
+             *const pb = static_cast<int32_t *>(pointer(begin.o));
+  const Scratch w(v[2], need, v[0], v[3]);
+  run("nvfp4_experts_sort", [&] { return finetune.experts_sort(pi, &p, pp, pt, pb, w.p, w.bytes, on.handle()); });
+  return PyTuple_Pack(3, place.o, token.o, begin.o);
+}
+
+// The sizes that place [tokens][top] gives.
+nvfp4_experts_params places(PyObject *o) {
+  const at::Tensor &t = tensor(o, "place");
+  if (t.dim() != 2) misfit("place", "a matrix");
+  nvfp4_experts_params p{};
+  p.tokens = t.size(0), p.top = t.size(1);
+  return p;
+}
+uint32_t dtype_of(at::ScalarType t) { return t == at::kFloat ? NVFP4_X_F32 : NVFP4_X_BF16; }
+
+// x, place, out_dtype or None, out or None, allocate, stream
+PyObject *experts_spread(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 6);
+  const at::Tensor &x = tensor(v[0], "x");
+  nvfp4_experts_params p = places(v[1]);
+  if (x.dim() != 2) misfit("x", "a matrix");
+  if (!known(x.scalar_type())) misfit("x", "BF16 or fp32");
+  p.width = x.size(1), p.token_dtype = dtype_of(x.scalar_type());
+  const void *const px = rows_of(v[0], "x", x, p.tokens, p.width, x.scalar_type(), &p.ld_token);
+  const auto *const pp = static_cast<const int32_t *>(dense(v[1], "place", x, {p.tokens, p.top}, at::kInt));
+  const at::ScalarType type = type_of(v[3], v[2] == Py_None ? x.scalar_type() : out_type(v[2]), "out");
+  p.slot_dtype = dtype_of(type);
+  const OnStream on(v[5], x);
+  Owned out = out_or_new(v[3], {p.tokens * p.top, p.width}, type, v[0], v[4]);
+  void *const po = rows_of(out.o, "out", x, p.tokens * p.top, p.width, type, &p.ld_slot);
+  run("nvfp4_experts_spread", [&] { return finetune.experts_spread(px, &p, pp, po, on.handle()); });
+  return out.release();
+}
+
+// ys, place, weights or None, base or None, out_dtype or None, out or None, allocate, stream
+PyObject *experts_combine(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 8);
+  const at::Tensor &ys = tensor(v[0], "ys");
+  nvfp4_experts_params p = places(v[1]);
+  if (ys.dim() != 2) misfit("ys", "a matrix");
+  if (!known(ys.scalar_type())) misfit("ys", "BF16 or fp32");
+  p.width = ys.size(1), p.slot_dtype = dtype_of(ys.scalar_type());
+  const void *const py = rows_of(v[0], "ys", ys, p.tokens * p.top, p.width, ys.scalar_type(), &p.ld_slot);
+  const auto *const pp = static_cast<const int32_t *>(dense(v[1], "place", ys, {p.tokens, p.top}, at::kInt));
+  const float *const pw =
+      v[2] == Py_None ? nullptr : static_cast<const float *>(dense(v[2], "weights", ys, {p.tokens, p.top}, at::kFloat));
+  const at::ScalarType type = type_of(v[3] != Py_None ? v[3] : v[5], v[4] == Py_None ? ys.scalar_type() : out_type(v[4]), "base and out");
+  p.token_dtype = dtype_of(type);
+  const void *const base = v[3] == Py_None ? nullptr : rows_of(v[3], "base", ys, p.tokens, p.width, type, &p.ld_base);
+  const OnStream on(v[7], ys);
+  Owned out = out_or_new(v[5], {p.tokens, p.width}, type, v[0], v[6]);
+  void *const po = rows_of(out.o, "out", ys, p.tokens, p.width, type, &p.ld_token);
+  run("nvfp4_experts_combine", [&] { return finetune.experts_combine(py, &p, pp, pw, base, po, on.handle()); });
+  return out.release();
+}
+
+// dy, ys, place, weights, out or None, allocate, stream -> dys, dweights
+PyObject *experts_combine_backward(PyObject *const *v, Py_ssize_t n) {
+  expect(n, 7);
+  const at::Tensor &ys = tensor(v[1], "ys"), &dy = tensor(v[0], "dy");
+  nvfp4_experts_params p = places(v[2]);
+  if (ys.dim() != 2) misfit("ys", "a matrix");
+  if (!known(ys.scalar_type()) || !known(dy.scalar_type())) misfit("ys and dy", "BF16 or fp32");
+  p.width = ys.size(1), p.slot_dtype = dtype_of(ys.scalar_type()), p.token_dtype = dtype_of(dy.scalar_type());
+  const void *const py = rows_of(v[1], "ys", ys, p.tokens * p.top, p.width, ys.scalar_type(), &p.ld_slot);
+  const void *const pd = rows_of(v[0], "dy", ys, p.tokens, p.width, dy.scalar_type(), &p.ld_token);
+  const auto *const pp = static_cast<const int32_t *>(dense(v[2], "place", ys, {p.tokens, p.top}, at::kInt));
+  const auto *const pw = static_cast<const float *>(dense(v[3], "weights", ys, {p.tokens, p.top}, at::kFloat));
+  const OnStream on(v[6], ys);
+  Owned dys = out_or_new(v[4], {p.tokens * p.top, p.width}, ys.scalar_type(), v[1], v[5]);
+  void *const po = rows_of(dys.o, "out", ys, p.tokens * p.top, p.width, ys.scalar_type(), &p.ld_dslot);
+  Owned dw(new_tensor({p.tokens, p.top}, at::kFloat, v[1], v[5]));
+  float *const pdw = static_cast<float *>(pointer(dw.o));
+  run("nvfp4_experts_combine_backward",
+      [&] { return finetune.experts_combine_backward(pd, &p, py, pp, pw, po, pdw, on.handle()); });
+  return PyTuple_Pack(2, dys.o, dw.o);
+}
+
 template <typename Points>
 void take_addresses(Points &points, PyObject *const *a, Py_ssize_t n) {
   constexpr Py_ssize_t kEntries = sizeof(Points) / sizeof(void *);
@@ -761,6 +942,8 @@ PyMethodDef methods[] = {NV_METHOD(connect), NV_METHOD(connect_layer),
                          NV_METHOD(product_of_rows), NV_METHOD(product_of_columns),
                          NV_METHOD(connect_finetune), NV_METHOD(adapters_forward), NV_METHOD(adapters_backward),
                          NV_METHOD(distill_forward), NV_METHOD(distill_backward), NV_METHOD(distill_step),
+                         NV_METHOD(weight_product), NV_METHOD(experts_product), NV_METHOD(experts_sort), NV_METHOD(experts_spread),
+                         NV_METHOD(experts_combine), NV_METHOD(experts_combine_backward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "nvfp4_46_python", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -19,7 +19,9 @@ from . import linear as L
 
 INDEX_I32, INDEX_I64 = 0, 1
 ENTRY_POINTS = ("nvfp4_adapters_workspace_bytes", "nvfp4_adapters_forward", "nvfp4_adapters_backward", "nvfp4_distill_forward",
-                "nvfp4_distill_backward", "nvfp4_distill_step")
+                "nvfp4_distill_backward", "nvfp4_distill_step", "nvfp4_weight_product", "nvfp4_experts_product",
+                "nvfp4_experts_workspace_bytes", "nvfp4_experts_sort", "nvfp4_experts_spread", "nvfp4_experts_combine",
+                "nvfp4_experts_combine_backward")        # (the last seven: experts.py)
 
 
 class AdaptersParams(C.Structure):
@@ -34,6 +36,19 @@ class DistillParams(C.Structure):
                 ("x_dtype", C.c_uint32), ("teacher_dtype", C.c_uint32), ("index_dtype", C.c_uint32)]
 
 
+class ProductParams(C.Structure):
+    """Mirror of ``nvfp4_product_params``."""
+    _fields_ = [("rows", C.c_int64), ("inp", C.c_int64), ("out", C.c_int64), ("experts", C.c_int64), ("slots", C.c_int64),
+                ("ld_x", C.c_int64), ("ld_out", C.c_int64), ("x_dtype", C.c_uint32), ("out_dtype", C.c_uint32), ("flags", C.c_uint32)]
+
+
+class ExpertsParams(C.Structure):
+    """Mirror of ``nvfp4_experts_params``."""
+    _fields_ = [("tokens", C.c_int64), ("top", C.c_int64), ("experts", C.c_int64), ("width", C.c_int64), ("ld_token", C.c_int64),
+                ("ld_base", C.c_int64), ("ld_slot", C.c_int64), ("ld_dslot", C.c_int64), ("token_dtype", C.c_uint32),
+                ("slot_dtype", C.c_uint32), ("index_dtype", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -43,14 +58,21 @@ def lib() -> C.CDLL:
     if _lib is None:
         library = B.lib()
         vp, size = C.c_void_p, C.c_size_t
-        a, d = C.POINTER(AdaptersParams), C.POINTER(DistillParams)
+        a, d, w, e = (C.POINTER(p) for p in (AdaptersParams, DistillParams, ProductParams, ExpertsParams))
         for name, result, arguments in (
                 ("nvfp4_adapters_workspace_bytes", size, [a, C.c_int]),
                 ("nvfp4_adapters_forward", C.c_int, [vp, a] + [vp] * 8 + [size, vp]),
                 ("nvfp4_adapters_backward", C.c_int, [vp, a] + [vp] * 11 + [size, vp]),
                 ("nvfp4_distill_forward", C.c_int, [vp, d] + [vp] * 5),
                 ("nvfp4_distill_backward", C.c_int, [vp, d] + [vp] * 6),
-                ("nvfp4_distill_step", C.c_int, [vp, d] + [vp] * 6)):
+                ("nvfp4_distill_step", C.c_int, [vp, d] + [vp] * 6),
+                ("nvfp4_weight_product", C.c_int, [vp, w] + [vp] * 5),
+                ("nvfp4_experts_product", C.c_int, [vp, w] + [vp] * 7),
+                ("nvfp4_experts_workspace_bytes", size, [e]),
+                ("nvfp4_experts_sort", C.c_int, [vp, e] + [vp] * 4 + [size, vp]),
+                ("nvfp4_experts_spread", C.c_int, [vp, e] + [vp] * 3),
+                ("nvfp4_experts_combine", C.c_int, [vp, e] + [vp] * 5),
+                ("nvfp4_experts_combine_backward", C.c_int, [vp, e] + [vp] * 6)):
             function = getattr(library, name)
             function.restype, function.argtypes = result, arguments
         _lib = library
