@@ -6,6 +6,8 @@
 // exact operands and accumulates in fp32.  fp32 activations are sums of three BF16 terms, a matrix instruction for each.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "finetune/nvfp4_finetune.h"
 #include "launch.hpp"
 
@@ -20,6 +22,15 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int64_t kMostRows = (1 << 24) - 1, kMostWidth = 1 << 22, kMostExperts = 1024, kMostSlots = (int64_t)1 << 30;
+
+// f(0), f(1), ..., f(N - 1) with the number as a constant
+template <int N, typename F>
+__device__ __forceinline__ void each_number(F f) {
+  if constexpr (N > 0) {
+    each_number<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
 
 struct ProductArgs {
   const void *x;
@@ -160,6 +171,311 @@ __global__ void __launch_bounds__(kFewWaves * 64) k_few(ProductArgs a) {
   }
 }
 
+// ---- k_tiles ------------------------------------------------------------------------------------------------------------
+
+// A workgroup's tile of out is BM x BN; SM x SN waves hold WM x WN tiles of the matrix instruction (32 x 32) each, in KS copies that share K: copy kg
+// takes 64 of every chunk of 64 KS.  NST chunks of x, codes and scales are in LDS or on their way there.
+template <typename T_, int WM_, int WN_, int SM_, int SN_, int KS_, int NST_>
+struct Shape {
+  typedef T_ T;
+  static constexpr int WM = WM_, WN = WN_, SM = SM_, SN = SN_, KS = KS_, NST = NST_;
+  static constexpr int kWaves = SM * SN * KS, kThreads = 64 * kWaves, BM = 32 * WM * SM, BN = 32 * WN * SN, CK = 64 * KS;
+  static constexpr int UA = CK * (int)sizeof(T) / 16, UB = CK / 32;       // 16-byte units of a row of x, of codes (= pairs of scales)
+  static constexpr uint32_t kCodes = BM * UA * 16, kScales = kCodes + BN * UB * 16, kStage = kScales + BN * UB * 4;
+  static constexpr int NA = BM * UA / 64 / kWaves, NB = BN * UB / 64 / kWaves, kCopies = NA + 2 * NB;     // copy instructions of a wave
+  static constexpr int kPitch = BN + 4;          // of the sums on their way out, in floats; 32 rows of every wave at a time
+  static constexpr uint32_t kSums = KS * SM * 32 * kPitch * 4;
+  static constexpr uint32_t kLds = NST * kStage > kSums ? NST * kStage : kSums;
+  static_assert(BM * UA % (64 * kWaves) == 0 && BN * UB % (64 * kWaves) == 0 && 64 % UA == 0 && 64 % UB == 0, "whole copies");
+  static_assert(kLds <= 160 * 1024 && (NST - 2) * kCopies < 63, "LDS; vmcnt counts to 63");
+};
+
+// What a lane copies in place of x past the end of K (a weight's scale there is any finite number, so x has to be 0).
+__device__ const u32x4 kZeros = {0, 0, 0, 0};
+
+// M0 = LDS byte address of lane 0's piece.  It needs a wait state before a copy reads it.
+#define NV_COPY16(lds, address) \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(address) : "memory", "m0")
+#define NV_COPY16_AT(lds, offset, base) \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0")
+#define NV_COPY2_AT(lds, offset, base) \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0")
+
+__device__ inline const uint8_t *uniform(const uint8_t *p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const uint8_t *>(((uint64_t)hi << 32) | lo);
+}
+
+// A tile's rows: of expert e, or (e = experts) rows behind the last one's.
+struct Unit {
+  int32_t e, first, last;
+};
+
+// Which tile this workgroup has; last <= first: none.  Workgroups go to the eight dies in turn and each die has its own L2: every die takes an
+// adjacent eighth of the tiles that there are, a row of tiles one after the other.
+template <int BM, int THREADS>
+__device__ inline Unit unit_of(const ProductArgs &a, int32_t tiles_n, int32_t &n) {
+  __shared__ int32_t sums[THREADS / 64];
+  __shared__ Unit found;
+  int32_t units;
+  const auto tile_of = [&](int32_t &unit) {
+    const int64_t all = (int64_t)units * tiles_n;
+    const int32_t share = (int32_t)((all + 7) / 8), seq = (int32_t)(blockIdx.x >> 3);
+    const int64_t tile = (int64_t)(blockIdx.x & 7) * share + seq;
+    if (seq >= share || tile >= all) return false;
+    unit = (int32_t)(tile / tiles_n);
+    n = (int32_t)(tile % tiles_n);
+    return true;
+  };
+  if (!a.begin) {
+    units = (a.slots + BM - 1) / BM;
+    int32_t unit;
+    if (!tile_of(unit)) return {0, 0, 0};
+    return {0, unit * BM, a.slots - unit * BM < BM ? a.slots : (unit + 1) * BM};
+  }
+  // experts one after the other, each thread adjacent ones, the rows behind the last one's as one more
+  const int32_t groups = a.experts + 1, per = (groups + THREADS - 1) / THREADS, g0 = (int32_t)threadIdx.x * per;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const auto rows = [&](int32_t g) -> Rows {
+    if (g < a.experts) return rows_of(a, g);
+    return {rows_of(a, a.experts - 1).last, a.slots};
+  };
+  int32_t mine = 0;
+  for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
+    const Rows r = rows(g);
+    mine += (r.last - r.first + BM - 1) / BM;
+  }
+  int32_t upto = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int32_t other = __shfl_up(upto, d);
+    if (lane >= d) upto += other;
+  }
+  if (lane == 63) sums[wave] = upto;
+  if (threadIdx.x == 0) found = {0, 0, 0};
+  __syncthreads();
+  int32_t before = upto - mine, unit;
+  units = 0;
+  for (int w = 0; w < THREADS / 64; ++w) {
+    if (w < wave) before += sums[w];
+    units += sums[w];
+  }
+  const bool any = tile_of(unit);
+  for (int32_t g = g0; any && g < g0 + per && g < groups; ++g) {
+    const Rows r = rows(g);
+    const int32_t tiles = (r.last - r.first + BM - 1) / BM, t = unit - before;
+    if (t >= 0 && t < tiles) found = {g, r.first + t * BM, r.last - r.first - t * BM < BM ? r.last : r.first + (t + 1) * BM};
+    before += tiles;
+  }
+  __syncthreads();
+  return found;
+}
+
+template <typename S, typename TO>
+__global__ void __launch_bounds__(S::kThreads, 1) k_tiles(ProductArgs a, int32_t tiles_n) {
+  typedef typename S::T T;
+  typedef float f32x16 __attribute__((ext_vector_type(16)));
+  constexpr int WM = S::WM, WN = S::WN, UA = S::UA, UB = S::UB, NA = S::NA, NB = S::NB, kTerms = sizeof(T) == 4 ? 3 : 1;
+  extern __shared__ __align__(16) uint8_t lds[];
+  __shared__ uint8_t is_row[S::BM];              // 0: the token is none of x's rows
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), line = lane & 31, half = lane / 32;
+  const int kg = wave / (S::SM * S::SN), wm = wave / S::SN % S::SM, wn = wave % S::SN;
+  int32_t tile_n;
+  const Unit unit = unit_of<S::BM, S::kThreads>(a, tiles_n, tile_n);
+  if (unit.last <= unit.first) return;
+  const int32_t N = a.out_width, K = a.inp, n0 = tile_n * S::BN, rows_m = unit.last - unit.first;
+  const int32_t rows_n = N - n0 < S::BN ? N - n0 : S::BN;
+  TO *const out = static_cast<TO *>(a.out) + (int64_t)unit.first * a.ld_out + n0;
+  if (unit.e == a.experts) {
+    for (int32_t i = threadIdx.x; i < rows_m * S::BN; i += S::kThreads)
+      if (i % S::BN < rows_n) out[(int64_t)(i / S::BN) * a.ld_out + i % S::BN] = (TO)0.0f;
+    return;
+  }
+  const auto row_of = [&](int32_t m) {           // of x; -1: none
+    const int32_t s = unit.first + (m < rows_m ? m : rows_m - 1), from = a.token ? a.token[s] : s;
+    return from >= 0 && from < a.rows ? from : -1;
+  };
+  for (int32_t m = threadIdx.x; m < S::BM; m += S::kThreads) is_row[m] = row_of(m) >= 0;
+  const float alpha = a.alpha[unit.e];
+
+  // ---- where a lane's copies come from.  Unit u of a row stands at the place u ^ swz(row), so that sixteen lanes that read a unit of sixteen
+  // rows meet all banks.
+  const auto swz_a = [](uint32_t row) { return UA == 8 ? row >> 1 & 7 : row & 15; };
+  const auto swz_b = [](uint32_t row) { return row / (16 / UB) & (UB - 1); };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+  const int32_t row_codes = K / 2, row_scales = K / 16;
+  const uint8_t *from_a[NA];
+  uint32_t unit_a[NA], at_b[NB], at_s[NB];
+#pragma unroll
+  for (int i = 0; i < NA; ++i) {
+    const uint32_t row = ((wave + S::kWaves * i) * 64 + lane) / UA, u = lane % UA ^ swz_a(row);
+    const int32_t r = row_of((int32_t)row);
+    from_a[i] = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.x) + (int64_t)(r < 0 ? 0 : r) * a.ld_x) + u * 16;
+    unit_a[i] = u;
+  }
+  const auto offsets = [&](uint32_t last) __attribute__((always_inline)) {       // units past `last` give that one instead
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const uint32_t row = ((wave + S::kWaves * i) * 64 + lane) / UB, have = (int32_t)row < rows_n ? row : (uint32_t)rows_n - 1;
+      uint32_t u = lane % UB ^ swz_b(row);
+      u = u < last ? u : last;
+      at_b[i] = have * (uint32_t)row_codes + u * 16;
+      at_s[i] = (have >> a.scale_shift) * (uint32_t)row_scales + u * 2;
+    }
+  };
+  const uint8_t *const codes = uniform(a.codes + ((int64_t)unit.e * N + n0) * row_codes);
+  const uint8_t *const scales = uniform(a.scales + ((int64_t)unit.e * (N >> a.scale_shift) + (n0 >> a.scale_shift)) * row_scales);
+  const int32_t chunks = (K + S::CK - 1) / S::CK;
+  const bool ragged = K % S::CK != 0;
+  const auto last_chunk = [&](int32_t c) __attribute__((always_inline)) {        // before the copies of chunk c
+    if (!ragged || c != chunks - 1) return;
+    const uint32_t left = (uint32_t)(K - c * S::CK) / 32;
+    offsets(left - 1);
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      if (unit_a[i] >= left * (32 * sizeof(T) / 16)) from_a[i] = reinterpret_cast<const uint8_t *>(&kZeros) - (int64_t)c * (S::CK * sizeof(T));
+  };
+  const auto copy = [&](int32_t c, uint32_t stage, auto number) __attribute__((always_inline)) {
+    constexpr int i = decltype(number)::value;
+    const uint32_t to = lds0 + stage * S::kStage;
+    if constexpr (i < NA) {
+      const uint8_t *const from = from_a[i] + (int64_t)c * (S::CK * sizeof(T));
+      NV_COPY16(to + (wave + S::kWaves * i) * 1024, from);
+    } else if constexpr (i < NA + NB) {
+      const uint32_t offset = at_b[i - NA];
+      const uint8_t *const base = codes + c * (S::CK / 2);
+      NV_COPY16_AT(to + S::kCodes + (wave + S::kWaves * (i - NA)) * 1024, offset, base);
+    } else {
+      const uint32_t offset = at_s[i - NA - NB];
+      const uint8_t *const base = scales + c * (S::CK / 16);
+      NV_COPY2_AT(to + S::kScales + (wave + S::kWaves * (i - NA - NB)) * 256, offset, base);
+    }
+  };
+  const auto clamp = [&](int32_t c) { return __builtin_amdgcn_readfirstlane(c < chunks ? c : chunks - 1); };
+
+  // ---- what a lane reads of a chunk: 32 codes of a column, k = 32 half + 0 .. 31 of the wave's 64, their two scales, and in step s x of k = 32 half + 8 s
+  u32x4 raw[WN];
+  uint32_t raw_scales[WN];
+  bf16x8 fb[2][WN], fa[2][WM][kTerms];
+  const auto read_b = [&](uint32_t stage, int j) __attribute__((always_inline)) {
+    const uint32_t row = (wn * WN + j) * 32 + line, u = (kg * 2 + half) ^ swz_b(row);
+    const uint8_t *const at = lds + stage * S::kStage;
+    raw[j] = *reinterpret_cast<const u32x4 *>(at + S::kCodes + (row * UB + u) * 16);
+    raw_scales[j] = *reinterpret_cast<const uint32_t *>(at + S::kScales + (row * UB + u) * 4);
+  };
+  const auto expand_b = [&](int s, int j) __attribute__((always_inline)) {
+    const float sc = s < 2 ? __builtin_amdgcn_cvt_f32_fp8((int)raw_scales[j], 0) : __builtin_amdgcn_cvt_f32_fp8((int)raw_scales[j], 1);
+    fb[s & 1][j] = expand8(raw[j][s], sc);
+  };
+  const auto read_a = [&](uint32_t stage, int s, int i) __attribute__((always_inline)) {
+    const uint32_t row = (wm * WM + i) * 32 + line;
+    const uint8_t *const at = lds + stage * S::kStage + row * (UA * 16);
+    if constexpr (kTerms == 1) {
+      fa[s & 1][i][0] = *reinterpret_cast<const bf16x8 *>(at + ((kg * 8 + half * 4 + s) ^ swz_a(row)) * 16);
+    } else {
+      const uint32_t u = kg * 16 + half * 8 + s * 2;
+      const f32x4 v[2] = {*reinterpret_cast<const f32x4 *>(at + (u ^ swz_a(row)) * 16),
+                          *reinterpret_cast<const f32x4 *>(at + ((u + 1) ^ swz_a(row)) * 16)};
+      u32x4 w[3];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float lo[3], hi[3];
+        terms_of(v[k / 2][k % 2 * 2], lo);
+        terms_of(v[k / 2][k % 2 * 2 + 1], hi);
+        for (int c = 0; c < 3; ++c) w[c][k] = pack_exact(lo[c], hi[c]);
+      }
+      for (int c = 0; c < 3; ++c) fa[s & 1][i][c] = __builtin_bit_cast(bf16x8, w[c]);
+    }
+  };
+
+  f32x16 acc[WM][WN] = {};
+  offsets(UB - 1);
+#pragma unroll 1
+  for (int32_t c = 0; c < S::NST - 1; ++c) {
+    last_chunk(clamp(c));
+    each_number<S::kCopies>([&](auto i) __attribute__((always_inline)) { copy(clamp(c), c, i); });
+  }
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((S::NST - 2) * S::kCopies) : "memory");
+#pragma unroll
+  for (int j = 0; j < WN; ++j) read_b(0, j);
+#pragma unroll
+  for (int i = 0; i < WM; ++i) read_a(0, 0, i);
+#pragma unroll
+  for (int j = 0; j < WN; ++j) expand_b(0, j);
+  // Chunk c stands in stage c % NST.  In its first three steps of four the copies of chunk c + NST - 1 start, into the stage of chunk c - 1, which every
+  // wave had read when it came to the barrier of chunk c - 1.  In the last step all waves meet, with chunk c + 1 there, and begin to read it.
+  uint32_t stage = 0, freed = S::NST - 1;
+#pragma unroll 1
+  for (int32_t c = 0; c < chunks; ++c) {
+    const uint32_t next = stage + 1 == (uint32_t)S::NST ? 0u : stage + 1;
+    const int32_t ahead = clamp(c + S::NST - 1);
+    if (c + S::NST - 1 == chunks - 1) last_chunk(ahead);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s == 3) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S::NST - 2) * S::kCopies) : "memory");
+#pragma unroll
+        for (int j = 0; j < WN; ++j) read_b(next, j);
+      } else {
+        each_number<S::kCopies>([&](auto i) __attribute__((always_inline)) {
+          if (decltype(i)::value * 3 / S::kCopies == s) copy(ahead, freed, i);
+        });
+      }
+#pragma unroll
+      for (int i = 0; i < WM; ++i) read_a(s == 3 ? next : stage, (s + 1) & 3, i);
+#pragma unroll
+      for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int j = 0; j < WN; ++j)
+#pragma unroll
+          for (int t = kTerms - 1; t >= 0; --t)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][j], fa[s & 1][i][t], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < WN; ++j) expand_b((s + 1) & 3, j);
+    }
+    freed = stage;
+    stage = next;
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+  // ---- sums -> LDS -> out, 32 rows of every wave at a time: the operands were exchanged in the matrix instruction, so that four
+  // accumulators are adjacent columns
+  constexpr int G = sizeof(TO) == 4 ? 4 : 8, kRows = 32 * S::SM, kPieces = kRows * S::BN / G;
+  float *const sums = reinterpret_cast<float *>(lds);
+#pragma unroll
+  for (int i = 0; i < WM; ++i) {
+    if (i) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < WN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4)
+        *reinterpret_cast<f32x4 *>(sums + (kg * kRows + wm * 32 + line) * S::kPitch + (wn * WN + j) * 32 + 2 * v + 4 * half) =
+            f32x4{acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]};
+    __syncthreads();
+#pragma unroll 2
+    for (int piece = (int)threadIdx.x; piece < kPieces; piece += S::kThreads) {
+      const int in = piece / (S::BN / G), col = piece % (S::BN / G) * G;
+      const int32_t m = in / 32 * (32 * WM) + i * 32 + in % 32;
+      f32x4 v[G / 4] = {};
+      for (int k = 0; k < S::KS; ++k)
+        for (int g = 0; g < G / 4; ++g) v[g] += *reinterpret_cast<const f32x4 *>(sums + (k * kRows + in) * S::kPitch + col + 4 * g);
+      const bool is = is_row[m];
+      for (int g = 0; g < G / 4; ++g) v[g] = is ? v[g] * alpha : f32x4{};
+      if (m >= rows_m || col >= rows_n) continue;
+      TO *const to = out + (int64_t)m * a.ld_out + col;
+      // (lines of out begin wherever its stride puts them)
+      typedef TO piece_of __attribute__((ext_vector_type(G)));
+      typedef piece_of piece_anywhere __attribute__((aligned(sizeof(TO))));
+      piece_of p;
+      for (int g = 0; g < G; ++g) p[g] = (TO)v[g / 4][g % 4];
+      if (col + G <= rows_n) *reinterpret_cast<piece_anywhere *>(to) = p;
+      else
+        for (int g = 0; g < G; ++g)
+          if (col + g < rows_n) to[g] = p[g];
+    }
+  }
+}
+
 // ---- host -----------------------------------------------------------------------------------------------------------------
 
 int64_t divide_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -173,10 +489,32 @@ bool sizes_fit(const nvfp4_product_params &p) {
          (!(p.flags & NVFP4_GEMM_B_TILE_SCALES) || p.out % 16 == 0);
 }
 
+template <typename S, typename TO>
+int run_tiles(const ProductArgs &a, hipStream_t s) {
+  const int64_t tiles_n = divide_up(a.out_width, S::BN);
+  const int64_t groups = a.begin ? (a.experts + 1 < a.slots ? a.experts + 1 : a.slots) : 0;
+  const int64_t units = a.begin ? a.slots / S::BM + groups : divide_up(a.slots, S::BM);       // at most
+  // (the limit belongs to the kernel and not to the call, so it is always the same)
+  if (S::kLds > 48 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k_tiles<S, TO>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)S::kLds) != hipSuccess)
+    return NVFP4_ERR_HIP;
+  const int64_t grid = divide_up(units * tiles_n, 8) * 8;
+  if (grid > 0x7fffffff) return NVFP4_ERR_UNSUPPORTED;
+  return launch(k_tiles<S, TO>, dim3((uint32_t)grid), dim3(S::kThreads), S::kLds, s, a, (int32_t)tiles_n);
+}
+template <typename T, typename TO, int MT>
+int run_few(const ProductArgs &a, hipStream_t s) {
+  const dim3 grid((uint32_t)divide_up(a.out_width, 16), (uint32_t)(a.experts + (a.begin ? 1 : 0)));
+  return launch(k_few<T, TO, MT>, grid, dim3(kFewWaves * 64), 0, s, a);
+}
+
 template <typename T, typename TO>
 int run_product(const ProductArgs &a, hipStream_t s) {
-  const dim3 grid((uint32_t)divide_up(a.out_width, 16), (uint32_t)(a.experts + (a.begin ? 1 : 0)));
-  return launch(k_few<T, TO, 1>, grid, dim3(kFewWaves * 64), 0, s, a);
+  const int64_t each = a.slots / a.experts;
+  if (a.rows == 0 || each <= 16) return run_few<T, TO, 1>(a, s);
+  if (each <= 256) return run_tiles<Shape<T, 2, 1, 1, 1, 4, sizeof(T) == 4 ? 2 : 3>, TO>(a, s);
+  if constexpr (sizeof(T) == 4) return run_tiles<Shape<T, 2, 2, 2, 2, 1, 3>, TO>(a, s);
+  else return run_tiles<Shape<T, 4, 4, 2, 2, 1, 3>, TO>(a, s);
 }
 
 int product(const void *x, const nvfp4_product_params *p, const int32_t *token, const int32_t *begin, const void *codes,
