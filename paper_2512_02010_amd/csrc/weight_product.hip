@@ -6,6 +6,7 @@
 // exact operands and accumulates in fp32.  fp32 activations are sums of three BF16 terms, a matrix instruction for each.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include "finetune/nvfp4_finetune.h"
@@ -68,6 +69,12 @@ __device__ inline bf16x8 expand8(uint32_t word, float scale) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// Byte `i` of four scales.
+__device__ inline float scale_of(uint32_t bytes, int i) {
+  return i == 0 ? __builtin_amdgcn_cvt_f32_fp8((int)bytes, 0) : i == 1 ? __builtin_amdgcn_cvt_f32_fp8((int)bytes, 1)
+       : i == 2 ? __builtin_amdgcn_cvt_f32_fp8((int)bytes, 2) : __builtin_amdgcn_cvt_f32_fp8((int)bytes, 3);
+}
+
 // The expert's rows of out, whatever begin holds.
 struct Rows {
   int32_t first, last;
@@ -80,94 +87,217 @@ __device__ inline Rows rows_of(const ProductArgs &a, int32_t e) {
   return {first, last};
 }
 
+// What a lane copies in place of x past the end of K (a weight's scale there is any finite number, so x has to be 0).
+__device__ const u32x4 kZeros = {0, 0, 0, 0};
+
+// M0 = LDS byte address of lane 0's piece.  It needs a wait state before a copy reads it.
+#define NV_COPY16(lds, address) \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(address) : "memory", "m0")
+#define NV_COPY16_AT(lds, offset, base) \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0")
+#define NV_COPY2_AT(lds, offset, base) \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0")
+
+__device__ inline const uint8_t *uniform(const uint8_t *p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const uint8_t *>(((uint64_t)hi << 32) | lo);
+}
+
 // ---- k_few --------------------------------------------------------------------------------------------------------------
 
-constexpr int kFewWaves = 8;
+// Few rows: bound by the codes, which pass through a compute unit once.  A workgroup has 32 columns of out and an expert's rows, XR of them at a time; its W
+// waves share K, every W-th chunk of 256 each, and their sums meet in LDS.  A wave copies its chunks into a ring of NST stages of its own, eight
+// neighbouring lanes a column's 128 bytes of codes, 16 bytes of scales a lane (WHOLE: K is a multiple of 256; else two bytes at a time), two rows (one
+// of fp32) of x at a time, as many as there are.
+template <typename T_, int XR_, int W_, int NST_, bool WHOLE_>
+struct FewShape {
+  typedef T_ T;
+  static constexpr int XR = XR_, W = W_, NST = NST_;
+  static constexpr bool WHOLE = WHOLE_;
+  static constexpr int UX = 256 * (int)sizeof(T) / 16, RX = 64 / UX, NX = XR / RX;         // units of a row of x; rows of a copy; copies
+  static constexpr int NS = WHOLE ? 1 : 4, kOthers = 4 + NS;
+  static constexpr uint32_t kScales = 32 * 128, kX = kScales + (WHOLE ? 512 : 1024), kStage = kX + XR * UX * 16;
+  static constexpr uint32_t kLds = W * NST * kStage;
+  static_assert(XR <= 16 && XR % RX == 0 && kLds >= W * 2048 && kLds <= 160 * 1024 && (NST - 1) * (kOthers + NX) < 63, "");
+};
 
-// A workgroup has 16 columns of out and an expert's rows, 16 MT of them at a time; its waves share K, 128 at a time, and their sums meet in LDS.
-// Lane l loads 16 bytes, 32 codes, of column l % 16 and x of row l % 16, in pieces of 64 adjacent bytes to four lanes.
-template <typename T, typename TO, int MT>
-__global__ void __launch_bounds__(kFewWaves * 64) k_few(ProductArgs a) {
-  constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;
-  __shared__ float part[kFewWaves][MT][4][64];
+template <typename S, typename TO>
+__global__ void __launch_bounds__(S::W * 64) k_few(ProductArgs a) {
+  typedef typename S::T T;
+  constexpr int kTerms = sizeof(T) == 4 ? 3 : 1, XR = S::XR, W = S::W, NST = S::NST, UX = S::UX, RX = S::RX, NX = S::NX;
+  extern __shared__ __align__(16) uint8_t lds[];
+  __shared__ uint8_t is_row[16];                 // 0: the token is none of x's rows
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), line = lane & 15, group = lane / 16;
-  const int32_t e = (int32_t)blockIdx.y, n0 = (int32_t)blockIdx.x * 16, N = a.out_width, K = a.inp;
-  TO *const out = static_cast<TO *>(a.out);
-  if (e == a.experts) {                          // behind the last expert's rows
-    for (int32_t s = rows_of(a, e - 1).last + (int32_t)threadIdx.x / 16; s < a.slots; s += kFewWaves * 4)
-      if (n0 + (int32_t)threadIdx.x % 16 < N) out[(int64_t)s * a.ld_out + n0 + threadIdx.x % 16] = (TO)0.0f;
+  const int32_t e = (int32_t)blockIdx.y, n0 = (int32_t)blockIdx.x * 32, N = a.out_width, K = a.inp;
+  TO *const out = static_cast<TO *>(a.out) + n0;
+  const int32_t rows_n = N - n0 < 32 ? N - n0 : 32;
+  const bool behind = e == a.experts;            // the rows behind the last expert's
+  const Rows r = behind ? Rows{rows_of(a, e - 1).last, a.slots} : rows_of(a, e);
+  if (r.first >= r.last) return;
+  if (behind || a.rows == 0) {
+    for (int32_t s = r.first + (int32_t)threadIdx.x / 32; s < r.last; s += W * 2)
+      if ((int32_t)threadIdx.x % 32 < rows_n) out[(int64_t)s * a.ld_out + threadIdx.x % 32] = (TO)0.0f;
     return;
   }
-  const Rows r = rows_of(a, e);
-  if (r.first >= r.last) return;
-  const int32_t n = n0 + line < N ? n0 + line : N - 1;
-  const uint8_t *const codes = a.codes + ((int64_t)e * N + n) * (K / 2);
-  const uint8_t *const scales = a.scales + ((int64_t)e * (N >> a.scale_shift) + (n >> a.scale_shift)) * (K / 16);
+  const int32_t row_codes = K / 2, row_scales = K / 16, chunks = (K + 255) / 256;
+  const uint8_t *const codes = uniform(a.codes + ((int64_t)e * N + n0) * row_codes);
+  const uint8_t *const scales = uniform(a.scales + ((int64_t)e * (N >> a.scale_shift) + (n0 >> a.scale_shift)) * row_scales);
   const float alpha = a.alpha[e];
-  for (int32_t m0 = r.first; m0 < r.last; m0 += 16 * MT) {
-    const T *row[MT];
-    bool is[MT];
+  const uint8_t *const own = lds + wave * (NST * S::kStage);
+  const uint32_t own_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * (NST * S::kStage);
+  for (int32_t m0 = r.first; m0 < r.last; m0 += XR) {
+    const int32_t rows_m = r.last - m0 < XR ? r.last - m0 : XR, nx = (rows_m + RX - 1) / RX;
+    // ---- where a lane's copies come from.  Unit u of a column stands at the place u ^ (column / 2 % 8), unit u of a row of x at u ^ (row % 16), so that
+    // sixteen lanes that read a unit of sixteen lines meet all banks.
+    uint32_t at_c[4], at_s[S::NS];
+    const uint8_t *from_x[NX];
+    const auto offsets = [&](uint32_t last) __attribute__((always_inline)) {     // units past `last` give that one instead
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int32_t s = m0 + m * 16 + line;
-      int32_t from = s < r.last ? s : r.last - 1;
-      if (a.token) from = a.token[from];
-      is[m] = from >= 0 && from < a.rows;
-      row[m] = static_cast<const T *>(a.x) + (int64_t)(is[m] ? from : 0) * a.ld_x;
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t n = i * 8 + lane / 8, have = (int32_t)n < rows_n ? n : (uint32_t)rows_n - 1, u = lane % 8 ^ (n >> 1 & 7);
+        at_c[i] = have * (uint32_t)row_codes + (u < last ? u : last) * 16;
+        if constexpr (!S::WHOLE) at_s[i] = (have >> a.scale_shift) * (uint32_t)row_scales + ((uint32_t)lane % 8 < last ? lane % 8 : last) * 2;
+      }
+      if constexpr (S::WHOLE) at_s[0] = (uint32_t)((lane & 31) < rows_n ? lane & 31 : rows_n - 1) >> a.scale_shift, at_s[0] *= (uint32_t)row_scales;
+    };
+    offsets(7);
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      const int32_t m = i * RX + lane / UX, s = m0 + (m < rows_m ? m : rows_m - 1), from = a.token ? a.token[s] : s;
+      const bool is = from >= 0 && from < a.rows;
+      from_x[i] = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.x) + (is ? from : 0) * a.ld_x) + (lane % UX ^ (m & 15)) * 16;
+      if (wave == 0 && lane % UX == 0) is_row[m] = is;
     }
-    f32x4 acc[MT] = {};
-    for (int32_t k0 = wave * 128; k0 < K; k0 += kFewWaves * 128) {
-      // of 32 codes, and of each of 4 x 8 numbers of x, there are all or none (K is a multiple of 32)
-      u32x4 w{};
-      if (k0 + group * 32 < K) w = *reinterpret_cast<const u32x4 *>(codes + (k0 + group * 32) / 2);
-      float sc[4];
-      bf16x8 x[MT][4][kTerms];
+    const auto copy_chunk = [&](int32_t c, uint32_t stage) __attribute__((always_inline)) {
+      const uint32_t to = own_at + stage * S::kStage;
+      if (!S::WHOLE && c == chunks - 1) {
+        const uint32_t left = (uint32_t)(K - c * 256) / 32;
+        offsets(left - 1);
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bool there = k0 + s * 32 < K;
-        sc[s] = there ? __builtin_amdgcn_cvt_f32_fp8((int)scales[(k0 + s * 32) / 16 + group / 2], 0) : 0.0f;
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const T *const from = row[m] + k0 + s * 32 + group * 8;
-          if constexpr (kTerms == 1) {
-            x[m][s][0] = there && is[m] ? *reinterpret_cast<const bf16x8 *>(from) : bf16x8{};
-          } else {
-            const f32x8 v = there && is[m] ? *reinterpret_cast<const f32x8 *>(from) : f32x8{};
-            for (int i = 0; i < 8; ++i) {
-              float t[3];
-              terms_of(v[i], t);
-              for (int c = 0; c < 3; ++c) x[m][s][c][i] = (__bf16)t[c];
-            }
-          }
+        for (int i = 0; i < NX; ++i) {
+          const uint32_t u = lane % UX ^ ((i * RX + lane / UX) & 15);
+          if (u >= left * (32 * sizeof(T) / 16)) from_x[i] = reinterpret_cast<const uint8_t *>(&kZeros) - (int64_t)c * (256 * sizeof(T));
         }
       }
-      // what lane group g holds of step s, and the other way round: then step s is the codes k0 + 32 s + 8 g
-      const u32x2 a02 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false));
-      const u32x2 a13 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false));
-      const u32x2 b01 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a02[0], a13[0], false, false));
-      const u32x2 b23 = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a02[1], a13[1], false, false));
-      const uint32_t words[4] = {b01[0], b01[1], b23[0], b23[1]};
+      const uint8_t *const c_at = codes + c * 128, *const s_at = scales + c * 16;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bf16x8 b = expand8(words[s], sc[s]);
+      for (int i = 0; i < 4; ++i) NV_COPY16_AT(to + i * 1024, at_c[i], c_at);
+      if constexpr (S::WHOLE) {
+        if (lane < 32) NV_COPY16_AT(to + S::kScales, at_s[0], s_at);
+      } else {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int c = kTerms - 1; c >= 0; --c) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[m][s][c], b, acc[m], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) NV_COPY2_AT(to + S::kScales + i * 256, at_s[i], s_at);
       }
-    }
-    __syncthreads();                             // (the sums of the rows before have been read)
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-      for (int v = 0; v < 4; ++v) part[wave][m][v][lane] = acc[m][v];
-    __syncthreads();
-    for (int i = threadIdx.x; i < MT * 256; i += kFewWaves * 64) {
-      const int m = i / 256, in = i % 256, l = in / 64 * 16 + in % 16, v = in / 16 % 4;       // row 4 (in / 64) + v of the tile, column in % 16
-      float sum = 0.0f;
-      for (int w = 0; w < kFewWaves; ++w) sum += part[w][m][v][l];
-      const int32_t s = m0 + m * 16 + in / 16;
-      if (s < r.last && n0 + in % 16 < N) out[(int64_t)s * a.ld_out + n0 + in % 16] = (TO)(sum * alpha);
+      for (int i = 0; i < NX; ++i)
+        if (i < nx) {
+          const uint8_t *const from = from_x[i] + (int64_t)c * (256 * sizeof(T));
+          NV_COPY16(to + S::kX + i * 1024, from);
+        }
+    };
+    // until but the copies of `young` stages have landed
+    const auto wait = [&](auto young) __attribute__((always_inline)) {
+      constexpr int n = decltype(young)::value;
+      if constexpr (n == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      else
+        each_number<NX>([&](auto i) __attribute__((always_inline)) {
+          if (nx == decltype(i)::value + 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n * (S::kOthers + decltype(i)::value + 1)) : "memory");
+        });
+    };
+    f32x4 acc[2] = {};
+    // lane group g has the codes 64 g .. 64 g + 63 of a column's chunk, step s of eight of them
+    const auto multiply = [&](uint32_t stage, auto after) __attribute__((always_inline)) {
+      const uint8_t *const st = own + stage * S::kStage;
+      u32x4 raw[2][2];
+      uint32_t sc[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t n = j * 16 + line;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) raw[j][q] = *reinterpret_cast<const u32x4 *>(st + n * 128 + ((2 * group + q) ^ (n >> 1 & 7)) * 16);
+        if constexpr (S::WHOLE) {
+          sc[j] = *reinterpret_cast<const uint32_t *>(st + S::kScales + n * 16 + 4 * group);
+        } else {
+          const u32x2 s = *reinterpret_cast<const u32x2 *>(st + S::kScales + n * 32 + 8 * group);
+          sc[j] = __builtin_amdgcn_perm(s[1], s[0], 0x05040100u);
+        }
+      }
+      T x[8][8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const uint8_t *const row = st + S::kX + (line % XR) * (UX * 16);
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+          const uint32_t u = (group * 8 + s) * (sizeof(T) / 2) + h;
+          *reinterpret_cast<u32x4 *>(&x[s][h * (16 / sizeof(T))]) = *reinterpret_cast<const u32x4 *>(row + (u ^ (line % XR)) * 16);
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      after();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        bf16x8 xs[kTerms];
+        if constexpr (kTerms == 1) {
+          xs[0] = *reinterpret_cast<bf16x8 *>(&x[s][0]);
+        } else {
+          u32x4 w[3];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float lo[3], hi[3];
+            terms_of(x[s][2 * k], lo);
+            terms_of(x[s][2 * k + 1], hi);
+            for (int c = 0; c < 3; ++c) w[c][k] = pack_exact(lo[c], hi[c]);
+          }
+          for (int c = 0; c < 3; ++c) xs[c] = __builtin_bit_cast(bf16x8, w[c]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const bf16x8 b = expand8(raw[j][s / 4][s % 4], scale_of(sc[j], s / 2));
+#pragma unroll
+          for (int c = kTerms - 1; c >= 0; --c) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs[c], b, acc[j], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int32_t c = wave;
+    uint32_t stage = 0;
+#pragma unroll
+    for (int p = 0; p < NST; ++p)
+      if (c + W * p < chunks) copy_chunk(c + W * p, p);
+    const auto step = [&](auto after) __attribute__((always_inline)) {
+      multiply(stage, after);
+      c += W;
+      stage = stage + 1 == (uint32_t)NST ? 0u : stage + 1;
+    };
+    while (c + W * NST < chunks) {
+      wait(std::integral_constant<int, NST - 1>{});
+      step([&] { copy_chunk(c + W * NST, stage); });
     }
+    // the last NST, with nothing left to copy
+    each_number<NST>([&](auto p) __attribute__((always_inline)) {
+      constexpr int young = NST - 1 - decltype(p)::value;
+      if (c + W * young < chunks && c < chunks) {
+        wait(std::integral_constant<int, young>{});
+        step([] {});
+      }
+    });
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                             // (no wave's stages are read any more)
+    float(*const part)[2][4][64] = reinterpret_cast<float(*)[2][4][64]>(lds);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      for (int v = 0; v < 4; ++v) part[wave][j][v][lane] = acc[j][v];
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows_m * 32; i += W * 64) {
+      const int n = i % 32, m = i / 32, l = m / 4 * 16 + n % 16;
+      float sum = 0.0f;
+      for (int w = 0; w < W; ++w) sum += part[w][n / 16][m % 4][l];
+      if (n < rows_n) out[(int64_t)(m0 + m) * a.ld_out + n] = (TO)(is_row[m] ? sum * alpha : 0.0f);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the counts above are of copies alone)
+    __syncthreads();                             // before the next rows are copied there
   }
 }
 
@@ -189,23 +319,6 @@ struct Shape {
   static_assert(BM * UA % (64 * kWaves) == 0 && BN * UB % (64 * kWaves) == 0 && 64 % UA == 0 && 64 % UB == 0, "whole copies");
   static_assert(kLds <= 160 * 1024 && (NST - 2) * kCopies < 63, "LDS; vmcnt counts to 63");
 };
-
-// What a lane copies in place of x past the end of K (a weight's scale there is any finite number, so x has to be 0).
-__device__ const u32x4 kZeros = {0, 0, 0, 0};
-
-// M0 = LDS byte address of lane 0's piece.  It needs a wait state before a copy reads it.
-#define NV_COPY16(lds, address) \
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(address) : "memory", "m0")
-#define NV_COPY16_AT(lds, offset, base) \
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0")
-#define NV_COPY2_AT(lds, offset, base) \
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0")
-
-__device__ inline const uint8_t *uniform(const uint8_t *p) {
-  const uint64_t v = reinterpret_cast<uint64_t>(p);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return reinterpret_cast<const uint8_t *>(((uint64_t)hi << 32) | lo);
-}
 
 // A tile's rows: of expert e, or (e = experts) rows behind the last one's.
 struct Unit {
@@ -364,8 +477,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_tiles(ProductArgs a, int32_t
     raw_scales[j] = *reinterpret_cast<const uint32_t *>(at + S::kScales + (row * UB + u) * 4);
   };
   const auto expand_b = [&](int s, int j) __attribute__((always_inline)) {
-    const float sc = s < 2 ? __builtin_amdgcn_cvt_f32_fp8((int)raw_scales[j], 0) : __builtin_amdgcn_cvt_f32_fp8((int)raw_scales[j], 1);
-    fb[s & 1][j] = expand8(raw[j][s], sc);
+    fb[s & 1][j] = expand8(raw[j][s], scale_of(raw_scales[j], s / 2));
   };
   const auto read_a = [&](uint32_t stage, int s, int i) __attribute__((always_inline)) {
     const uint32_t row = (wm * WM + i) * 32 + line;
@@ -412,26 +524,69 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_tiles(ProductArgs a, int32_t
     if (c + S::NST - 1 == chunks - 1) last_chunk(ahead);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      if (s == 3) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S::NST - 2) * S::kCopies) : "memory");
+      if (s == 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S::NST - 2) * S::kCopies) : "memory");
+      const auto multiply = [&](int i, int j) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < WN; ++j) read_b(next, j);
+        for (int t = kTerms - 1; t >= 0; --t)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][j], fa[s & 1][i][t], acc[i][j], 0, 0, 0);
+      };
+      if constexpr (kTerms == 1 && WM * WN >= 8) {
+        // A part of the step for every column tile, its instructions told apart: the expansion of the next step's fragment between the matrix
+        // instructions of this one.
+#pragma unroll
+        for (int j = 0; j < WN; ++j) {
+          if (s < 3)
+            each_number<S::kCopies>([&](auto i) __attribute__((always_inline)) {
+              if (decltype(i)::value * (3 * WN) / S::kCopies == s * WN + j) copy(ahead, freed, i);
+            });
+          __builtin_amdgcn_sched_barrier(0);
+          int reads = 0;
+          if (s == 3 && j == 0) {
+#pragma unroll
+            for (int b = 0; b < WN; ++b) read_b(next, b);
+            ++reads;
+          }
+          // (all of the rows' pieces with the first column: the next step begins with them)
+#pragma unroll
+          for (int i = j * 2; i < WM && i < j * 2 + 2; ++i) {
+            read_a(s == 3 ? next : stage, (s + 1) & 3, i);
+            ++reads;
+          }
+          // in the last step a column later, when its codes have come
+          if (s < 3) expand_b((s + 1) & 3, j);
+          else if (j > 0) expand_b(0, j - 1);
+          if (s == 3 && j == WN - 1) expand_b(0, j);
+#pragma unroll
+          for (int i = 0; i < WM; ++i) multiply(i, j);
+          if (reads) __builtin_amdgcn_sched_group_barrier(0x100, 16, 0);
+          constexpr int kEach = (20 + WM - 1) / WM;
+          const int each = s == 3 && j == WN - 1 ? 2 * kEach : kEach;
+#pragma unroll
+          for (int i = 0; i < WM; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (each == kEach) __builtin_amdgcn_sched_group_barrier(0x002, kEach, 0);
+            else __builtin_amdgcn_sched_group_barrier(0x002, 2 * kEach, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       } else {
-        each_number<S::kCopies>([&](auto i) __attribute__((always_inline)) {
-          if (decltype(i)::value * 3 / S::kCopies == s) copy(ahead, freed, i);
-        });
+        if (s == 3) {
+#pragma unroll
+          for (int j = 0; j < WN; ++j) read_b(next, j);
+        } else {
+          each_number<S::kCopies>([&](auto i) __attribute__((always_inline)) {
+            if (decltype(i)::value * 3 / S::kCopies == s) copy(ahead, freed, i);
+          });
+        }
+#pragma unroll
+        for (int i = 0; i < WM; ++i) read_a(s == 3 ? next : stage, (s + 1) & 3, i);
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+          for (int j = 0; j < WN; ++j) multiply(i, j);
+#pragma unroll
+        for (int j = 0; j < WN; ++j) expand_b((s + 1) & 3, j);
       }
-#pragma unroll
-      for (int i = 0; i < WM; ++i) read_a(s == 3 ? next : stage, (s + 1) & 3, i);
-#pragma unroll
-      for (int i = 0; i < WM; ++i)
-#pragma unroll
-        for (int j = 0; j < WN; ++j)
-#pragma unroll
-          for (int t = kTerms - 1; t >= 0; --t)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][j], fa[s & 1][i][t], acc[i][j], 0, 0, 0);
-#pragma unroll
-      for (int j = 0; j < WN; ++j) expand_b((s + 1) & 3, j);
     }
     freed = stage;
     stage = next;
@@ -489,32 +644,125 @@ bool sizes_fit(const nvfp4_product_params &p) {
          (!(p.flags & NVFP4_GEMM_B_TILE_SCALES) || p.out % 16 == 0);
 }
 
+// ---- which kernel -----------------------------------------------------------------------------------------------------------
+//
+// Few rows for each expert: k_few, whose passes over an expert's weight stand one after the other, so that the rows of a pass decide.  (us, BF16, rows of
+// a pass 4 / 8 / 16: 1 x 4096 x 4096 5.4 / 6.1 / 5.9, 4 x 15376 x 3584 9.3 / 10.3 / 11.8, 8 x 28672 x 4096 28 / 18.3 / 24, 16 x 8192 x 8192 30 / 19.6 / 13.7; 32
+// tokens of 4 among 64 experts, 1024 x 2048, 17.9 / 16.7 / 25.7.  Against the best tiles: 16 x 8192 x 8192 13.7 / 14, 28 x 480 x 512 5.4 / 4.8, 96 rows of 8
+// experts, 1024 x 2560, 7.3 / 11.2; but 200 of 32, 3216 x 256, 20 / 17.7 and 1024 of 64, 1024 x 2048, 54 / 34.5.)
+// Else k_tiles in the shape that takes least by the estimate below: turns of tiles over the compute units, each a + f microseconds for 1024 of K and besides.
+// The constants are fitted to 150 products, 1 to 4096 tokens, K 256 to 8192, up to 16384 columns, 1 to 128 experts (uneven), each in all shapes: the
+// choice is 2.7 % (fp32: 1.7 %) slower than the best of each, 30 % at most.
+
+enum Kernel { kFew4, kFew8, kFew16, kTile32, kTile64x32, kTile64, kTile64x128, kTile64x256, kTile128, kTile128x256, kTile128x256Pair, kTile256 };
+
+struct Cost {
+  Kernel kernel;
+  int32_t rows, columns;
+  double a, f;                 // us a turn: for 1024 of K, and besides
+};
+constexpr Cost kCostBf16[] = {{kTile32, 32, 32, 0.90, 3.9},      {kTile64x32, 64, 32, 1.88, 3.7},     {kTile64, 64, 64, 3.09, 3.9},
+                              {kTile64x128, 64, 128, 5.98, 3.9}, {kTile128, 128, 128, 7.71, 5.3},     {kTile128x256, 128, 256, 15.04, 6.8},
+                              {kTile128x256Pair, 128, 256, 18.21, 8.7}, {kTile256, 256, 256, 20.43, 13.5}};
+constexpr Cost kCostF32[] = {{kTile32, 32, 32, 3.54, 3.0},
+                             {kTile64, 64, 64, 9.68, 5.0},
+                             {kTile64x128, 64, 128, 17.72, 6.1},
+                             {kTile64x256, 64, 256, 34.47, 5.7},
+                             {kTile128x256, 128, 256, 42.74, 11.3}};
+
+double turns_of(double tiles) {
+  const double t = tiles / 256;
+  return t <= 1 ? 1 : t + (std::ceil(t) - t) / 2;
+}
+// Tiles down the rows: half a tile of every expert's is empty on average, and each that has rows has one.
+double tiles_down(const ProductArgs &a, int32_t rows) {
+  if (a.experts == 1) return (double)divide_up(a.slots, rows);
+  const double used = a.experts < a.slots ? a.experts : a.slots, more = (double)a.slots / rows - used / 2;
+  return used + (more > 0 ? more : 0);
+}
+template <int N>
+Kernel least(const ProductArgs &a, const Cost (&costs)[N]) {
+  Kernel best = costs[0].kernel;
+  double least = 1e300;
+  for (const Cost &c : costs) {
+    const double us = turns_of(tiles_down(a, c.rows) * (double)divide_up(a.out_width, c.columns)) * (c.a * a.inp / 1024 + c.f);
+    if (us < least) least = us, best = c.kernel;
+  }
+  return best;
+}
+// (of fp32 rows half as many stand in a stage)
+Kernel choose(const ProductArgs &a, bool f32) {
+  if (a.rows == 0) return kFew4;                 // (out is 0)
+  const int64_t used = a.experts < a.slots ? a.experts : a.slots, wide = a.experts * divide_up(a.out_width, 32);
+  if (a.experts == 1) {
+    if (a.slots <= (f32 ? 2 : 4)) return kFew4;
+    if (!f32 && a.slots <= 8) return kFew8;
+    if (a.slots <= (f32 ? 12 : 16)) return kFew16;
+  } else {
+    if (a.slots <= (f32 ? used * 5 / 2 : used * 4)) return kFew8;
+    if (a.slots <= (f32 ? used * 8 : used * 16) && wide <= 512) return kFew16;
+  }
+  return f32 ? least(a, kCostF32) : least(a, kCostBf16);
+}
+
+template <typename S, typename TO>
+int run_few_of(const ProductArgs &a, hipStream_t s) {
+  const dim3 grid((uint32_t)divide_up(a.out_width, 32), (uint32_t)(a.experts + (a.begin ? 1 : 0)));
+  // (the limit belongs to the kernel and not to the call, so it is always the same)
+  if (S::kLds > 48 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k_few<S, TO>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)S::kLds) != hipSuccess)
+    return NVFP4_ERR_HIP;
+  return launch(k_few<S, TO>, grid, dim3(S::W * 64), S::kLds, s, a);
+}
+template <typename T, typename TO, int XR, int W, int NST>
+int run_few(const ProductArgs &a, hipStream_t s) {
+  return a.inp % 256 ? run_few_of<FewShape<T, XR, W, NST, false>, TO>(a, s) : run_few_of<FewShape<T, XR, W, NST, true>, TO>(a, s);
+}
 template <typename S, typename TO>
 int run_tiles(const ProductArgs &a, hipStream_t s) {
   const int64_t tiles_n = divide_up(a.out_width, S::BN);
   const int64_t groups = a.begin ? (a.experts + 1 < a.slots ? a.experts + 1 : a.slots) : 0;
   const int64_t units = a.begin ? a.slots / S::BM + groups : divide_up(a.slots, S::BM);       // at most
-  // (the limit belongs to the kernel and not to the call, so it is always the same)
   if (S::kLds > 48 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k_tiles<S, TO>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)S::kLds) != hipSuccess)
     return NVFP4_ERR_HIP;
   const int64_t grid = divide_up(units * tiles_n, 8) * 8;
-  if (grid > 0x7fffffff) return NVFP4_ERR_UNSUPPORTED;
+  if (grid * S::kThreads > 0xffffffff) return NVFP4_ERR_UNSUPPORTED;             // (more threads than a launch has: an output of a terabyte)
   return launch(k_tiles<S, TO>, dim3((uint32_t)grid), dim3(S::kThreads), S::kLds, s, a, (int32_t)tiles_n);
 }
-template <typename T, typename TO, int MT>
-int run_few(const ProductArgs &a, hipStream_t s) {
-  const dim3 grid((uint32_t)divide_up(a.out_width, 16), (uint32_t)(a.experts + (a.begin ? 1 : 0)));
-  return launch(k_few<T, TO, MT>, grid, dim3(kFewWaves * 64), 0, s, a);
-}
 
-template <typename T, typename TO>
-int run_product(const ProductArgs &a, hipStream_t s) {
-  const int64_t each = a.slots / a.experts;
-  if (a.rows == 0 || each <= 16) return run_few<T, TO, 1>(a, s);
-  if (each <= 256) return run_tiles<Shape<T, 2, 1, 1, 1, 4, sizeof(T) == 4 ? 2 : 3>, TO>(a, s);
-  if constexpr (sizeof(T) == 4) return run_tiles<Shape<T, 2, 2, 2, 2, 1, 3>, TO>(a, s);
-  else return run_tiles<Shape<T, 4, 4, 2, 2, 1, 3>, TO>(a, s);
+template <typename TO>
+int run_product(const ProductArgs &a, __bf16, hipStream_t s) {
+  typedef __bf16 T;
+  switch (choose(a, false)) {
+    case kFew4: return run_few<T, TO, 4, 8, 1>(a, s);
+    case kFew8: return run_few<T, TO, 8, 4, 2>(a, s);
+    case kFew16: return run_few<T, TO, 16, 8, 1>(a, s);
+    case kTile32: return run_tiles<Shape<T, 1, 1, 1, 1, 8, 3>, TO>(a, s);
+    case kTile64x32: return run_tiles<Shape<T, 2, 1, 1, 1, 4, 3>, TO>(a, s);
+    case kTile64: return run_tiles<Shape<T, 2, 2, 1, 1, 4, 3>, TO>(a, s);
+    case kTile64x128: return run_tiles<Shape<T, 2, 2, 1, 2, 2, 4>, TO>(a, s);
+    case kTile128: return run_tiles<Shape<T, 4, 2, 1, 2, 2, 3>, TO>(a, s);
+    case kTile128x256: return run_tiles<Shape<T, 2, 4, 2, 2, 1, 3>, TO>(a, s);
+    case kTile128x256Pair: return run_tiles<Shape<T, 4, 4, 1, 2, 1, 3>, TO>(a, s);      // (two waves, and two such workgroups a compute unit)
+    case kTile256: return run_tiles<Shape<T, 4, 4, 2, 2, 1, 3>, TO>(a, s);
+    default: return NVFP4_ERR_UNSUPPORTED;       // (not among the costs)
+  }
+}
+template <typename TO>
+int run_product(const ProductArgs &a, float, hipStream_t s) {
+  typedef float T;
+  switch (choose(a, true)) {
+    case kFew4: return run_few<T, TO, 2, 8, 1>(a, s);
+    case kFew8: return run_few<T, TO, 4, 4, 2>(a, s);
+    case kFew16: return run_few<T, TO, 8, 8, 1>(a, s);
+    case kTile32: return run_tiles<Shape<T, 1, 1, 1, 1, 4, 2>, TO>(a, s);
+    case kTile64: return run_tiles<Shape<T, 2, 2, 1, 1, 4, 2>, TO>(a, s);
+    case kTile64x128: return run_tiles<Shape<T, 2, 2, 1, 2, 2, 3>, TO>(a, s);
+    case kTile64x256: return run_tiles<Shape<T, 2, 4, 1, 2, 1, 3>, TO>(a, s);
+    case kTile128x256: return run_tiles<Shape<T, 2, 4, 2, 2, 1, 3>, TO>(a, s);
+    default: return NVFP4_ERR_UNSUPPORTED;
+  }
 }
 
 int product(const void *x, const nvfp4_product_params *p, const int32_t *token, const int32_t *begin, const void *codes,
@@ -529,8 +777,8 @@ int product(const void *x, const nvfp4_product_params *p, const int32_t *token, 
                       p->flags & NVFP4_GEMM_B_TILE_SCALES ? 4 : 0};
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool of32 = p->x_dtype == NVFP4_X_F32, to32 = p->out_dtype == NVFP4_OUT_F32;
-  return of32 ? to32 ? run_product<float, float>(a, s) : run_product<float, __bf16>(a, s)
-              : to32 ? run_product<__bf16, float>(a, s) : run_product<__bf16, __bf16>(a, s);
+  return of32 ? to32 ? run_product<float>(a, float{}, s) : run_product<__bf16>(a, float{}, s)
+              : to32 ? run_product<float>(a, __bf16{}, s) : run_product<__bf16>(a, __bf16{}, s);
 }
 
 }  // namespace
