@@ -21,6 +21,7 @@ namespace {
 
 constexpr int64_t kMostTokens = (1 << 24) - 1, kMostWidth = 1 << 22, kMostTop = 64, kMostExperts = 1024, kMostPairs = (int64_t)1 << 30;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kHeld = 4;                        // steps of 64 pairs that a wave keeps in registers
 constexpr int64_t kSortOne = 4096;              // pairs that one workgroup sorts by itself
 constexpr int64_t kSortBlocks = 128;            // ... and of more pairs at most so many workgroups
 
@@ -36,21 +37,35 @@ struct Piece;
 template <>
 struct Piece<__bf16> {
   bf16x8 v;
-  __device__ void load(const __bf16 *p) { v = *reinterpret_cast<const bf16x8 *>(p); }
-  __device__ void store(__bf16 *p) const { *reinterpret_cast<bf16x8 *>(p) = v; }
+  template <bool PAST = false>
+  __device__ void load(const __bf16 *p) {
+    const auto *const q = reinterpret_cast<const bf16x8 *>(p);
+    if constexpr (PAST) v = __builtin_nontemporal_load(q);
+    else v = *q;
+  }
+  template <bool PAST = false>
+  __device__ void store(__bf16 *p) const {
+    auto *const q = reinterpret_cast<bf16x8 *>(p);
+    if constexpr (PAST) __builtin_nontemporal_store(v, q);
+    else *q = v;
+  }
   __device__ f32x8 wide() const { return __builtin_convertvector(v, f32x8); }
   __device__ void round(f32x8 f) { v = __builtin_convertvector(f, bf16x8); }
 };
 template <>
 struct Piece<float> {
   f32x4 lo, hi;
+  template <bool PAST = false>
   __device__ void load(const float *p) {
-    lo = *reinterpret_cast<const f32x4 *>(p);
-    hi = *reinterpret_cast<const f32x4 *>(p + 4);
+    const auto *const q = reinterpret_cast<const f32x4 *>(p);
+    if constexpr (PAST) lo = __builtin_nontemporal_load(q), hi = __builtin_nontemporal_load(q + 1);
+    else lo = q[0], hi = q[1];
   }
+  template <bool PAST = false>
   __device__ void store(float *p) const {
-    *reinterpret_cast<f32x4 *>(p) = lo;
-    *reinterpret_cast<f32x4 *>(p + 4) = hi;
+    auto *const q = reinterpret_cast<f32x4 *>(p);
+    if constexpr (PAST) __builtin_nontemporal_store(lo, q), __builtin_nontemporal_store(hi, q + 1);
+    else q[0] = lo, q[1] = hi;
   }
   __device__ f32x8 wide() const { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
   __device__ void round(f32x8 f) {
@@ -120,9 +135,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(SortArgs a) {
     }
     return m;
   };
+  const auto load = [&](int32_t i) { return i < end ? group_of(a, i) : groups; };         // (past the end: a group of its own, which nobody reads)
+  int32_t held[kHeld];                           // the first ones, for both passes
+#pragma unroll
+  for (int n = 0; n < kHeld; ++n) held[n] = load(begin + n * 64 + lane);
   for (int pass = 0; pass < 2; ++pass) {
-    for (int32_t i0 = begin; i0 < end; i0 += 64) {
-      const int32_t i = i0 + lane, l = i < end ? group_of(a, i) : groups;       // (past the end: a group of its own, which nobody reads)
+    const auto take = [&](int32_t i0, int32_t l) __attribute__((always_inline)) {
+      const int32_t i = i0 + lane;
       const uint64_t m = alike(l);
       const int32_t before = __popcll(m & (((uint64_t)1 << lane) - 1));
       // A wave's LDS instructions run in their order, so the lanes have all read before the first of each group adds; the fences keep
@@ -138,7 +157,11 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(SortArgs a) {
       }
       if (before == 0) __hip_atomic_fetch_add(mine + l, __popcll(m), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
+    };
+#pragma unroll
+    for (int n = 0; n < kHeld; ++n)
+      if (begin + n * 64 < end) take(begin + n * 64, held[n]);
+    for (int32_t i0 = begin + kHeld * 64; i0 < end; i0 += 64) take(i0, load(i0 + lane));
     if (pass == 1) break;
     if (gridDim.x > 1) {
       // (as many threads to a group as there are; whole numbers, whose sums do not depend on their order)
@@ -215,7 +238,7 @@ __device__ inline Spot spot_of(const RowArgs &a) {
   return {(int32_t)blockIdx.x * (kRowThreads / a.lanes) + of, (int32_t)blockIdx.y * (a.lanes * U) + in};
 }
 
-template <typename TI, typename TO, int U>
+template <typename TI, typename TO, int U, bool PAST>
 __global__ void __launch_bounds__(kRowThreads) k_spread(RowArgs a) {
   const Spot at = spot_of<U>(a);
   if (at.token >= a.tokens) return;
@@ -241,14 +264,16 @@ __global__ void __launch_bounds__(kRowThreads) k_spread(RowArgs a) {
       if (piece >= a.pieces) continue;
       Piece<TO> out = v[u];
       if (p < 0) out.round(f32x8{});
-      out.store(to + (int64_t)piece * 8);
+      out.template store<PAST>(to + (int64_t)piece * 8);
     }
   }
 }
 
 // ---- combine ------------------------------------------------------------------------------------------------------------
 
-template <typename TS, typename TT, int U>
+constexpr int kAhead = 4;                        // places whose rows are on their way at once
+
+template <typename TS, typename TT, int U, bool PAST>
 __global__ void __launch_bounds__(kRowThreads) k_combine(RowArgs a) {
   const Spot at = spot_of<U>(a);
   if (at.token >= a.tokens) return;
@@ -264,18 +289,29 @@ __global__ void __launch_bounds__(kRowThreads) k_combine(RowArgs a) {
     }
   }
   const int32_t *const place = a.place + (int64_t)at.token * a.top;
-  for (int32_t j = 0; j < a.top; ++j) {
-    const int32_t p = place[j];
-    if (p < 0 || p >= a.slots) continue;
-    const float w = a.weights ? a.weights[(int64_t)at.token * a.top + j] : 1.0f;
-    const TS *const from = static_cast<const TS *>(a.slot_rows) + (int64_t)p * a.ld_slot;
+  const float *const weights = a.weights ? a.weights + (int64_t)at.token * a.top : nullptr;
+  for (int32_t j0 = 0; j0 < a.top; j0 += kAhead) {
+    int32_t p[kAhead];
+    float w[kAhead];
+    Piece<TS> in[kAhead][U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int32_t piece = at.piece + u * a.lanes;
-      if (piece >= a.pieces) continue;
-      Piece<TS> in;
-      in.load(from + (int64_t)piece * 8);
-      sum[u] += w * in.wide();
+    for (int i = 0; i < kAhead; ++i) {
+      p[i] = j0 + i < a.top ? place[j0 + i] : -1;
+      w[i] = weights && j0 + i < a.top ? weights[j0 + i] : 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (p[i] < 0 || p[i] >= a.slots) continue;
+      const TS *const from = static_cast<const TS *>(a.slot_rows) + (int64_t)p[i] * a.ld_slot;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (at.piece + u * a.lanes < a.pieces) in[i][u].template load<PAST>(from + (int64_t)(at.piece + u * a.lanes) * 8);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (p[i] < 0 || p[i] >= a.slots) continue;
+#pragma unroll
+      for (int u = 0; u < U; ++u) sum[u] += w[i] * in[i][u].wide();
     }
   }
 #pragma unroll
@@ -288,42 +324,63 @@ __global__ void __launch_bounds__(kRowThreads) k_combine(RowArgs a) {
   }
 }
 
-// A workgroup has a token.  (ys may be dys: an element is read before the same lane writes it.)
-template <typename TS, typename TT>
+// WAVES waves have a token, each P pieces a lane at a time, and keep those of dy while they go through the places; a row of more pieces than that is
+// gone through again and again.  (ys may be dys: an element is read before the same lane writes it.)
+template <typename TS, typename TT, int WAVES, int P, bool PAST>
 __global__ void __launch_bounds__(kRowThreads) k_combine_backward(RowArgs a) {
-  __shared__ float part[kRowThreads / 64];
-  const int32_t token = (int32_t)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  constexpr int kTokens = kRowThreads / 64 / WAVES, kLanes = 64 * WAVES;
+  __shared__ float part[2][kTokens][WAVES];
+  const int32_t in = (int32_t)threadIdx.x % kLanes, of = (int32_t)threadIdx.x / kLanes, wave = __builtin_amdgcn_readfirstlane(in / 64);
+  const int32_t token = __builtin_amdgcn_readfirstlane((int32_t)blockIdx.x * kTokens + of);
+  const bool is_token = token < a.tokens;
+  if (WAVES == 1 && !is_token) return;           // (no barriers)
   const TT *const dy = static_cast<const TT *>(a.token_rows) + (int64_t)token * a.ld_token;
+  Piece<TT> held[P];
+  const auto fetch = [&](int32_t first) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (is_token && first + i * kLanes < a.pieces) held[i].load(dy + (int64_t)(first + i * kLanes) * 8);
+  };
+  fetch(in);
+  const bool whole = a.pieces <= P * kLanes;
   for (int32_t j = 0; j < a.top; ++j) {
-    const int32_t p = a.place[(int64_t)token * a.top + j], slot = p < 0 ? ~p : p;
-    const bool is = p >= 0 && p < a.slots;
+    const int32_t p = is_token ? a.place[(int64_t)token * a.top + j] : 0, slot = p < 0 ? ~p : p;
+    const bool there = is_token && slot < a.slots, is = there && p >= 0;
     const float w = is ? a.weights[(int64_t)token * a.top + j] : 0.0f;
     const TS *const ys = static_cast<const TS *>(a.slot_rows) + (int64_t)slot * a.ld_slot;
     TS *const dys = static_cast<TS *>(a.slot_out) + (int64_t)slot * a.ld_dslot;
     float dot = 0.0f;
-    for (int32_t piece = threadIdx.x; slot < a.slots && piece < a.pieces; piece += kRowThreads) {
-      Piece<TS> out;
-      out.round(f32x8{});
+    for (int32_t first = in; there && first < a.pieces; first += P * kLanes) {
+      if (!whole) fetch(first);
+      Piece<TS> y[P];
       if (is) {
-        Piece<TT> d;
-        d.load(dy + (int64_t)piece * 8);
-        Piece<TS> y;
-        y.load(ys + (int64_t)piece * 8);
-        const f32x8 dv = d.wide(), yv = y.wide();
-        for (int i = 0; i < 8; ++i) dot += dv[i] * yv[i];
-        out.round(w * dv);
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+          if (first + i * kLanes < a.pieces) y[i].template load<PAST>(ys + (int64_t)(first + i * kLanes) * 8);
       }
-      out.store(dys + (int64_t)piece * 8);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        if (first + i * kLanes >= a.pieces) continue;
+        Piece<TS> out;
+        if (is) {
+          const f32x8 dv = held[i].wide(), yv = y[i].wide();
+          for (int k = 0; k < 8; ++k) dot += dv[k] * yv[k];
+          out.round(w * dv);
+        } else {
+          out.round(f32x8{});
+        }
+        out.template store<PAST>(dys + (int64_t)(first + i * kLanes) * 8);
+      }
     }
     for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
-    if (lane == 0) part[wave] = dot;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      float all = 0.0f;
-      for (int i = 0; i < kRowThreads / 64; ++i) all += part[i];
-      a.dweights[(int64_t)token * a.top + j] = is ? all : 0.0f;
+    if constexpr (WAVES > 1) {
+      float(*const mine)[WAVES] = part[j & 1];   // (read again only behind the next place's barrier)
+      if (in % 64 == 0) mine[of][wave] = dot;
+      __syncthreads();
+      dot = 0.0f;
+      for (int i = 0; i < WAVES; ++i) dot += mine[of][i];
     }
-    __syncthreads();
+    if (is_token && in == 0) a.dweights[(int64_t)token * a.top + j] = is ? dot : 0.0f;
   }
 }
 
@@ -361,6 +418,16 @@ dim3 row_grid(RowArgs &a) {
   a.lanes = lanes;
   return dim3((uint32_t)divide_up(a.tokens, kRowThreads / lanes), (uint32_t)divide_up(a.pieces, lanes * U));
 }
+
+// More rows of slots than the caches keep are written, and read for the last time, past them.  BF16, us, through / past: spread 33.5 / 35.7 for 134 MB,
+// 66 / 61 for 262, 139 / 118 for 537; combine 38.6 / 34.1 for 134 MB, 49 / 43 for 131 of two places a token, 149 / 131 for 537 (fp32 80 / 82
+// for 346); gradients 50 / 55 for 134 MB, 94.4 / 93.7 for 230, 114 / 105 for 268.
+bool past_caches(const nvfp4_experts_params &p, int64_t mbytes) {
+  return p.tokens * p.top * p.width * (p.slot_dtype == NVFP4_X_F32 ? 4 : 2) > mbytes << 20;
+}
+// Four pieces a lane where that leaves eight waves for each compute unit (us, one / two / four: spread of 16384 x 4096, past the caches, 139 / 141 / 118,
+// combine 150 / 157 / 131), else one (1000 tokens, 2048 columns, combine 5.8 / 6.1 / 7.0).
+bool many(const nvfp4_experts_params &p) { return p.tokens * divide_up(p.width, 8 * 64 * 4) >= 2048; }
 
 // kernel<types of slots and tokens> for the types of a call
 template <typename F>
@@ -429,9 +496,13 @@ extern "C" int nvfp4_experts_spread(const void *x, const nvfp4_experts_params *p
   RowArgs a = row_args(*p, place);
   a.token_rows = x;
   a.slot_out = xs;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
   return by_types(*p, [&](auto slot, auto token) {
-    const dim3 grid = row_grid<2>(a);
-    return launch(k_spread<decltype(token), decltype(slot), 2>, grid, dim3(kRowThreads), 0, static_cast<hipStream_t>(stream), a);
+    typedef decltype(slot) TO;
+    typedef decltype(token) TI;
+    const bool four = many(*p), past = four && past_caches(*p, 192);
+    const dim3 grid = four ? row_grid<4>(a) : row_grid<1>(a);
+    return launch(past ? k_spread<TI, TO, 4, true> : four ? k_spread<TI, TO, 4, false> : k_spread<TI, TO, 1, false>, grid, dim3(kRowThreads), 0, s, a);
   });
 }
 
@@ -453,9 +524,14 @@ extern "C" int nvfp4_experts_combine(const void *ys, const nvfp4_experts_params 
   a.token_out = y;
   a.slot_rows = ys;
   a.weights = weights;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
   return by_types(*p, [&](auto slot, auto token) {
-    const dim3 grid = row_grid<2>(a);
-    return launch(k_combine<decltype(slot), decltype(token), 2>, grid, dim3(kRowThreads), 0, static_cast<hipStream_t>(stream), a);
+    typedef decltype(slot) TS;
+    typedef decltype(token) TT;
+    const bool four = many(*p), past = four && past_caches(*p, 96);
+    const dim3 grid = four ? row_grid<4>(a) : row_grid<1>(a);
+    return launch(past ? k_combine<TS, TT, 4, true> : four ? k_combine<TS, TT, 4, false> : k_combine<TS, TT, 1, false>, grid, dim3(kRowThreads), 0, s,
+                  a);
   });
 }
 
@@ -478,8 +554,14 @@ extern "C" int nvfp4_experts_combine_backward(const void *dy, const nvfp4_expert
   a.slot_out = dys;
   a.weights = weights;
   a.dweights = dweights;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
   return by_types(*p, [&](auto slot, auto token) {
-    return launch(k_combine_backward<decltype(slot), decltype(token)>, dim3((uint32_t)a.tokens), dim3(kRowThreads), 0,
-                  static_cast<hipStream_t>(stream), a);
+    typedef decltype(slot) TS;
+    typedef decltype(token) TT;
+    const auto run = [&](auto kernel, int tokens) { return launch(kernel, dim3((uint32_t)divide_up(a.tokens, tokens)), dim3(kRowThreads), 0, s, a); };
+    // (two waves a token for short rows, us, two / four waves: 4000 x 1024 12.4 / 15.4, 1000 x 2048 8.8 / 8.6, 4096 x 4096 50 / 50, 5001 x 2880 99.8 / 94.4)
+    if (a.pieces <= 64) return run(k_combine_backward<TS, TT, 1, 1, false>, 4);
+    if (a.pieces <= 256) return run(k_combine_backward<TS, TT, 2, 2, false>, 2);
+    return past_caches(*p, 192) ? run(k_combine_backward<TS, TT, 4, 2, true>, 1) : run(k_combine_backward<TS, TT, 4, 2, false>, 1);
   });
 }

@@ -652,26 +652,28 @@ bool sizes_fit(const nvfp4_product_params &p) {
 // experts, 1024 x 2560, 7.3 / 11.2; but 200 of 32, 3216 x 256, 20 / 17.7 and 1024 of 64, 1024 x 2048, 54 / 34.5.)
 // Else k_tiles in the shape that takes least by the estimate below: turns of tiles over the compute units, each a + f microseconds for 1024 of K and besides.
 // The constants are fitted to 150 products, 1 to 4096 tokens, K 256 to 8192, up to 16384 columns, 1 to 128 experts (uneven), each in all shapes: the
-// choice is 2.7 % (fp32: 1.7 %) slower than the best of each, 30 % at most.
+// choice is 2.3 % (fp32: 1.9 %) slower than the best of each, 30 % at most.
 
 enum Kernel { kFew4, kFew8, kFew16, kTile32, kTile64x32, kTile64, kTile64x128, kTile64x256, kTile128, kTile128x256, kTile128x256Pair, kTile256 };
 
 struct Cost {
   Kernel kernel;
   int32_t rows, columns;
+  int32_t at_once;             // tiles of a turn
   double a, f;                 // us a turn: for 1024 of K, and besides
 };
-constexpr Cost kCostBf16[] = {{kTile32, 32, 32, 0.90, 3.9},      {kTile64x32, 64, 32, 1.88, 3.7},     {kTile64, 64, 64, 3.09, 3.9},
-                              {kTile64x128, 64, 128, 5.98, 3.9}, {kTile128, 128, 128, 7.71, 5.3},     {kTile128x256, 128, 256, 15.04, 6.8},
-                              {kTile128x256Pair, 128, 256, 18.21, 8.7}, {kTile256, 256, 256, 20.43, 13.5}};
-constexpr Cost kCostF32[] = {{kTile32, 32, 32, 3.54, 3.0},
-                             {kTile64, 64, 64, 9.68, 5.0},
-                             {kTile64x128, 64, 128, 17.72, 6.1},
-                             {kTile64x256, 64, 256, 34.47, 5.7},
-                             {kTile128x256, 128, 256, 42.74, 11.3}};
+constexpr Cost kCostBf16[] = {{kTile32, 32, 32, 256, 0.90, 3.9},      {kTile64x32, 64, 32, 256, 1.88, 3.7},
+                              {kTile64, 64, 64, 256, 3.09, 3.9},      {kTile64x128, 64, 128, 256, 5.98, 3.9},
+                              {kTile128, 128, 128, 256, 8.6, 5.3},    {kTile128x256, 128, 256, 256, 15.0, 6.8},
+                              {kTile128x256Pair, 128, 256, 512, 25.0, 16.0}, {kTile256, 256, 256, 256, 25.0, 13.5}};
+constexpr Cost kCostF32[] = {{kTile32, 32, 32, 256, 3.54, 3.0},
+                             {kTile64, 64, 64, 256, 9.68, 5.0},
+                             {kTile64x128, 64, 128, 256, 17.72, 6.1},
+                             {kTile64x256, 64, 256, 256, 34.47, 5.7},
+                             {kTile128x256, 128, 256, 256, 42.74, 11.3}};
 
-double turns_of(double tiles) {
-  const double t = tiles / 256;
+double turns_of(double tiles, int32_t at_once) {
+  const double t = tiles / at_once;
   return t <= 1 ? 1 : t + (std::ceil(t) - t) / 2;
 }
 // Tiles down the rows: half a tile of every expert's is empty on average, and each that has rows has one.
@@ -685,7 +687,7 @@ Kernel least(const ProductArgs &a, const Cost (&costs)[N]) {
   Kernel best = costs[0].kernel;
   double least = 1e300;
   for (const Cost &c : costs) {
-    const double us = turns_of(tiles_down(a, c.rows) * (double)divide_up(a.out_width, c.columns)) * (c.a * a.inp / 1024 + c.f);
+    const double us = turns_of(tiles_down(a, c.rows) * (double)divide_up(a.out_width, c.columns), c.at_once) * (c.a * a.inp / 1024 + c.f);
     if (us < least) least = us, best = c.kernel;
   }
   return best;
