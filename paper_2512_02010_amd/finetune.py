@@ -157,16 +157,16 @@ def nvfp4_distill_step(logits: torch.Tensor, teacher: torch.Tensor, index: torch
 # ---- a quantized layer with adapters ------------------------------------------------------------
 
 def adapted_fprop(x: torch.Tensor, qw: dict, a: torch.Tensor, b: torch.Tensor, which: torch.Tensor, scales: torch.Tensor,
-                  want_h: bool = False, workspace: torch.Tensor | None = None):
+                  want_h: bool = False, workspace: torch.Tensor | None = None, weight_only: bool = False):
     """y [T][N] BF16 = x W^T of a quantized weight (``linear.quantize_weight``), with every token's adapter added; with
-    ``want_h`` (y, h).  ``workspace`` is that of ``linear.fprop``."""
-    y = L.fprop(x, qw, workspace=workspace)
+    ``want_h`` (y, h).  ``workspace`` and ``weight_only`` are those of ``linear.fprop``."""
+    y = L.fprop(x, qw, workspace=workspace, weight_only=weight_only)
     return nvfp4_adapters_forward(x, y, a, b, which, scales, want_h=want_h, out=y)
 
 
 def adapted_backward(dy: torch.Tensor, x: torch.Tensor, h: torch.Tensor, qw: dict, a: torch.Tensor, b: torch.Tensor,
                      which: torch.Tensor, scales: torch.Tensor, sr_seed: int, want_dx: bool = True,
-                     workspace: torch.Tensor | None = None):
+                     workspace: torch.Tensor | None = None, weight_only: bool = False):
     """(dx, da, db) of ``adapted_fprop``; the weight itself stays as it is."""
-    dx = L.dgrad(dy, qw, sr_seed, workspace=workspace) if want_dx else None
+    dx = L.dgrad(dy, qw, sr_seed, workspace=workspace, weight_only=weight_only) if want_dx else None
     return nvfp4_adapters_backward(dy, x, h, a, b, which, scales, dx_base=dx, want_dx=want_dx, out=dx)

@@ -24,6 +24,9 @@ Every function takes an optional ``workspace`` (``binding.new_workspace()``).  W
 a tensor scale is one launch; on another stream without a workspace it is three.  ``wgrad`` on the current stream finds the
 scales of its two operands in one launch and their codes in a second where such scratch words are at hand and the operands
 are not too large for it (``nvfp4_46_wgrad_operands`` in csrc/nvfp4_46.hip).  One workspace serves all calls issued on one stream.
+
+With ``weight_only`` FPROP and DGRAD take their other operand as it is, BF16 or fp32 (``experts.nvfp4_weight_product``): how a
+quantized weight is served where activations are not quantized, and differentiated where gradients are not.
 """
 from __future__ import annotations
 
@@ -52,9 +55,16 @@ def _columnwise(t, stream, workspace, rht_seed, **kw):
     return q["codes_col"], q["scales_col"], q["alpha"]
 
 
+def _weight_only(x, codes, scales, qw, stream):
+    from . import experts
+    return experts.nvfp4_weight_product(x, codes, scales, qw["alpha"], flags=B.GEMM_B_TILE_SCALES if qw["block2d"] else 0, stream=stream)
+
+
 def fprop(x: torch.Tensor, qw: dict, select: int = B.SEL_46_MSE, stream=None,
-          workspace: torch.Tensor | None = None) -> torch.Tensor:
+          workspace: torch.Tensor | None = None, weight_only: bool = False) -> torch.Tensor:
     """y [T][N] BF16 = x W^T."""
+    if weight_only:
+        return _weight_only(x, qw["codes_row"], qw["scales_row"], qw, stream)
     flags = B.GEMM_B_TILE_SCALES if qw["block2d"] else 0
     if stream is None:
         y = B.product_of_rows(x, qw["codes_row"], qw["scales_row"], qw["alpha"], flags, B.RTN, select, 0, workspace)
@@ -66,8 +76,10 @@ def fprop(x: torch.Tensor, qw: dict, select: int = B.SEL_46_MSE, stream=None,
 
 
 def dgrad(dy: torch.Tensor, qw: dict, sr_seed: int, select: int = B.SEL_46_MSE,
-          stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """dx [T][K] BF16 = dy W, the gradient rounded stochastically."""
+          stream=None, workspace: torch.Tensor | None = None, weight_only: bool = False) -> torch.Tensor:
+    """dx [T][K] BF16 = dy W, the gradient rounded stochastically (or, with ``weight_only``, not at all)."""
+    if weight_only:
+        return _weight_only(dy, qw["codes_col"], qw["scales_col"], qw, stream)
     flags = B.GEMM_B_TILE_SCALES if qw["block2d"] else 0
     if stream is None:
         dx = B.product_of_rows(dy, qw["codes_col"], qw["scales_col"], qw["alpha"], flags, B.SR, select, sr_seed, workspace)

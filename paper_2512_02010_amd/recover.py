@@ -1,12 +1,14 @@
-"""Recovering what quantization lost: ``python -m paper_2512_02010_amd.recover``.
+"""Recovering what quantization lost: ``python -m paper_2512_02010_amd.recover [--weight-only]``.
 
 A small example that runs the package's pieces as they are meant to be used together.  A feed-forward model with random
 weights is the teacher, in full precision.  Its weights quantized to NVFP4 are the student, which stays frozen; beside each of its layers
 stand low-rank adapters, one for each of two tasks.  Every step distils the teacher's top logits into the adapters of the tokens'
 tasks (``finetune.nvfp4_distill_step``, ``adapted_fprop``, ``adapted_backward``).  At the end one batch mixes both tasks and tokens without an
-adapter, as a server's does.
+adapter, as a server's does.  With ``weight_only`` the student's activations and gradients are not quantized.
 """
 from __future__ import annotations
+
+import sys
 
 import torch
 
@@ -17,8 +19,9 @@ from . import linear as L
 class AdaptedLinear:
     """A quantized, frozen weight [N][K] with an adapter of rank r for each of several tasks; fp32 master copies, Adam."""
 
-    def __init__(self, weight: torch.Tensor, adapters: int, rank: int, generator: torch.Generator):
+    def __init__(self, weight: torch.Tensor, adapters: int, rank: int, generator: torch.Generator, weight_only: bool = False):
         n, k = weight.shape
+        self.weight_only = weight_only
         self.quantized = L.quantize_weight(weight)
         a = torch.randn((adapters, rank, k), generator=generator, device=weight.device) / k ** 0.5
         self.master = [a, torch.zeros((adapters, n, rank), device=weight.device)]          # B = 0: no change at first
@@ -30,14 +33,16 @@ class AdaptedLinear:
         self.a, self.b = (t.bfloat16() for t in self.master)
 
     def forward(self, x, which, keep: bool):
-        y, h = F.adapted_fprop(x, self.quantized, self.a, self.b, which, self.scales, want_h=True)
+        y, h = F.adapted_fprop(x, self.quantized, self.a, self.b, which, self.scales, want_h=True,
+                               weight_only=self.weight_only)
         if keep:
             self.kept = (x, h, which)
         return y
 
     def backward(self, dy, seed: int, want_dx: bool = True):
         x, h, which = self.kept
-        dx, *self.grads = F.adapted_backward(dy, x, h, self.quantized, self.a, self.b, which, self.scales, seed, want_dx=want_dx)
+        dx, *self.grads = F.adapted_backward(dy, x, h, self.quantized, self.a, self.b, which, self.scales, seed, want_dx=want_dx,
+                                             weight_only=self.weight_only)
         return dx
 
     def update(self, step: int, rate: float):
@@ -49,7 +54,7 @@ class AdaptedLinear:
 
 
 def run(steps: int = 60, tokens: int = 512, width: int = 256, hidden: int = 512, vocab: int = 2048, rank: int = 16, top: int = 32,
-        seed: int = 0, rate: float = 2e-3, say=lambda *a: None):
+        seed: int = 0, rate: float = 2e-3, say=lambda *a: None, weight_only: bool = False):
     """Returns (mean loss of every step, mean loss with adapters and without in the last, mixed batch)."""
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
@@ -60,7 +65,7 @@ def run(steps: int = 60, tokens: int = 512, width: int = 256, hidden: int = 512,
     shapes = ((hidden, width), (width, hidden), (vocab, width))
     weights = [normal(*s) * (1.6 / s[1] ** 0.5) for s in shapes]
     words = normal(vocab, width)
-    layers = [AdaptedLinear(w, 2, rank, g) for w in weights]
+    layers = [AdaptedLinear(w, 2, rank, g, weight_only) for w in weights]
 
     def teacher(x):
         x = x.float()
@@ -98,4 +103,4 @@ def run(steps: int = 60, tokens: int = 512, width: int = 256, hidden: int = 512,
 
 
 if __name__ == "__main__":
-    run(say=print)
+    run(say=print, weight_only="--weight-only" in sys.argv[1:])

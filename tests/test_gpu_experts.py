@@ -81,12 +81,14 @@ def slots_of(T, k, W, dtype, seed=4):
 
 ROWS = [  # T, k, W
     (0, 2, 8), (1, 1, 8), (1, 3, 4096), (2, 64, 24), (5, 2, 16), (33, 4, 56), (64, 4, 4096), (100, 6, 520), (257, 8, 2880), (1000, 2, 1032),
-    (3, 5, 20000), (4100, 1, 64), (7, 2, 8192), (9, 4, 8200), (300, 9, 264),
+    (3, 5, 20000), (4100, 1, 64), (7, 2, 8192), (9, 4, 8200), (300, 9, 264), (2100, 1, 2056),
 ]
+# rows that are written and read past the caches: 96 MB and 192 MB of slots at least, in BF16
+ROWS_LARGE = [(9000, 3, 4104)]
 
 
 @pytest.mark.parametrize("dtype, slot_dtype", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
-@pytest.mark.parametrize("T, k, W", ROWS)
+@pytest.mark.parametrize("T, k, W", ROWS + ROWS_LARGE)
 def test_spread(T, k, W, dtype, slot_dtype):
     ids = ids_of(T, k, 6)
     place, token, begin = X.nvfp4_experts_sort(ids, 6)
@@ -111,7 +113,7 @@ def combined(ys, place, weights, base):
 
 @pytest.mark.parametrize("weighted, based", [(True, True), (False, False), (True, False)])
 @pytest.mark.parametrize("dtype, slot_dtype", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
-@pytest.mark.parametrize("T, k, W", ROWS[1:])
+@pytest.mark.parametrize("T, k, W", ROWS[1:] + ROWS_LARGE)
 def test_combine(T, k, W, dtype, slot_dtype, weighted, based):
     place, _, _ = X.nvfp4_experts_sort(ids_of(T, k, 6), 6)
     ys = slots_of(T, k, W, slot_dtype)
@@ -129,7 +131,7 @@ def test_combine(T, k, W, dtype, slot_dtype, weighted, based):
 
 
 @pytest.mark.parametrize("dtype, slot_dtype", [(BF16, BF16), (F32, F32), (BF16, F32), (F32, BF16)])
-@pytest.mark.parametrize("T, k, W", ROWS[1:])
+@pytest.mark.parametrize("T, k, W", ROWS[1:] + ROWS_LARGE)
 def test_combine_backward(T, k, W, dtype, slot_dtype):
     place, _, _ = X.nvfp4_experts_sort(ids_of(T, k, 6), 6)
     ys, dy, weights = slots_of(T, k, W, slot_dtype), slots_of(T, 1, W, dtype, 6), torch.rand((T, k), device="cuda")
@@ -234,3 +236,50 @@ def test_what_is_masked_does_not_reach_a_sum():
     # ... and what is not masked does
     ys[int(place[place >= 0][0])] = float("inf")
     assert bool(X.nvfp4_experts_combine(ys, place, None).isinf().any())
+
+
+def test_replayed_from_graphs_and_on_other_streams():
+    """Two captured graphs of sort, spread and combine with their gradients, replayed in turn beside eager calls on another stream."""
+    for T, k, E, W in ((30, 3, 5, 64), (3000, 4, 70, 264)):
+        ids, x, w = ids_of(T, k, E), slots_of(T, 1, W, BF16), torch.rand((T, k), device="cuda")
+
+        def call(stream=None):
+            place, token, begin = X.nvfp4_experts_sort(ids, E, stream=stream)
+            xs = X.nvfp4_experts_spread(x, place, stream=stream)
+            y = X.nvfp4_experts_combine(xs, place, w, base=x, stream=stream)
+            dys, dw = X.nvfp4_experts_combine_backward(y, xs, place, w, stream=stream)
+            return place, token, begin, xs, y, dys, dw
+
+        graphs = []
+        for _ in range(2):
+            call()
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                got = call()
+            graphs.append((graph, got))
+        side = torch.cuda.Stream()
+        for _ in range(3):
+            for graph, got in graphs:
+                ids.copy_(torch.roll(ids, 1, 0))
+                x.copy_(torch.roll(x, 3, 0))
+                side.wait_stream(torch.cuda.current_stream())
+                other = call(side)
+                graph.replay()
+                eager = call()
+                torch.cuda.synchronize()
+                assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(eager, got, other))
+
+
+def test_outputs_that_do_not_fit_are_refused():
+    place, _, _ = X.nvfp4_experts_sort(ids_of(4, 2, 3), 3)
+    x, xs, w = slots_of(4, 1, 64, BF16), slots_of(4, 2, 64, BF16), torch.rand((4, 2), device="cuda")
+    for call, text in (
+            (lambda: X.nvfp4_experts_spread(x, place, out=xs[:7]), "out must be of a shape"),
+            (lambda: X.nvfp4_experts_combine(xs, place, base=x, out=x.float()), "out must be BFloat16"),
+            (lambda: X.nvfp4_experts_combine_backward(x, xs, place, w, out=xs.float()), "out must be BFloat16"),
+            (lambda: X.nvfp4_experts_combine_backward(x, xs, place, w, out=xs[:, :32]), "out must be of a shape")):
+        with pytest.raises(AssertionError, match=text):
+            call()
+    with pytest.raises(B.Nvfp4Error, match="ALIGN"):
+        X.nvfp4_experts_spread(x, place, out=torch.empty((8, 68), dtype=BF16, device="cuda")[:, :64])

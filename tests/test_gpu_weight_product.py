@@ -59,6 +59,9 @@ SIZES = [  # T, K, N, tiles
     (64, 512, 4096, False), (65, 544, 130, False), (100, 2048, 1024, True), (127, 256, 257, False), (128, 1024, 1024, False),
     (129, 1056, 336, True), (200, 4096, 304, True), (255, 128, 511, False), (256, 8192, 256, False), (300, 32, 2000, False), (513, 992, 1008, True),
     (1000, 2048, 2049, False), (1025, 1024, 3008, True), (2049, 608, 1023, False),
+    (2, 256, 100, False), (4, 96, 64, True), (6, 512, 72, False), (7, 224, 60, False), (9, 256, 40, False), (12, 96, 300, False), (13, 768, 144, True),
+    (48, 512, 8192, False), (60, 96, 1000, False), (300, 2048, 4096, True), (2049, 608, 4096, False), (4096, 256, 4096, True),
+    (4000, 1056, 3000, False),
 ]
 
 
@@ -146,11 +149,13 @@ EXPERTS = [  # T, k, E, K, N, tiles
     (1, 1, 1, 32, 16, True), (1, 2, 4, 64, 100, False), (7, 3, 5, 160, 33, False), (32, 4, 64, 512, 256, True), (50, 2, 3, 1056, 144, True),
     (64, 8, 16, 256, 520, False), (200, 1, 200, 96, 40, False), (333, 2, 7, 288, 272, True), (600, 4, 8, 512, 500, False),
     (1500, 2, 2, 128, 384, True), (2000, 1, 1, 320, 64, False), (900, 6, 30, 224, 1040, True), (4000, 2, 3, 1024, 264, False),
+    (20, 2, 4, 96, 250, False), (4, 2, 4, 256, 256, True), (3, 3, 8, 160, 72, False), (30, 2, 16, 512, 64, True), (100, 2, 1024, 64, 48, True),
+    (4096, 4, 32, 2080, 2300, False), (6000, 2, 8, 128, 2048, True),
 ]
 
 
 @pytest.mark.parametrize("gather", [True, False])
-@pytest.mark.parametrize("dtype, out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32),
+@pytest.mark.parametrize("dtype, out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32),
                                               (torch.float32, torch.bfloat16)])
 @pytest.mark.parametrize("T, k, E, K, N, tiles", EXPERTS)
 def test_experts(T, k, E, K, N, tiles, dtype, out_dtype, gather):
@@ -210,3 +215,61 @@ def test_on_another_stream():
     got = X.nvfp4_weight_product(x, codes[0], scales[0], alpha, stream=side)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, want)
+
+
+def _in_two_graphs(call, inputs):
+    """Captured twice, replayed in turn with new values in the same tensors, eager work of the program's own between them."""
+    graphs = []
+    for _ in range(2):
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = call()
+        graphs.append((graph, got))
+    for turn in range(3):
+        for graph, got in graphs:
+            for t in inputs:
+                t.copy_(torch.roll(t, 1, 0))
+            eager = call()
+            graph.replay()
+            assert torch.equal(got, eager), turn
+            torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T", [1, 12, 40, 600])
+def test_replayed_from_a_graph(T):
+    codes, scales, alpha = weights(3, 512, 512, False)
+    x = rows(T, 512, torch.bfloat16)
+    _in_two_graphs(lambda: X.nvfp4_weight_product(x, codes[0], scales[0], alpha[:1]), [x])
+    begin = torch.tensor([0, T // 2, T // 2, T], dtype=torch.int32, device="cuda")
+    _in_two_graphs(lambda: X.nvfp4_experts_product(x, begin, codes, scales, alpha), [x])
+
+
+def test_two_streams_at_once():
+    """Nothing is shared between calls: many at once on two streams, of different sizes."""
+    (codes, scales, alpha), xs = weights(4, 1024, 1024, True), [rows(T, 1024, torch.bfloat16, T) for T in (3, 700)]
+    begin = [torch.tensor([0, 1, 1, 2, 3], dtype=torch.int32, device="cuda"), torch.tensor([0, 300, 301, 690, 700], dtype=torch.int32, device="cuda")]
+    want = [X.nvfp4_experts_product(x, b, codes, scales, alpha, flags=B.GEMM_B_TILE_SCALES) for x, b in zip(xs, begin)]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            got[i].append(X.nvfp4_experts_product(xs[i], begin[i], codes, scales, alpha, flags=B.GEMM_B_TILE_SCALES, stream=s))
+    torch.cuda.synchronize()
+    for i, w in enumerate(want):
+        assert all(torch.equal(g, w) for g in got[i])
+
+
+@pytest.mark.parametrize("T", [5, 200])
+def test_linear_layer_of_a_weight_alone(T):
+    """linear.fprop and dgrad with ``weight_only``: the library's products of the same operands, in the caller's types."""
+    g = torch.Generator().manual_seed(1)
+    q = L.quantize_weight(torch.randn((160, 96), generator=g).cuda())
+    for x, dy in ((rows(T, 96, torch.bfloat16), rows(T, 160, torch.bfloat16, 3)), (rows(T, 96, torch.float32), rows(T, 160, torch.float32, 3))):
+        w = values(q["codes_row"], q["scales_row"], True)
+        ref = q["alpha"].double() * (x.double() @ w.T)
+        close(L.fprop(x, q, weight_only=True), ref, bound(x, w, q["alpha"], ref, x.dtype, torch.bfloat16))
+        ref = q["alpha"].double() * (dy.double() @ w)
+        close(L.dgrad(dy, q, 0, weight_only=True), ref, bound(dy, w.T, q["alpha"], ref, dy.dtype, torch.bfloat16))
