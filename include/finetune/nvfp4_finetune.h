@@ -211,7 +211,9 @@ size_t nvfp4_experts_workspace_bytes(const nvfp4_experts_params *p);
  *   place      out  [tokens][top] int32, dense
  *   token      out  [tokens * top] int32
  *   begin      out  [experts + 1] int32
- *   workspace  scratch, 16-byte aligned; holds nothing between calls.  Calls whose work may overlap need one each.
+ *   workspace  scratch, 16-byte aligned; holds nothing between calls.  Calls whose work may overlap need one each.  Where 16 bytes are
+ *              enough, they are left alone.
+ * No output may overlap ids or another output.
  * Errors: NULL pointer -> ERR_NULL; sizes out of range -> ERR_SHAPE; a pointer that is not aligned to its elements -> ERR_ALIGN;
  * index_dtype, or workspace too small -> ERR_PARAM.                                                             */
 int nvfp4_experts_sort(const void *ids, const nvfp4_experts_params *p, int32_t *place, int32_t *token, int32_t *begin,

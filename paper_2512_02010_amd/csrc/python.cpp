@@ -831,8 +831,13 @@ PyObject *experts_sort(PyObject *const *v, Py_ssize_t n) {
       begin(new_tensor({p.experts + 1}, at::kInt, v[0], v[3]));
   auto *const pp = static_cast<int32_t *>(pointer(place.o)), *const pt = static_cast<int32_t *>(pointer(token.o)),
              *const pb = static_cast<int32_t *>(pointer(begin.o));
-  const Scratch w(v[2], need, v[0], v[3]);
-  run("nvfp4_experts_sort", [&] { return finetune.experts_sort(pi, &p, pp, pt, pb, w.p, w.bytes, on.handle()); });
+  // (the least workspace is one that the call leaves alone: any memory of its own will do, which saves an allocation)
+  if (v[2] == Py_None && need <= 16 && reinterpret_cast<uintptr_t>(pb) % 16 == 0) {
+    run("nvfp4_experts_sort", [&] { return finetune.experts_sort(pi, &p, pp, pt, pb, pb, 16, on.handle()); });
+  } else {
+    const Scratch w(v[2], need, v[0], v[3]);
+    run("nvfp4_experts_sort", [&] { return finetune.experts_sort(pi, &p, pp, pt, pb, w.p, w.bytes, on.handle()); });
+  }
   return PyTuple_Pack(3, place.o, token.o, begin.o);
 }
 

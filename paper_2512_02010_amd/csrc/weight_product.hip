@@ -650,31 +650,32 @@ bool sizes_fit(const nvfp4_product_params &p) {
 // a pass 4 / 8 / 16: 1 x 4096 x 4096 5.4 / 6.1 / 5.9, 4 x 15376 x 3584 9.3 / 10.3 / 11.8, 8 x 28672 x 4096 28 / 18.3 / 24, 16 x 8192 x 8192 30 / 19.6 / 13.7; 32
 // tokens of 4 among 64 experts, 1024 x 2048, 17.9 / 16.7 / 25.7.  Against the best tiles: 16 x 8192 x 8192 13.7 / 14, 28 x 480 x 512 5.4 / 4.8, 96 rows of 8
 // experts, 1024 x 2560, 7.3 / 11.2; but 200 of 32, 3216 x 256, 20 / 17.7 and 1024 of 64, 1024 x 2048, 54 / 34.5.)
-// Else k_tiles in the shape that takes least by the estimate below: turns of tiles over the compute units, each a + f microseconds for 1024 of K and besides.
-// The constants are fitted to 150 products, 1 to 4096 tokens, K 256 to 8192, up to 16384 columns, 1 to 128 experts (uneven), each in all shapes: the
-// choice is 2.3 % (fp32: 1.9 %) slower than the best of each, 30 % at most.
-
-enum Kernel { kFew4, kFew8, kFew16, kTile32, kTile64x32, kTile64, kTile64x128, kTile64x256, kTile128, kTile128x256, kTile128x256Pair, kTile256 };
+// Else k_tiles in the shape that takes least by the estimate below: turns of tiles over the 256 compute units, each a + f microseconds for 1024 of K and
+// besides.  The constants are fitted to 230 products, up to 8192 tokens, K 256 to 8192, up to 16384 columns, 1 to 128 experts (uneven), each
+// in all shapes: the choice is 1.8 % (fp32: 1.9 %) slower than the best of each on average.  (us at K = 8192 for up to one turn / 4096 x 8192 x 8192, BF16: 32 x 32
+// 14 / 1374, 64 x 32 23 / 1112, 64 x 64 30 / 835, 64 x 128 47.5 / 740, 128 x 128 55 to 70 / 510, 128 x 256 100 / 448, in two parts of K
+// 84 / 450, 256 x 256 144 / 411 to 428.  A wave of 128 x 64 expands least and leaves room for a second one on its SIMD: waves of 128 x 128 one by one took 160 /
+// 418 to 435, of 64 x 128 in tiles of 128 x 256 122 / 505.)
+// (K: in two parts of K)
+enum Kernel { kFew4, kFew8, kFew16, kTile32, kTile64x32, kTile64, kTile64x128, kTile64x256, kTile64x256K, kTile128, kTile128x256, kTile128x256K,
+              kTile256 };
 
 struct Cost {
   Kernel kernel;
   int32_t rows, columns;
-  int32_t at_once;             // tiles of a turn
   double a, f;                 // us a turn: for 1024 of K, and besides
 };
-constexpr Cost kCostBf16[] = {{kTile32, 32, 32, 256, 0.90, 3.9},      {kTile64x32, 64, 32, 256, 1.88, 3.7},
-                              {kTile64, 64, 64, 256, 3.09, 3.9},      {kTile64x128, 64, 128, 256, 5.98, 3.9},
-                              {kTile128, 128, 128, 256, 8.6, 5.3},    {kTile128x256, 128, 256, 256, 15.0, 6.8},
-                              {kTile128x256Pair, 128, 256, 512, 25.0, 16.0}, {kTile256, 256, 256, 256, 25.0, 13.5}};
-constexpr Cost kCostF32[] = {{kTile32, 32, 32, 256, 3.54, 3.0},
-                             {kTile64, 64, 64, 256, 9.68, 5.0},
-                             {kTile64x128, 64, 128, 256, 17.72, 6.1},
-                             {kTile64x256, 64, 256, 256, 34.47, 5.7},
-                             {kTile128x256, 128, 256, 256, 42.74, 11.3}};
+constexpr Cost kCostBf16[] = {{kTile32, 32, 32, 0.98, 3.9},        {kTile64x32, 64, 32, 1.92, 3.8},       {kTile64, 64, 64, 3.07, 4.3},
+                              {kTile64x128, 64, 128, 5.8, 4.6},    {kTile128, 128, 128, 8.0, 6.6},        {kTile128x256K, 128, 256, 12.0, 11.0},
+                              {kTile128x256, 128, 256, 13.4, 6.8}, {kTile256, 256, 256, 21.4, 18.0}};
+constexpr Cost kCostF32[] = {{kTile32, 32, 32, 3.8, 2.7},          {kTile64, 64, 64, 9.5, 5.5},           {kTile64x128, 64, 128, 16.3, 6.1},
+                             {kTile64x256K, 64, 256, 21.6, 8.5},   {kTile64x256, 64, 256, 23.6, 7.5},     {kTile128x256, 128, 256, 41.4, 11.1},
+                             {kTile256, 256, 256, 75.7, 10.3}};
 
-double turns_of(double tiles, int32_t at_once) {
-  const double t = tiles / at_once;
-  return t <= 1 ? 1 : t + (std::ceil(t) - t) / 2;
+// The last turn is nearly as long as a full one; of fp32 tiles, which leave a compute unit room for no second one, as long.
+double turns_of(double tiles, bool f32) {
+  const double t = tiles / 256;
+  return t <= 1 ? 1 : f32 ? std::ceil(t) : t + 0.75 * (std::ceil(t) - t);
 }
 // Tiles down the rows: half a tile of every expert's is empty on average, and each that has rows has one.
 double tiles_down(const ProductArgs &a, int32_t rows) {
@@ -683,11 +684,11 @@ double tiles_down(const ProductArgs &a, int32_t rows) {
   return used + (more > 0 ? more : 0);
 }
 template <int N>
-Kernel least(const ProductArgs &a, const Cost (&costs)[N]) {
+Kernel least(const ProductArgs &a, bool f32, const Cost (&costs)[N]) {
   Kernel best = costs[0].kernel;
   double least = 1e300;
   for (const Cost &c : costs) {
-    const double us = turns_of(tiles_down(a, c.rows) * (double)divide_up(a.out_width, c.columns), c.at_once) * (c.a * a.inp / 1024 + c.f);
+    const double us = turns_of(tiles_down(a, c.rows) * (double)divide_up(a.out_width, c.columns), f32) * (c.a * a.inp / 1024 + c.f);
     if (us < least) least = us, best = c.kernel;
   }
   return best;
@@ -704,7 +705,7 @@ Kernel choose(const ProductArgs &a, bool f32) {
     if (a.slots <= (f32 ? used * 5 / 2 : used * 4)) return kFew8;
     if (a.slots <= (f32 ? used * 8 : used * 16) && wide <= 512) return kFew16;
   }
-  return f32 ? least(a, kCostF32) : least(a, kCostBf16);
+  return f32 ? least(a, true, kCostF32) : least(a, false, kCostBf16);
 }
 
 template <typename S, typename TO>
@@ -745,9 +746,9 @@ int run_product(const ProductArgs &a, __bf16, hipStream_t s) {
     case kTile64: return run_tiles<Shape<T, 2, 2, 1, 1, 4, 3>, TO>(a, s);
     case kTile64x128: return run_tiles<Shape<T, 2, 2, 1, 2, 2, 4>, TO>(a, s);
     case kTile128: return run_tiles<Shape<T, 4, 2, 1, 2, 2, 3>, TO>(a, s);
-    case kTile128x256: return run_tiles<Shape<T, 2, 4, 2, 2, 1, 3>, TO>(a, s);
-    case kTile128x256Pair: return run_tiles<Shape<T, 4, 4, 1, 2, 1, 3>, TO>(a, s);      // (two waves, and two such workgroups a compute unit)
-    case kTile256: return run_tiles<Shape<T, 4, 4, 2, 2, 1, 3>, TO>(a, s);
+    case kTile128x256: return run_tiles<Shape<T, 4, 2, 1, 4, 1, 3>, TO>(a, s);
+    case kTile128x256K: return run_tiles<Shape<T, 4, 2, 1, 4, 2, 3>, TO>(a, s);
+    case kTile256: return run_tiles<Shape<T, 4, 2, 2, 4, 1, 3>, TO>(a, s);
     default: return NVFP4_ERR_UNSUPPORTED;       // (not among the costs)
   }
 }
@@ -762,7 +763,9 @@ int run_product(const ProductArgs &a, float, hipStream_t s) {
     case kTile64: return run_tiles<Shape<T, 2, 2, 1, 1, 4, 2>, TO>(a, s);
     case kTile64x128: return run_tiles<Shape<T, 2, 2, 1, 2, 2, 3>, TO>(a, s);
     case kTile64x256: return run_tiles<Shape<T, 2, 4, 1, 2, 1, 3>, TO>(a, s);
+    case kTile64x256K: return run_tiles<Shape<T, 2, 4, 1, 2, 2, 2>, TO>(a, s);
     case kTile128x256: return run_tiles<Shape<T, 2, 4, 2, 2, 1, 3>, TO>(a, s);
+    case kTile256: return run_tiles<Shape<T, 2, 4, 4, 2, 1, 2>, TO>(a, s);
     default: return NVFP4_ERR_UNSUPPORTED;
   }
 }
