@@ -47,13 +47,13 @@ struct ProductArgs {
 // ---- pieces -------------------------------------------------------------------------------------------------------------
 
 // v as a sum of three BF16 terms, eight of its 24 bits each, exactly.  (Below 2^-110 BF16 has no numbers for all three.)  Of an infinity the first
-// term is all there is: a weight is finite, so that what the others, 0, add is 0.  Of a NaN the second is one too.
+// term is all there is: a weight is finite, so that what the others, 0, add is 0.  Of a NaN the rest is one.
 __device__ inline void terms_of(float v, float (&t)[3]) {
   const auto cut = [](float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); };
   t[0] = cut(v);
   const float rest = t[0] == v ? 0.0f : v - t[0];
   t[1] = cut(rest);
-  t[2] = rest == t[1] ? 0.0f : rest - t[1];
+  t[2] = rest - t[1];
 }
 
 // Two fp32 numbers that are BF16 numbers, in one word.
@@ -586,6 +586,16 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_tiles(ProductArgs a, int32_t
           for (int j = 0; j < WN; ++j) multiply(i, j);
 #pragma unroll
         for (int j = 0; j < WN; ++j) expand_b((s + 1) & 3, j);
+        if constexpr (kTerms == 3) {             // (the next step's terms and fragments among this one's matrix instructions)
+          constexpr int kAll = 3 * WM * WN, kEach = (64 * WM + 20 * WN + kAll - 1) / kAll;
+          __builtin_amdgcn_sched_group_barrier(0x100, 2 * WM + 2 * WN, 0);
+#pragma unroll
+          for (int q = 0; q < kAll; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, kEach, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
     freed = stage;
@@ -652,7 +662,7 @@ bool sizes_fit(const nvfp4_product_params &p) {
 // experts, 1024 x 2560, 7.3 / 11.2; but 200 of 32, 3216 x 256, 20 / 17.7 and 1024 of 64, 1024 x 2048, 54 / 34.5.)
 // Else k_tiles in the shape that takes least by the estimate below: turns of tiles over the 256 compute units, each a + f microseconds for 1024 of K and
 // besides.  The constants are fitted to 230 products, up to 8192 tokens, K 256 to 8192, up to 16384 columns, 1 to 128 experts (uneven), each
-// in all shapes: the choice is 1.8 % (fp32: 1.9 %) slower than the best of each on average.  (us at K = 8192 for up to one turn / 4096 x 8192 x 8192, BF16: 32 x 32
+// in all shapes: the choice is 2.2 % (fp32: 0.4 %) slower than the best of each on average.  (us at K = 8192 for up to one turn / 4096 x 8192 x 8192, BF16: 32 x 32
 // 14 / 1374, 64 x 32 23 / 1112, 64 x 64 30 / 835, 64 x 128 47.5 / 740, 128 x 128 55 to 70 / 510, 128 x 256 100 / 448, in two parts of K
 // 84 / 450, 256 x 256 144 / 411 to 428.  A wave of 128 x 64 expands least and leaves room for a second one on its SIMD: waves of 128 x 128 one by one took 160 /
 // 418 to 435, of 64 x 128 in tiles of 128 x 256 122 / 505.)
@@ -663,19 +673,21 @@ enum Kernel { kFew4, kFew8, kFew16, kTile32, kTile64x32, kTile64, kTile64x128, k
 struct Cost {
   Kernel kernel;
   int32_t rows, columns;
+  bool pair;                   // two workgroups fit a compute unit's LDS: then the last turn costs half of what is missing in it, else all
   double a, f;                 // us a turn: for 1024 of K, and besides
 };
-constexpr Cost kCostBf16[] = {{kTile32, 32, 32, 0.98, 3.9},        {kTile64x32, 64, 32, 1.92, 3.8},       {kTile64, 64, 64, 3.07, 4.3},
-                              {kTile64x128, 64, 128, 5.8, 4.6},    {kTile128, 128, 128, 8.0, 6.6},        {kTile128x256K, 128, 256, 12.0, 11.0},
-                              {kTile128x256, 128, 256, 13.4, 6.8}, {kTile256, 256, 256, 21.4, 18.0}};
-constexpr Cost kCostF32[] = {{kTile32, 32, 32, 3.8, 2.7},          {kTile64, 64, 64, 9.5, 5.5},           {kTile64x128, 64, 128, 16.3, 6.1},
-                             {kTile64x256K, 64, 256, 21.6, 8.5},   {kTile64x256, 64, 256, 23.6, 7.5},     {kTile128x256, 128, 256, 41.4, 11.1},
-                             {kTile256, 256, 256, 75.7, 10.3}};
+constexpr Cost kCostBf16[] = {{kTile32, 32, 32, false, 0.96, 3.8},       {kTile64x32, 64, 32, false, 1.86, 3.7},
+                              {kTile64, 64, 64, false, 3.02, 4.3},       {kTile64x128, 64, 128, false, 5.7, 4.5},
+                              {kTile128, 128, 128, false, 7.3, 6.5},     {kTile128x256K, 128, 256, false, 12.0, 8.7},
+                              {kTile128x256, 128, 256, true, 12.6, 6.8}, {kTile256, 256, 256, false, 21.4, 15.0}};
+constexpr Cost kCostF32[] = {{kTile32, 32, 32, true, 3.5, 2.7},          {kTile64, 64, 64, false, 8.6, 5.3},
+                             {kTile64x128, 64, 128, false, 14.1, 5.9},   {kTile64x256K, 64, 256, false, 19.9, 8.3},
+                             {kTile64x256, 64, 256, true, 24.1, 7.8},    {kTile128x256, 128, 256, false, 39.2, 10.5}};
 
-// The last turn is nearly as long as a full one; of fp32 tiles, which leave a compute unit room for no second one, as long.
-double turns_of(double tiles, bool f32) {
-  const double t = tiles / 256;
-  return t <= 1 ? 1 : f32 ? std::ceil(t) : t + 0.75 * (std::ceil(t) - t);
+// (of several experts' tiles, whose number follows from what the router did, a tenth more may well begin another turn)
+double turns_of(double tiles, bool pair, bool several) {
+  const double t = tiles / 256, whole = std::ceil(several ? 1.1 * t : t);
+  return whole <= 1 ? 1 : pair ? (t + whole) / 2 : whole;
 }
 // Tiles down the rows: half a tile of every expert's is empty on average, and each that has rows has one.
 double tiles_down(const ProductArgs &a, int32_t rows) {
@@ -684,11 +696,11 @@ double tiles_down(const ProductArgs &a, int32_t rows) {
   return used + (more > 0 ? more : 0);
 }
 template <int N>
-Kernel least(const ProductArgs &a, bool f32, const Cost (&costs)[N]) {
+Kernel least(const ProductArgs &a, const Cost (&costs)[N]) {
   Kernel best = costs[0].kernel;
   double least = 1e300;
   for (const Cost &c : costs) {
-    const double us = turns_of(tiles_down(a, c.rows) * (double)divide_up(a.out_width, c.columns), f32) * (c.a * a.inp / 1024 + c.f);
+    const double us = turns_of(tiles_down(a, c.rows) * (double)divide_up(a.out_width, c.columns), c.pair, a.experts > 1) * (c.a * a.inp / 1024 + c.f);
     if (us < least) least = us, best = c.kernel;
   }
   return best;
@@ -705,7 +717,7 @@ Kernel choose(const ProductArgs &a, bool f32) {
     if (a.slots <= (f32 ? used * 5 / 2 : used * 4)) return kFew8;
     if (a.slots <= (f32 ? used * 8 : used * 16) && wide <= 512) return kFew16;
   }
-  return f32 ? least(a, true, kCostF32) : least(a, false, kCostBf16);
+  return f32 ? least(a, kCostF32) : least(a, kCostBf16);
 }
 
 template <typename S, typename TO>
@@ -765,7 +777,6 @@ int run_product(const ProductArgs &a, float, hipStream_t s) {
     case kTile64x256: return run_tiles<Shape<T, 2, 4, 1, 2, 1, 3>, TO>(a, s);
     case kTile64x256K: return run_tiles<Shape<T, 2, 4, 1, 2, 2, 2>, TO>(a, s);
     case kTile128x256: return run_tiles<Shape<T, 2, 4, 2, 2, 1, 3>, TO>(a, s);
-    case kTile256: return run_tiles<Shape<T, 2, 4, 4, 2, 1, 2>, TO>(a, s);
     default: return NVFP4_ERR_UNSUPPORTED;
   }
 }

@@ -174,7 +174,7 @@ for T in (1, 10, 100, 1000, 5000):
 
 def test_no_kernel_spills():
     """The products count their copies by hand: a spill would add memory instructions of the compiler's own to the counts."""
-    for source, least in (("weight_product.hip", 54), ("experts.hip", 42)):
+    for source, least in (("weight_product.hip", 52), ("experts.hip", 42)):
         kernels = {k: v for k, v in _report(source).items() if "LDS" in v}
         assert len(kernels) >= least, (source, len(kernels))
         spilled = {k: v["ScratchSize"] for k, v in kernels.items() if v["ScratchSize"]}

@@ -55,5 +55,5 @@ for T, k, W in {ROWS + ROWS_LARGE!r}:
     base = int(re.search(r"(\w+) T nvfp4_distill_step$", out, flags=re.M).group(1), 16)
     known = _kernels()
     reached = {known[base + at] for at in launched}
-    assert len(known) == 54 + 42
+    assert len(known) == 52 + 42
     assert reached == set(known.values()), "\n".join(sorted(set(known.values()) - reached))

@@ -61,7 +61,7 @@ SIZES = [  # T, K, N, tiles
     (1000, 2048, 2049, False), (1025, 1024, 3008, True), (2049, 608, 1023, False),
     (2, 256, 100, False), (4, 96, 64, True), (6, 512, 72, False), (7, 224, 60, False), (9, 256, 40, False), (12, 96, 300, False), (13, 768, 144, True),
     (48, 512, 8192, False), (60, 96, 1000, False), (300, 2048, 4096, True), (2049, 608, 4096, False), (4096, 256, 4096, True),
-    (4000, 1056, 3000, False), (500, 4096, 9001, False),
+    (4000, 1056, 3000, False), (500, 4096, 9001, False), (3900, 2080, 4096, True),
 ]
 
 
