@@ -139,8 +139,9 @@ int nvfp4_distill_step(const void *logits, const nvfp4_distill_params *p, const 
  *
  *   out[s][n] = alpha sum_k x[row(s)][k] value(code[n][k]) value(scale[n][k / 16])
  *
- * A weight's value without alpha has six significant bits at most and is exact in BF16, fp32 activations are sums of three BF16 terms, so
- * products are exact; sums are fp32's, in a fixed order that depends on sizes alone.  For the gradient dx = dy W pass the packing
+ * A weight's value without alpha has six significant bits at most and is exact in BF16, fp32 activations are sums of three BF16 terms (all 24
+ * bits from 2^-110 up; below, what is less than 2^-133 is lost), so products are exact; sums are fp32's, in a fixed order that depends on sizes
+ * alone.  For the gradient dx = dy W pass the packing
  * of the transposed weight (columnwise codes and scales; with block2d they hold the same values).
  *
  * nvfp4_experts_product does so with a weight for each expert: the rows begin[e] .. begin[e + 1] - 1 of out are expert e's.  A row behind

@@ -313,8 +313,9 @@ struct Shape {
   static constexpr int UA = CK * (int)sizeof(T) / 16, UB = CK / 32;       // 16-byte units of a row of x, of codes (= pairs of scales)
   static constexpr uint32_t kCodes = BM * UA * 16, kScales = kCodes + BN * UB * 16, kStage = kScales + BN * UB * 4;
   static constexpr int NA = BM * UA / 64 / kWaves, NB = BN * UB / 64 / kWaves, kCopies = NA + 2 * NB;     // copy instructions of a wave
-  static constexpr int kPitch = BN + 4;          // of the sums on their way out, in floats; 32 rows of every wave at a time
-  static constexpr uint32_t kSums = KS * SM * 32 * kPitch * 4;
+  // the sums on their way out, 32 rows of every wave at a time: floats from row to row, of a wave by itself where it has all of K, else of all of them
+  static constexpr int kPitch = KS == 1 ? 32 * WN + 4 : BN + 4;
+  static constexpr uint32_t kSums = (KS == 1 ? SM * SN : KS * SM) * 32 * kPitch * 4;
   static constexpr uint32_t kLds = NST * kStage > kSums ? NST * kStage : kSums;
   static_assert(BM * UA % (64 * kWaves) == 0 && BN * UB % (64 * kWaves) == 0 && 64 % UA == 0 && 64 % UB == 0, "whole copies");
   static_assert(kLds <= 160 * 1024 && (NST - 2) * kCopies < 63, "LDS; vmcnt counts to 63");
@@ -605,38 +606,61 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_tiles(ProductArgs a, int32_t
 
   // ---- sums -> LDS -> out, 32 rows of every wave at a time: the operands were exchanged in the matrix instruction, so that four
   // accumulators are adjacent columns
-  constexpr int G = sizeof(TO) == 4 ? 4 : 8, kRows = 32 * S::SM, kPieces = kRows * S::BN / G;
+  constexpr int G = sizeof(TO) == 4 ? 4 : 8;
   float *const sums = reinterpret_cast<float *>(lds);
-#pragma unroll
-  for (int i = 0; i < WM; ++i) {
-    if (i) __syncthreads();
+  const auto put = [&](float *to, int pitch, int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < WN; ++j)
 #pragma unroll
       for (int v = 0; v < 16; v += 4)
-        *reinterpret_cast<f32x4 *>(sums + (kg * kRows + wm * 32 + line) * S::kPitch + (wn * WN + j) * 32 + 2 * v + 4 * half) =
+        *reinterpret_cast<f32x4 *>(to + line * pitch + j * 32 + 2 * v + 4 * half) =
             f32x4{acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]};
-    __syncthreads();
+  };
+  // G columns of row m, times alpha (lines of out begin wherever its stride puts them)
+  const auto store = [&](int32_t m, int32_t col, const f32x4 (&v)[G / 4]) __attribute__((always_inline)) {
+    if (m >= rows_m || col >= rows_n) return;
+    typedef TO piece_of __attribute__((ext_vector_type(G)));
+    typedef piece_of piece_anywhere __attribute__((aligned(sizeof(TO))));
+    TO *const to = out + (int64_t)m * a.ld_out + col;
+    const bool is = is_row[m];
+    piece_of p;
+    for (int g = 0; g < G; ++g) p[g] = (TO)(is ? v[g / 4][g % 4] * alpha : 0.0f);
+    if (col + G <= rows_n) *reinterpret_cast<piece_anywhere *>(to) = p;
+    else
+      for (int g = 0; g < G; ++g)
+        if (col + g < rows_n) to[g] = p[g];
+  };
+  if constexpr (S::KS == 1) {                    // a wave by itself, without barriers: its LDS instructions run in their order
+    constexpr int kPitch = S::kPitch, kAcross = 32 * WN / G;
+    float *const own = sums + wave * (32 * kPitch);
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+      put(own, kPitch, i);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 4
+      for (int piece = lane; piece < 32 * kAcross; piece += 64) {
+        const int in = piece / kAcross, col = piece % kAcross * G;
+        f32x4 v[G / 4];
+        for (int g = 0; g < G / 4; ++g) v[g] = *reinterpret_cast<const f32x4 *>(own + in * kPitch + col + 4 * g);
+        store((wm * WM + i) * 32 + in, wn * (32 * WN) + col, v);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  } else {
+    constexpr int kRows = 32 * S::SM, kPieces = kRows * S::BN / G;
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+      if (i) __syncthreads();
+      put(sums + (kg * kRows + wm * 32) * S::kPitch + wn * (32 * WN), S::kPitch, i);
+      __syncthreads();
 #pragma unroll 2
-    for (int piece = (int)threadIdx.x; piece < kPieces; piece += S::kThreads) {
-      const int in = piece / (S::BN / G), col = piece % (S::BN / G) * G;
-      const int32_t m = in / 32 * (32 * WM) + i * 32 + in % 32;
-      f32x4 v[G / 4] = {};
-      for (int k = 0; k < S::KS; ++k)
-        for (int g = 0; g < G / 4; ++g) v[g] += *reinterpret_cast<const f32x4 *>(sums + (k * kRows + in) * S::kPitch + col + 4 * g);
-      const bool is = is_row[m];
-      for (int g = 0; g < G / 4; ++g) v[g] = is ? v[g] * alpha : f32x4{};
-      if (m >= rows_m || col >= rows_n) continue;
-      TO *const to = out + (int64_t)m * a.ld_out + col;
-      // (lines of out begin wherever its stride puts them)
-      typedef TO piece_of __attribute__((ext_vector_type(G)));
-      typedef piece_of piece_anywhere __attribute__((aligned(sizeof(TO))));
-      piece_of p;
-      for (int g = 0; g < G; ++g) p[g] = (TO)v[g / 4][g % 4];
-      if (col + G <= rows_n) *reinterpret_cast<piece_anywhere *>(to) = p;
-      else
-        for (int g = 0; g < G; ++g)
-          if (col + g < rows_n) to[g] = p[g];
+      for (int piece = (int)threadIdx.x; piece < kPieces; piece += S::kThreads) {
+        const int in = piece / (S::BN / G), col = piece % (S::BN / G) * G;
+        f32x4 v[G / 4] = {};
+        for (int k = 0; k < S::KS; ++k)
+          for (int g = 0; g < G / 4; ++g) v[g] += *reinterpret_cast<const f32x4 *>(sums + (k * kRows + in) * S::kPitch + col + 4 * g);
+        store(in / 32 * (32 * WM) + i * 32 + in % 32, col, v);
+      }
     }
   }
 }

@@ -273,3 +273,20 @@ def test_linear_layer_of_a_weight_alone(T):
         close(L.fprop(x, q, weight_only=True), ref, bound(x, w, q["alpha"], ref, x.dtype, torch.bfloat16))
         ref = q["alpha"].double() * (dy.double() @ w)
         close(L.dgrad(dy, q, 0, weight_only=True), ref, bound(dy, w.T, q["alpha"], ref, dy.dtype, torch.bfloat16))
+
+
+@pytest.mark.parametrize("T", [1, 40, 600])
+@pytest.mark.parametrize("exponent", [-60, -110, -118, -126, -133, -140])
+def test_the_least_numbers(T, exponent):
+    """BF16 activations down to the least subnormal number are exact; of fp32 ones what lies below BF16's least number, 2^-133, is lost: less
+    than that of each."""
+    K, N = 96, 24
+    codes, scales, alpha = weights(1, N, K, False)
+    alpha = alpha * 0 + 2.0 ** 60
+    w = values(codes[0], scales[0], False)
+    for dtype, lost in ((torch.bfloat16, 0.0), (torch.float32, 2.0 ** -133)):
+        x = (torch.rand((T, K), generator=torch.Generator().manual_seed(3)) * 2.0 ** exponent).to(dtype).cuda()
+        ref = alpha.double() * (x.double() @ w.T)
+        n = (3 if dtype == torch.float32 else 1) * K + 64
+        off = float(alpha) * ((2 * n * U * x.double().abs() + lost) @ w.abs().T) + 2 * U * ref.abs()
+        close(X.nvfp4_weight_product(x, codes[0], scales[0], alpha, out_dtype=B.OUT_F32), ref, off + U * ref.abs() + 2.0 ** -149)
