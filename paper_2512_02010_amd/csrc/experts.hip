@@ -11,6 +11,10 @@
 //   k_spread                x to its places
 //   k_combine               weighted sums of places
 //   k_combine_backward      both gradients, ys read once
+//
+// Among others, 16384 tokens of 4096 columns, four experts each, BF16: sort 11 us (two launches), spread 128 (671 MB: 5.2 TB/s, a copy 5.1), combine 139
+// (779 MB: 5.6); gradients of 5001 x 2880, eight each, 93 (479 MB); back from 5001 x 2880 fp32, six each, 82 (386 MB).  64 tokens: sort 4 us, spread 3.5,
+// the two calls 10.7 (the host's part of them).
 #include <hip/hip_runtime.h>
 
 #include "finetune/nvfp4_finetune.h"
@@ -112,8 +116,9 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs a) {
   for (int32_t g = threadIdx.x; g < groups; g += kSortThreads) a.counts[(int64_t)blockIdx.x * groups + g] = count[g];
 }
 
-// Stable counting sort.  A wave has an adjacent part of its workgroup's stretch, 64 pairs at a time: how many of each group (pass 0), then, from where
-// the group's first pair of the wave goes, every pair's place (pass 1).
+// Stable counting sort, bound by turns to memory one after the other: 256 pairs 3.9 us, 65536 4.7 for the counts and 6.5.  A wave has an adjacent part of
+// its workgroup's stretch, 64 pairs at a time: how many of each group (pass 0), then, from where the group's first pair of the wave goes, every
+// pair's place (pass 1).
 __global__ void __launch_bounds__(kSortThreads) k_sort(SortArgs a) {
   extern __shared__ int32_t counts[];            // [16][line]: each wave's pairs of a group, then where the next of them goes
   const int32_t groups = a.experts + 1, line = groups + 1;
@@ -238,6 +243,8 @@ __device__ inline Spot spot_of(const RowArgs &a) {
   return {(int32_t)blockIdx.x * (kRowThreads / a.lanes) + of, (int32_t)blockIdx.y * (a.lanes * U) + in};
 }
 
+// Bound by its stores.  A wave holds up to 64 U pieces of a token's row and writes them to one place after the other; a pair without an expert has a slot
+// of its own too, which its wave clears, so that no slot is left out and none written twice.
 template <typename TI, typename TO, int U, bool PAST>
 __global__ void __launch_bounds__(kRowThreads) k_spread(RowArgs a) {
   const Spot at = spot_of<U>(a);
@@ -273,6 +280,8 @@ __global__ void __launch_bounds__(kRowThreads) k_spread(RowArgs a) {
 
 constexpr int kAhead = 4;                        // places whose rows are on their way at once
 
+// Bound by its loads: the pieces of four places are on their way together (place by place, and through the caches, 16384 x 4096 took 178 us instead of
+// 132).  Slots of pairs without an expert are not read.
 template <typename TS, typename TT, int U, bool PAST>
 __global__ void __launch_bounds__(kRowThreads) k_combine(RowArgs a) {
   const Spot at = spot_of<U>(a);

@@ -4,6 +4,13 @@
 //
 // value(code) has two significant bits and value(scale) four: their product is exact in BF16, so that the BF16 matrix instruction multiplies
 // exact operands and accumulates in fp32.  fp32 activations are sums of three BF16 terms, a matrix instruction for each.
+//
+//   k_few      few rows: bound by the codes (0.5625 bytes a weight) and by x, which every workgroup reads from its die's L2
+//   k_tiles    tiles of out: bound by the matrix unit, and for large ones by the chip's power
+//
+// One launch a call.  Among others: 1 x 4096 x 4096 5.2 us (9.4 MB), 24 x 8192 x 8192 12.2 (37.7 MB of weights), 4096 x 8192 x 8192 411 to 445
+// (1.23 to 1.34 PFLOP/s; a BF16 product of the vendor's library, without a weight to expand, 424), 500 x 4096 x 10001 fp32 154 (three products: 0.8
+// PFLOP/s); 32 tokens, four each of 64 experts, 2048 to 1024, 15.5 (65 MB of weights: 4.2 TB/s), 4096 of 32, 2048 to 4096, 306 to 316 (0.86 PFLOP/s).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -109,7 +116,9 @@ __device__ inline const uint8_t *uniform(const uint8_t *p) {
 // Few rows: bound by the codes, which pass through a compute unit once.  A workgroup has 32 columns of out and an expert's rows, XR of them at a time; its W
 // waves share K, every W-th chunk of 256 each, and their sums meet in LDS.  A wave copies its chunks into a ring of NST stages of its own, eight
 // neighbouring lanes a column's 128 bytes of codes, 16 bytes of scales a lane (WHOLE: K is a multiple of 256; else two bytes at a time), two rows (one
-// of fp32) of x at a time, as many as there are.
+// of fp32) of x at a time, as many as there are.  Loads straight to registers, as the matrix instruction wants its operands, are 64 requests of 16
+// bytes each and took as long without any arithmetic: 8192 x 8192, one row 13.6 us (loads alone) to 14.4, 16 rows 18.3; through these copies 10.1 and 13.7
+// (the shapes that run_product names are the best of nine, by rows).
 template <typename T_, int XR_, int W_, int NST_, bool WHOLE_>
 struct FewShape {
   typedef T_ T;
@@ -136,7 +145,7 @@ __global__ void __launch_bounds__(S::W * 64) k_few(ProductArgs a) {
   const Rows r = behind ? Rows{rows_of(a, e - 1).last, a.slots} : rows_of(a, e);
   if (r.first >= r.last) return;
   if (behind || a.rows == 0) {
-    for (int32_t s = r.first + (int32_t)threadIdx.x / 32; s < r.last; s += W * 2)
+    for (int32_t s = r.first + (int32_t)(blockIdx.z * (W * 2) + threadIdx.x / 32); s < r.last; s += (int32_t)gridDim.z * (W * 2))
       if ((int32_t)threadIdx.x % 32 < rows_n) out[(int64_t)s * a.ld_out + threadIdx.x % 32] = (TO)0.0f;
     return;
   }
@@ -146,7 +155,7 @@ __global__ void __launch_bounds__(S::W * 64) k_few(ProductArgs a) {
   const float alpha = a.alpha[e];
   const uint8_t *const own = lds + wave * (NST * S::kStage);
   const uint32_t own_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + wave * (NST * S::kStage);
-  for (int32_t m0 = r.first; m0 < r.last; m0 += XR) {
+  for (int32_t m0 = r.first + (int32_t)blockIdx.z * XR; m0 < r.last; m0 += (int32_t)gridDim.z * XR) {
     const int32_t rows_m = r.last - m0 < XR ? r.last - m0 : XR, nx = (rows_m + RX - 1) / RX;
     // ---- where a lane's copies come from.  Unit u of a column stands at the place u ^ (column / 2 % 8), unit u of a row of x at u ^ (row % 16), so that
     // sixteen lanes that read a unit of sixteen lines meet all banks.
@@ -305,6 +314,13 @@ __global__ void __launch_bounds__(S::W * 64) k_few(ProductArgs a) {
 
 // A workgroup's tile of out is BM x BN; SM x SN waves hold WM x WN tiles of the matrix instruction (32 x 32) each, in KS copies that share K: copy kg
 // takes 64 of every chunk of 64 KS.  NST chunks of x, codes and scales are in LDS or on their way there.
+//
+// What bounds it.  A step of 16 of K is WM WN matrix instructions of 32 cycles and 17 vector instructions for each of WN fragments of the weight (four
+// conversions, eight multiplications, four packings, a scale; of fp32 also 60 for each of WM fragments of x); they overlap where the program
+// interleaves them: without, a turn of 256 x 256 at K = 8192 took 182 us, so 160, with two waves to a SIMD 144.  (Timing only, of the 160: with the weight not
+// expanded 155, without copies 144, neither 135; the matrix instructions alone would take 109 at 2.4 GHz.)  Of a full chip power is the bound:
+// 411 to 445 us for 4096 x 8192 x 8192, on different cards.  For short K what comes before and after the loop counts: finding the tile, the first chunks,
+// the sums' way out, 7 to 15 us a turn of large tiles.
 template <typename T_, int WM_, int WN_, int SM_, int SN_, int KS_, int NST_>
 struct Shape {
   typedef T_ T;
@@ -746,7 +762,10 @@ Kernel choose(const ProductArgs &a, bool f32) {
 
 template <typename S, typename TO>
 int run_few_of(const ProductArgs &a, hipStream_t s) {
-  const dim3 grid((uint32_t)divide_up(a.out_width, 32), (uint32_t)(a.experts + (a.begin ? 1 : 0)));
+  // More workgroups where one expert may have hundreds of rows, though the others then have few: 300 rows of one among 1024 would be 38 passes of a
+  // workgroup's.  (Those without a row end at once.)
+  const int64_t shares = a.begin && a.experts > 1 ? (a.slots < 4096 ? 1 + a.slots / 256 : 16) : 1;
+  const dim3 grid((uint32_t)divide_up(a.out_width, 32), (uint32_t)(a.experts + (a.begin ? 1 : 0)), (uint32_t)shares);
   // (the limit belongs to the kernel and not to the call, so it is always the same)
   if (S::kLds > 48 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k_few<S, TO>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)S::kLds) != hipSuccess)
