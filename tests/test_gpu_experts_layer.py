@@ -113,3 +113,16 @@ def test_recovering_with_activations_as_they_are():
     from paper_2512_02010_amd import recover
     losses, adapted, plain = recover.run(steps=3, weight_only=True)
     assert all(v == v and 0 <= v < 1e3 for v in losses) and adapted == adapted and plain == plain
+
+
+def test_without_tokens_and_without_rows():
+    """A batch of no tokens goes through the layer and back; rows of out whose x has no rows at all are 0."""
+    E, K, H, k = 3, 64, 96, 2
+    up, down = _layer(E, K, H, True)
+    x, ids, w = torch.empty((0, K), dtype=torch.bfloat16, device="cuda"), torch.empty((0, k), dtype=torch.int64, device="cuda"), torch.empty((0, k), device="cuda")
+    y, kept = X.feed_forward(x, ids, w, up, down)
+    dx, dw = X.feed_forward_backward(y, kept, w, up, down)
+    assert y.shape == dx.shape == (0, K) and dw.shape == (0, k) and kept[1].tolist() == [0] * (E + 1)
+    token, begin = torch.zeros(500, dtype=torch.int32, device="cuda"), torch.tensor([0, 5, 300, 400], dtype=torch.int32, device="cuda")
+    ys = X.experts_fprop(x, begin, up, token)
+    assert ys.shape == (500, H) and not bool(ys.any())
