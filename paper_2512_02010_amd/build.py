@@ -12,14 +12,15 @@ ROOT = PKG.parent
 # (source, extra defines, object name).  The quantizers' and the product's sources are compiled in
 # parts, side by side: part 0 holds the entry points, the others one group of kernels each (see the
 # sources for the grouping).  The slowest parts come first so that they start first.
-UNITS = [(PKG / "csrc" / "gemm.hip", {"NVFP4_46_GEMM_PART": part}, f"gemm.part{part}")
-         for part in (5, 1, 2, 3, 4)]
+UNITS = [(PKG / "csrc" / "weight_product.hip", {}, "weight_product")]
+UNITS += [(PKG / "csrc" / "gemm.hip", {"NVFP4_46_GEMM_PART": part}, f"gemm.part{part}")
+          for part in (5, 1, 2, 3, 4)]
 UNITS += [(PKG / "csrc" / "nvfp4_46.hip", {"NVFP4_46_PART": part}, f"nvfp4_46.part{part}")
           for part in range(1, 7)]
 UNITS += [(PKG / "csrc" / "gemm.hip", {"NVFP4_46_GEMM_PART": part}, f"gemm.part{part}")
           for part in (6, 0)]
 UNITS.append((PKG / "csrc" / "nvfp4_46.hip", {"NVFP4_46_PART": 0}, "nvfp4_46.part0"))
-UNITS += [(PKG / "csrc" / f"{name}.hip", {}, name) for name in ("adapters", "distill", "weight_product", "experts")]
+UNITS += [(PKG / "csrc" / f"{name}.hip", {}, name) for name in ("adapters", "distill", "experts")]
 SO = PKG / "libnvfp4_46.so"
 PYTHON_SO = PKG / "nvfp4_46_python.so"
 

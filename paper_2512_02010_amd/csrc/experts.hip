@@ -14,7 +14,7 @@
 //
 // Among others, 16384 tokens of 4096 columns, four experts each, BF16: sort 11 us (two launches), spread 128 (671 MB: 5.2 TB/s, a copy 5.1), combine 139
 // (779 MB: 5.6); gradients of 5001 x 2880, eight each, 93 (479 MB); back from 5001 x 2880 fp32, six each, 82 (386 MB).  64 tokens: sort 4 us, spread 3.5,
-// the two calls 10.7 (the host's part of them).
+// the two calls 8.1 (the host's part of them as long).
 #include <hip/hip_runtime.h>
 
 #include "finetune/nvfp4_finetune.h"

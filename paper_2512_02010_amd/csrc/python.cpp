@@ -8,6 +8,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <array>
 #include <cstring>
 
 #include <ATen/ATen.h>
@@ -813,6 +814,36 @@ PyObject *experts_product(PyObject *const *v, Py_ssize_t n) {
   return out.release();
 }
 
+// `n` int32 tensors of these sizes: by the caller's allocator one by one, else parts of one allocation that begin at multiples of 256 bytes (of
+// three and a workspace 4.2 us a call instead of 6.6).
+template <size_t n>
+std::array<PyObject *, n> int_tensors(const c10::SmallVector<int64_t, 2> (&sizes)[n], PyObject *like, PyObject *allocate) {
+  std::array<PyObject *, n> out{};
+  const auto release = [&] {
+    for (PyObject *o : out) Py_XDECREF(o);
+  };
+  try {
+    if (allocate != Py_None) {
+      for (size_t i = 0; i < n; ++i) out[i] = Owned(new_tensor(sizes[i], at::kInt, like, allocate)).release();
+      return out;
+    }
+    int64_t begin[n + 1] = {0};
+    for (size_t i = 0; i < n; ++i) begin[i + 1] = begin[i] + round_up(4 * c10::multiply_integers(sizes[i])) / 4;
+    const Owned all(new_tensor({begin[n]}, at::kInt, like, allocate));
+    const at::Tensor &whole = THPVariable_Unpack(all.o);
+    for (size_t i = 0; i < n; ++i) {
+      auto part = whole.unsafeGetTensorImpl()->shallow_copy_and_detach(c10::VariableVersion(0), false);
+      part->set_storage_offset(begin[i]);
+      part->set_sizes_contiguous(sizes[i]);
+      out[i] = Owned(THPVariable_Wrap(at::Tensor(std::move(part)))).release();
+    }
+  } catch (...) {
+    release();
+    throw;
+  }
+  return out;
+}
+
 // ids, experts, workspace or None, allocate, stream -> place, token, begin
 PyObject *experts_sort(PyObject *const *v, Py_ssize_t n) {
   expect(n, 5);
@@ -827,8 +858,8 @@ PyObject *experts_sort(PyObject *const *v, Py_ssize_t n) {
   const int64_t need = (int64_t)finetune.experts_workspace_bytes(&p);
   if (need == 0) run("nvfp4_experts_sort", [] { return (int)NVFP4_ERR_SHAPE; });          // (before anything of these sizes is made)
   const OnStream on(v[4], ids);
-  Owned place(new_tensor({p.tokens, p.top}, at::kInt, v[0], v[3])), token(new_tensor({p.tokens * p.top}, at::kInt, v[0], v[3])),
-      begin(new_tensor({p.experts + 1}, at::kInt, v[0], v[3]));
+  const auto made = int_tensors<3>({{p.tokens, p.top}, {p.tokens * p.top}, {p.experts + 1}}, v[0], v[3]);
+  const Owned place(made[0]), token(made[1]), begin(made[2]);
   auto *const pp = static_cast<int32_t *>(pointer(place.o)), *const pt = static_cast<int32_t *>(pointer(token.o)),
              *const pb = static_cast<int32_t *>(pointer(begin.o));
   // (the least workspace is one that the call leaves alone: any memory of its own will do, which saves an allocation)

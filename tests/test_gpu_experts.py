@@ -283,3 +283,26 @@ def test_outputs_that_do_not_fit_are_refused():
             call()
     with pytest.raises(B.Nvfp4Error, match="ALIGN"):
         X.nvfp4_experts_spread(x, place, out=torch.empty((8, 68), dtype=BF16, device="cuda")[:, :64])
+
+
+@pytest.mark.parametrize("T, k, E", [(1, 1, 1), (37, 3, 9), (64, 4, 64), (2000, 5, 100)])
+def test_outputs_that_the_calls_allocate_themselves(T, k, E, monkeypatch):
+    """As in a user's program (other tests hand in an allocator): the same values, in tensors that do not overlap and may be changed apart."""
+    ids, x, w = ids_of(T, k, E), slots_of(T, 1, 72, BF16), torch.rand((T, k), device="cuda")
+
+    def call():
+        place, token, begin = X.nvfp4_experts_sort(ids, E)
+        xs = X.nvfp4_experts_spread(x, place)
+        y = X.nvfp4_experts_combine(xs, place, w, base=x)
+        return (place, token, begin, xs, y, *X.nvfp4_experts_combine_backward(y, xs, place, w))
+
+    want = call()
+    monkeypatch.setattr(B, "OUTPUT_ALLOCATOR", B._device_empty)
+    got = call()
+    assert all(a.shape == b.shape and a.dtype == b.dtype and a.stride() == b.stride() and torch.equal(a, b) for a, b in zip(want, got))
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.nbytes) for t in got)
+    assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])) and all(t.data_ptr() % 256 == 0 for t in got)
+    kept = [t.clone() for t in got]
+    got[1].fill_(-7)
+    got[0].add_(1)
+    assert torch.equal(got[2], kept[2]) and bool((got[1] == -7).all()) and torch.equal(got[0], kept[0] + 1)
