@@ -753,7 +753,8 @@ Kernel choose(const ProductArgs &a, bool f32) {
     if (a.slots <= (f32 ? 2 : 4)) return kFew4;
     if (!f32 && a.slots <= 8) return kFew8;
     if (a.slots <= (f32 ? 12 : 16)) return kFew16;
-  } else {
+  } else if (a.inp > 512 || used * divide_up(a.out_width, 32) < 2048) {
+    // (else thousands of workgroups with a chunk or two for each wave: 512 rows of 128 experts, 2048 x 512, 45 us, in tiles of 128 x 256 35; 1024 x 2048 44 / 59)
     if (a.slots <= (f32 ? used * 5 / 2 : used * 4)) return kFew8;
     if (a.slots <= (f32 ? used * 8 : used * 16) && wide <= 512) return kFew16;
   }
@@ -762,10 +763,13 @@ Kernel choose(const ProductArgs &a, bool f32) {
 
 template <typename S, typename TO>
 int run_few_of(const ProductArgs &a, hipStream_t s) {
-  // More workgroups where one expert may have hundreds of rows, though the others then have few: 300 rows of one among 1024 would be 38 passes of a
-  // workgroup's.  (Those without a row end at once.)
-  const int64_t shares = a.begin && a.experts > 1 ? (a.slots < 4096 ? 1 + a.slots / 256 : 16) : 1;
-  const dim3 grid((uint32_t)divide_up(a.out_width, 32), (uint32_t)(a.experts + (a.begin ? 1 : 0)), (uint32_t)shares);
+  // More workgroups where one expert may have hundreds of rows, though the others then have few: 1024 rows of one among 256 would be 128 passes of a
+  // workgroup's.  Those without a row end at once, but thousands of them take time: 1024 rows of 256 experts, 1024 x 2048, with one / five shares 77 / 92 us
+  // evenly, 321 / 103 all of one expert.
+  const int64_t across = divide_up(a.out_width, 32), groups = a.experts + (a.begin ? 1 : 0);
+  const int64_t rows_shares = a.begin && a.experts > 1 ? 1 + a.slots / 256 : 1, room = 24576 / (across * groups);
+  const int64_t shares = rows_shares < room ? rows_shares : room > 0 ? room : 1;
+  const dim3 grid((uint32_t)across, (uint32_t)groups, (uint32_t)(shares < 16 ? shares : 16));
   // (the limit belongs to the kernel and not to the call, so it is always the same)
   if (S::kLds > 48 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k_few<S, TO>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)S::kLds) != hipSuccess)
