@@ -144,8 +144,8 @@ int nvfp4_distill_step(const void *logits, const nvfp4_distill_params *p, const 
  * alone.  For the gradient dx = dy W pass the packing
  * of the transposed weight (columnwise codes and scales; with block2d they hold the same values).
  *
- * nvfp4_experts_product does so with a weight for each expert: the rows begin[e] .. begin[e + 1] - 1 of out are expert e's.  A row behind
- * the last expert's, and one whose token is none of x's rows, is 0.
+ * nvfp4_experts_product does so with a weight for each expert: the rows begin[e] .. begin[e + 1] - 1 of out are expert e's.  A row in front
+ * of the first expert's or behind the last one's, and one whose token is none of x's rows, is 0.
  */
 typedef struct {
   int64_t rows;           /* rows of x, 0 .. 2^24 - 1                                                           */

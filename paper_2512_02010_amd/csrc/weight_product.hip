@@ -93,6 +93,15 @@ __device__ inline Rows rows_of(const ProductArgs &a, int32_t e) {
   last = last < first ? first : last < a.slots ? last : a.slots;
   return {first, last};
 }
+// Rows of out that no expert has, numbered through: those in front of the first one's, then those behind the last one's.
+struct Others {
+  int32_t front, skipped, count;
+  __device__ int32_t row(int32_t i) const { return i < front ? i : i + skipped; }
+};
+__device__ inline Others others_of(const ProductArgs &a) {
+  const int32_t front = rows_of(a, 0).first, last = rows_of(a, a.experts - 1).last, behind = last > front ? last : front;
+  return {front, behind - front, front + a.slots - behind};
+}
 
 // What a lane copies in place of x past the end of K (a weight's scale there is any finite number, so x has to be 0).
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
@@ -141,14 +150,15 @@ __global__ void __launch_bounds__(S::W * 64) k_few(ProductArgs a) {
   const int32_t e = (int32_t)blockIdx.y, n0 = (int32_t)blockIdx.x * 32, N = a.out_width, K = a.inp;
   TO *const out = static_cast<TO *>(a.out) + n0;
   const int32_t rows_n = N - n0 < 32 ? N - n0 : 32;
-  const bool behind = e == a.experts;            // the rows behind the last expert's
-  const Rows r = behind ? Rows{rows_of(a, e - 1).last, a.slots} : rows_of(a, e);
-  if (r.first >= r.last) return;
-  if (behind || a.rows == 0) {
-    for (int32_t s = r.first + (int32_t)(blockIdx.z * (W * 2) + threadIdx.x / 32); s < r.last; s += (int32_t)gridDim.z * (W * 2))
-      if ((int32_t)threadIdx.x % 32 < rows_n) out[(int64_t)s * a.ld_out + threadIdx.x % 32] = (TO)0.0f;
+  const bool none = e == a.experts;              // the rows that no expert has
+  const Rows r = none ? Rows{0, 0} : rows_of(a, e);
+  if (none || a.rows == 0) {
+    const Others o = none ? others_of(a) : Others{0, r.first, r.last - r.first};
+    for (int32_t i = (int32_t)(blockIdx.z * (W * 2) + threadIdx.x / 32); i < o.count; i += (int32_t)gridDim.z * (W * 2))
+      if ((int32_t)threadIdx.x % 32 < rows_n) out[(int64_t)o.row(i) * a.ld_out + threadIdx.x % 32] = (TO)0.0f;
     return;
   }
+  if (r.first >= r.last) return;
   const int32_t row_codes = K / 2, row_scales = K / 16, chunks = (K + 255) / 256;
   const uint8_t *const codes = uniform(a.codes + ((int64_t)e * N + n0) * row_codes);
   const uint8_t *const scales = uniform(a.scales + ((int64_t)e * (N >> a.scale_shift) + (n0 >> a.scale_shift)) * row_scales);
@@ -337,7 +347,7 @@ struct Shape {
   static_assert(kLds <= 160 * 1024 && (NST - 2) * kCopies < 63, "LDS; vmcnt counts to 63");
 };
 
-// A tile's rows: of expert e, or (e = experts) rows behind the last one's.
+// A tile's rows: of expert e, or (e = experts) numbers of those that no expert has.
 struct Unit {
   int32_t e, first, last;
 };
@@ -364,12 +374,12 @@ __device__ inline Unit unit_of(const ProductArgs &a, int32_t tiles_n, int32_t &n
     if (!tile_of(unit)) return {0, 0, 0};
     return {0, unit * BM, a.slots - unit * BM < BM ? a.slots : (unit + 1) * BM};
   }
-  // experts one after the other, each thread adjacent ones, the rows behind the last one's as one more
+  // experts one after the other, each thread adjacent ones, the rows that none has as one more
   const int32_t groups = a.experts + 1, per = (groups + THREADS - 1) / THREADS, g0 = (int32_t)threadIdx.x * per;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   const auto rows = [&](int32_t g) -> Rows {
     if (g < a.experts) return rows_of(a, g);
-    return {rows_of(a, a.experts - 1).last, a.slots};
+    return {0, others_of(a).count};
   };
   int32_t mine = 0;
   for (int32_t g = g0; g < g0 + per && g < groups; ++g) {
@@ -415,12 +425,14 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_tiles(ProductArgs a, int32_t
   if (unit.last <= unit.first) return;
   const int32_t N = a.out_width, K = a.inp, n0 = tile_n * S::BN, rows_m = unit.last - unit.first;
   const int32_t rows_n = N - n0 < S::BN ? N - n0 : S::BN;
-  TO *const out = static_cast<TO *>(a.out) + (int64_t)unit.first * a.ld_out + n0;
   if (unit.e == a.experts) {
+    const Others o = others_of(a);
+    TO *const rest = static_cast<TO *>(a.out) + n0;
     for (int32_t i = threadIdx.x; i < rows_m * S::BN; i += S::kThreads)
-      if (i % S::BN < rows_n) out[(int64_t)(i / S::BN) * a.ld_out + i % S::BN] = (TO)0.0f;
+      if (i % S::BN < rows_n) rest[(int64_t)o.row(unit.first + i / S::BN) * a.ld_out + i % S::BN] = (TO)0.0f;
     return;
   }
+  TO *const out = static_cast<TO *>(a.out) + (int64_t)unit.first * a.ld_out + n0;
   const auto row_of = [&](int32_t m) {           // of x; -1: none
     const int32_t s = unit.first + (m < rows_m ? m : rows_m - 1), from = a.token ? a.token[s] : s;
     return from >= 0 && from < a.rows ? from : -1;

@@ -41,7 +41,7 @@ def nvfp4_experts_product(x: torch.Tensor, begin: torch.Tensor, codes: torch.Ten
                           token: torch.Tensor | None = None, out_dtype: int = B.OUT_BF16, flags: int = 0,
                           out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """[S][N]: row s, begin[e] <= s < begin[e + 1], is x[token[s]] (x[s] without ``token``) times the weight of expert e; codes
-    [E][N][K/2], scales [E][N][K/16], alpha [E].  Rows behind begin[E] are 0."""
+    [E][N][K/2], scales [E][N][K/16], alpha [E].  Rows in front of begin[0] and from begin[E] on are 0."""
     return (_native or native()).experts_product(x, token, begin, codes, scales, alpha, out_dtype, flags, out, F._allocate(),
                                                  F._handle(stream))
 
