@@ -426,10 +426,13 @@ __global__ void __launch_bounds__(S::kThreads, 1) k_tiles(ProductArgs a, int32_t
   const int32_t N = a.out_width, K = a.inp, n0 = tile_n * S::BN, rows_m = unit.last - unit.first;
   const int32_t rows_n = N - n0 < S::BN ? N - n0 : S::BN;
   if (unit.e == a.experts) {
+    // (a begin that falls can make the count of tiles pass 32 bits and several threads find this one: only rows that there are)
     const Others o = others_of(a);
     TO *const rest = static_cast<TO *>(a.out) + n0;
-    for (int32_t i = threadIdx.x; i < rows_m * S::BN; i += S::kThreads)
-      if (i % S::BN < rows_n) rest[(int64_t)o.row(unit.first + i / S::BN) * a.ld_out + i % S::BN] = (TO)0.0f;
+    for (int32_t i = threadIdx.x; i < S::BM * S::BN; i += S::kThreads) {
+      const int32_t m = i / S::BN, n = i % S::BN;
+      if (m < rows_m && m < o.count - unit.first && n < rows_n) rest[(int64_t)o.row(unit.first + m) * a.ld_out + n] = (TO)0.0f;
+    }
     return;
   }
   TO *const out = static_cast<TO *>(a.out) + (int64_t)unit.first * a.ld_out + n0;

@@ -58,3 +58,15 @@ def test_a_span_of_the_experts():
             close(some[s], ref, off, (T, e))
             close(all_[s], ref, off, (T, e))
         assert not bool(some[:first].any()) and not bool(some[last:].any())
+
+
+def test_begins_that_fall_over_a_billion_rows():
+    """Every other expert claims all rows: their tiles, added up, pass 32 bits.  No result is promised, but nothing outside the result is
+    written (its margins are checked after the test)."""
+    S, E, K, N = 1 << 30, 1024, 32, 1
+    (codes, scales, alpha), x = weights(E, N, K, False), rows(8, K, torch.bfloat16)
+    token = torch.full((S,), 3, dtype=torch.int32, device="cuda")
+    for b in ([0, S] * 512 + [0], [S, 0] * 512 + [S], [S // 2, S, 0, S] * 256 + [S // 4]):
+        begin = torch.tensor(b, dtype=torch.int32, device="cuda")
+        assert X.nvfp4_experts_product(x, begin, codes, scales, alpha, token=token).shape == (S, N)
+        torch.cuda.synchronize()
