@@ -804,7 +804,9 @@ int run_tiles(const ProductArgs &a, hipStream_t s) {
                                                  (int)S::kLds) != hipSuccess)
     return NVFP4_ERR_HIP;
   const int64_t grid = divide_up(units * tiles_n, 8) * 8;
-  if (grid * S::kThreads > 0xffffffff) return NVFP4_ERR_UNSUPPORTED;             // (more threads than a launch has: an output of a terabyte)
+  // More threads than a launch has: a thousand experts of two million columns and more, whose rows may be few, or an output of a terabyte.  The grid of
+  // k_few has an axis for columns and one for experts.
+  if (grid * S::kThreads > 0xffffffff) return run_few<typename S::T, TO, (int)(32 / sizeof(typename S::T)), 8, 1>(a, s);
   return launch(k_tiles<S, TO>, dim3((uint32_t)grid), dim3(S::kThreads), S::kLds, s, a, (int32_t)tiles_n);
 }
 
