@@ -117,16 +117,20 @@ def experts_dgrad(dy, begin, q: dict, out_dtype: int = B.OUT_BF16) -> torch.Tens
 
 
 def feed_forward(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, up: dict, down: dict, base: torch.Tensor | None = None):
-    """y_t = base_t + sum_j weights[t][j] W_down relu(W_up x_t) of the experts ids[t][j], and what the backward pass needs."""
+    """y_t = base_t + sum_j weights[t][j] W_down relu(W_up x_t) of the experts ids[t][j], and what the backward pass needs.  The rows in between have
+    x's type."""
+    dtype = B.x_dtype_of(x)
     place, token, begin = nvfp4_experts_sort(ids, up["shape"][0])
-    h = experts_fprop(x, begin, up, token)
-    ys = experts_fprop(torch.relu(h), begin, down)
-    return nvfp4_experts_combine(ys, place, weights, base, out_dtype=B.x_dtype_of(x)), (place, begin, h, ys)
+    h = experts_fprop(x, begin, up, token, dtype)
+    ys = experts_fprop(torch.relu(h), begin, down, None, dtype)
+    return nvfp4_experts_combine(ys, place, weights, base, out_dtype=dtype), (place, begin, h, ys)
 
 
 def feed_forward_backward(dy: torch.Tensor, kept, weights: torch.Tensor, up: dict, down: dict):
-    """(dx, dweights) of ``feed_forward``; the experts' weights stay as they are, and base's gradient is dy."""
+    """(dx, dweights) of ``feed_forward``; the experts' weights stay as they are, and base's gradient is dy.  dx has dy's type, the rows in between that
+    of x."""
     place, begin, h, ys = kept
+    dtype = B.x_dtype_of(h)
     dys, dweights = nvfp4_experts_combine_backward(dy, ys, place, weights)
-    dh = experts_dgrad(dys, begin, down) * (h > 0)
-    return nvfp4_experts_combine(experts_dgrad(dh, begin, up), place, out_dtype=B.x_dtype_of(dy)), dweights
+    dh = experts_dgrad(dys, begin, down, dtype) * (h > 0)
+    return nvfp4_experts_combine(experts_dgrad(dh, begin, up, dtype), place, out_dtype=B.x_dtype_of(dy)), dweights
