@@ -132,5 +132,6 @@ def feed_forward_backward(dy: torch.Tensor, kept, weights: torch.Tensor, up: dic
     place, begin, h, ys = kept
     dtype = B.x_dtype_of(h)
     dys, dweights = nvfp4_experts_combine_backward(dy, ys, place, weights)
-    dh = experts_dgrad(dys, begin, down, dtype) * (h > 0)
+    # (not times the mask: a gradient that overflowed, times 0, would be NaN)
+    dh = experts_dgrad(dys, begin, down, dtype).masked_fill_(h <= 0, 0)
     return nvfp4_experts_combine(experts_dgrad(dh, begin, up, dtype), place, out_dtype=B.x_dtype_of(dy)), dweights

@@ -82,3 +82,25 @@ def test_a_base_of_another_type(dtype, other):
     for a, b in zip(made[torch.float32][:2], made[torch.bfloat16][:2]):
         assert torch.equal(a.bfloat16(), b)
     assert all(torch.equal(a, b) for a, b in zip(made[dtype][2:], made[other][2:]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [3, 200])
+def test_infinities_behind_the_activation_do_not_come_through(T, dtype):
+    """Where the activation is cut off its gradient is 0, also of a gradient that has overflowed: a token whose hidden columns are all negative
+    gets none, whatever comes back to it."""
+    E, K, H, k = 3, 64, 96, 2
+    g = torch.Generator().manual_seed(4)
+    up = X.quantize_experts((0.5 + torch.rand((E, H, K), generator=g)).cuda())
+    down = X.quantize_experts(torch.randn((E, K, H), generator=g).cuda())
+    x, dy = ((0.5 + torch.rand((T, K), generator=g)).to(dtype).cuda() for _ in range(2))
+    x[1] *= -1                                     # (positive weights: all of its hidden columns are negative, all others' positive)
+    ids, w = torch.randint(0, E, (T, k), generator=g).cuda(), 0.5 + torch.rand((T, k), generator=g).cuda()
+    y, kept = X.feed_forward(x, ids, w, up, down)
+    assert not bool(y[1].any())
+    want, _ = X.feed_forward_backward(dy, kept, w, up, down)
+    assert not bool(want[1].any()) and bool(want[0].any())
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        dy[1] = bad
+        dx, _ = X.feed_forward_backward(dy, kept, w, up, down)
+        assert torch.equal(dx, want), bad
