@@ -12,9 +12,10 @@
 //   k_combine               weighted sums of places
 //   k_combine_backward      both gradients, ys read once
 //
-// Among others, 16384 tokens of 4096 columns, four experts each, BF16: sort 11 us (two launches), spread 128 (671 MB: 5.2 TB/s, a copy 5.1), combine 139
-// (779 MB: 5.6); gradients of 5001 x 2880, eight each, 93 (479 MB); back from 5001 x 2880 fp32, six each, 82 (386 MB).  64 tokens: sort 4 us, spread 3.5,
-// the two calls 8.1 (the host's part of them as long).
+// Among others, 16384 tokens of 4096 columns, four experts each, BF16: sort 11 us (two launches), spread 128 (671 MB: 5.2 TB/s, a copy 5.1), combine 131 to 140
+// (779 MB: 5.6 to 5.9); gradients of 5001 x 2880, eight each, 93 (479 MB); back from 5001 x 2880 fp32, six each, 82 (386 MB).  64 tokens: sort 4 us, spread 3.5,
+// the two calls 7.8 to 9.7 (the host's part of them as long); 64 tokens of 4096 columns, eight each: combine 4.1, its gradients 9.9 (one place after the other);
+// gradients of 8192 tokens of 64 columns, eight each, 13.9.
 #include <hip/hip_runtime.h>
 
 #include "finetune/nvfp4_finetune.h"

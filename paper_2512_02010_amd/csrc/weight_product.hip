@@ -8,9 +8,11 @@
 //   k_few      few rows: bound by the codes (0.5625 bytes a weight) and by x, which every workgroup reads from its die's L2
 //   k_tiles    tiles of out: bound by the matrix unit, and for large ones by the chip's power
 //
-// One launch a call.  Among others: 1 x 4096 x 4096 5.2 us (9.4 MB), 24 x 8192 x 8192 12.2 (37.7 MB of weights), 4096 x 8192 x 8192 411 to 445
-// (1.23 to 1.34 PFLOP/s; a BF16 product of the vendor's library, without a weight to expand, 424), 500 x 4096 x 10001 fp32 154 (three products: 0.8
-// PFLOP/s); 32 tokens, four each of 64 experts, 2048 to 1024, 15.5 (65 MB of weights: 4.2 TB/s), 4096 of 32, 2048 to 4096, 306 to 316 (0.86 PFLOP/s).
+// One launch a call.  Among others, on different cards, rows x K x N: 1 x 4096 x 4096 5.2 to 5.6 us (9.4 MB), 24 x 8192 x 8192 11.9 to 12.9 (scales of tiles,
+// 33.8 MB of weights; of rows, 37.7 MB, 12.6), 4096 x 8192 x 8192 410 to 447 (1.23 to 1.34 PFLOP/s; a BF16 product of the vendor's library, without a
+// weight to expand, 410 to 424), 500 x 4096 x 10001 fp32 155 (three products: 0.8 PFLOP/s); 32 tokens, four each of 64 experts, 2048 to 1024, 15.3 to
+// 17.2 (65 MB of weights: 3.8 to 4.2 TB/s), 4096 of 32, 2048 to 4096, 306 to 325 (0.83 to 0.88 PFLOP/s).  fp32 activations and results: 1 x 4096 x 4096 9.1,
+// 4 x 8192 x 8192 17.7, 12 x 8192 x 8192 33, 32 tokens of 64 experts as above 35, 4096 of 32 914 (three products: 0.88 PFLOP/s).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -329,7 +331,7 @@ __global__ void __launch_bounds__(S::W * 64) k_few(ProductArgs a) {
 // conversions, eight multiplications, four packings, a scale; of fp32 also 60 for each of WM fragments of x); they overlap where the program
 // interleaves them: without, a turn of 256 x 256 at K = 8192 took 182 us, so 160, with two waves to a SIMD 144.  (Timing only, of the 160: with the weight not
 // expanded 155, without copies 144, neither 135; the matrix instructions alone would take 109 at 2.4 GHz.)  Of a full chip power is the bound:
-// 411 to 445 us for 4096 x 8192 x 8192, on different cards.  For short K what comes before and after the loop counts: finding the tile, the first chunks,
+// 410 to 447 us for 4096 x 8192 x 8192, on different cards.  For short K what comes before and after the loop counts: finding the tile, the first chunks,
 // the sums' way out, 7 to 15 us a turn of large tiles.
 template <typename T_, int WM_, int WN_, int SM_, int SN_, int KS_, int NST_>
 struct Shape {
@@ -711,7 +713,7 @@ bool sizes_fit(const nvfp4_product_params &p) {
 
 // ---- which kernel -----------------------------------------------------------------------------------------------------------
 //
-// Few rows for each expert: k_few, whose passes over an expert's weight stand one after the other, so that the rows of a pass decide.  (us, BF16, rows of
+// (Sizes here are rows x N x K, of experts rows and N x K.)  Few rows for each expert: k_few, whose passes over an expert's weight stand one after the other, so that the rows of a pass decide.  (us, BF16, rows of
 // a pass 4 / 8 / 16: 1 x 4096 x 4096 5.4 / 6.1 / 5.9, 4 x 15376 x 3584 9.3 / 10.3 / 11.8, 8 x 28672 x 4096 28 / 18.3 / 24, 16 x 8192 x 8192 30 / 19.6 / 13.7; 32
 // tokens of 4 among 64 experts, 1024 x 2048, 17.9 / 16.7 / 25.7.  Against the best tiles: 16 x 8192 x 8192 13.7 / 14, 28 x 480 x 512 5.4 / 4.8, 96 rows of 8
 // experts, 1024 x 2560, 7.3 / 11.2; but 200 of 32, 3216 x 256, 20 / 17.7 and 1024 of 64, 1024 x 2048, 54 / 34.5.)
@@ -779,8 +781,10 @@ Kernel choose(const ProductArgs &a, bool f32) {
 template <typename S, typename TO>
 int run_few_of(const ProductArgs &a, hipStream_t s) {
   // More workgroups where one expert may have hundreds of rows, though the others then have few: 1024 rows of one among 256 would be 128 passes of a
-  // workgroup's.  Those without a row end at once, but thousands of them take time: 1024 rows of 256 experts, 1024 x 2048, with one / five shares 77 / 92 us
-  // evenly, 321 / 103 all of one expert.
+  // workgroup's.  Those without a row end at once, but 8192 of them take 4 us and more, of every call, so that shares end where their workgroups pass 24576
+  // (us evenly / all of one expert, shares: 256 rows of 64 experts, N x K 1024 x 2048, one 20.6 / 80.6, two 20.8 / 50.9, five 24.7 / 26.4, it gets two, as many
+  // as 256 rows ask for; 1024 rows of 256, 1024 x 2048, one 80 / 322, two 84 / 219, five 97 / 103, it gets two).  So a batch of very many experts that is
+  // nearly all one's keeps most of its passes: 4096 rows of 1024 experts, 512 x 1024, gets one share, 99 / 915, where five would be 138 / 241.
   const int64_t across = divide_up(a.out_width, 32), groups = a.experts + (a.begin ? 1 : 0);
   const int64_t rows_shares = a.begin && a.experts > 1 ? 1 + a.slots / 256 : 1, room = 24576 / (across * groups);
   const int64_t shares = rows_shares < room ? rows_shares : room > 0 ? room : 1;
