@@ -713,7 +713,8 @@ bool sizes_fit(const nvfp4_product_params &p) {
 
 // ---- which kernel -----------------------------------------------------------------------------------------------------------
 //
-// (Sizes here are rows x N x K, of experts rows and N x K.)  Few rows for each expert: k_few, whose passes over an expert's weight stand one after the other, so that the rows of a pass decide.  (us, BF16, rows of
+// Sizes here are rows x N x K, of several experts rows, then N x K.
+// Few rows for each expert: k_few, whose passes over an expert's weight stand one after the other, so that the rows of a pass decide.  (us, BF16, rows of
 // a pass 4 / 8 / 16: 1 x 4096 x 4096 5.4 / 6.1 / 5.9, 4 x 15376 x 3584 9.3 / 10.3 / 11.8, 8 x 28672 x 4096 28 / 18.3 / 24, 16 x 8192 x 8192 30 / 19.6 / 13.7; 32
 // tokens of 4 among 64 experts, 1024 x 2048, 17.9 / 16.7 / 25.7.  Against the best tiles: 16 x 8192 x 8192 13.7 / 14, 28 x 480 x 512 5.4 / 4.8, 96 rows of 8
 // experts, 1024 x 2560, 7.3 / 11.2; but 200 of 32, 3216 x 256, 20 / 17.7 and 1024 of 64, 1024 x 2048, 54 / 34.5.)
